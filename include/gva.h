@@ -27,6 +27,9 @@
  * contrast workload.  A prompt is attended causally in one pass with
  * gva_prefill, or gva_prefill_absorb + gva_prefill_attention (gva_gqa_prefill_attention
  * for the matched GQA baseline).
+ * A value cache may be held in 4 bits (gva_q4_append_kv, gva_q4_decode_step,
+ * gva_q4_unpack_kv), and rows may be evicted from a cache by the attention
+ * weight that they drew (gva_accumulate_weights, gva_evict_rows).
  *
  * Conventions shared by every call
  * --------------------------------
@@ -462,6 +465,136 @@ int gva_pick_splits(const gva_dims* dims, int32_t max_len, int64_t total_len, in
  * invalid dims.  Pure host code; enqueues nothing.
  */
 int gva_prefer_fused(const gva_dims* dims, int32_t num_splits, int32_t split_rows, int32_t n_cu);
+
+/*
+ * ------------------------------------------------- a cache held in 4 bits
+ * The value cache as e2m1 codes (sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6)
+ * with one power-of-two scale byte per 32 columns of a row, 4.25 bits an
+ * element; the positional key cache stays bf16, in the layout above.
+ *   value   = code * 2^(byte - 127); byte 255: every element of the block NaN
+ *   byte    = e + 127, 2^e the smallest with amax <= 7 * 2^e, -119 <= e <= 125
+ *   code    = the nearest (ties to the even code; past 6 it saturates), with
+ *             the element's sign; a block that holds a NaN or an infinity is
+ *             stored as NaN throughout
+ * so an element is off by at most 2^e, and every value is exactly a bf16.
+ * v4_cache  B*G streams of T rows, d_v / 2 bytes a row, in blocks of 1 KB, R =
+ *           2048 / d_v rows each: column i of row t is in byte
+ *             (t/R)*1024 + ((i/P)*16 + t%16)*16 + (t%R/16)*8 + (i%P)/2,
+ *           P = d_v / 4, the low four bits for even i
+ * v4_scale  B*G streams of T rows, d_v / 32 bytes a row, in tiles of 32 rows:
+ *           the byte of columns 32 c .. of row t is
+ *             (t/32)*d_v + (c*16 + t%16)*2 + t%32/16
+ * Shapes: dtype bf16, d_v in {64, 128}, d_r a multiple of 8 (<= 64), T % 32 ==
+ * 0; others GVA_ERR_UNSUPPORTED.  Pointers 16-byte aligned (lens, seen, seq,
+ * row, pos, row_pos, lse and weights 4, kr_new 4).
+ *
+ * Rows and positions.  After an eviction (gva_evict_rows) a cache holds fewer
+ * rows than the sequence has had tokens.  `row` is a place in the cache, `pos`
+ * a token's position; `seen` [B] int32 counts the tokens of a sequence so far,
+ * the newest included, so that one stands at position seen[b] - 1.  Where pos
+ * is NULL it equals row, where seen is NULL it equals lens.  row_pos [B][T]
+ * int32 (optional) is the position of every cached row.
+ */
+
+/*
+ * gva_q4_append_kv -- gva_append_kv into a 4-bit cache.  For each r < n_rows,
+ * with b = seq[r], t = row[r], p = pos[r] (pos NULL: row[r]):
+ *   v4_cache, v4_scale [b][g][t] = v_new[r][g] in 4 bits, for every g < G
+ *   kr_cache[b][t]               = RoPE(kr_new[r], p)
+ *   row_pos[b][t]                = p    (row_pos may be NULL)
+ * Rows with b or t out of range are skipped; two rows naming the same (b, t)
+ * in one call race.  n_rows == 0 is a no-op.
+ */
+int gva_q4_append_kv(const gva_dims* dims, void* v4_cache, void* v4_scale, void* kr_cache, const void* v_new,
+                     const void* kr_new, const int32_t* seq, const int32_t* row, const int32_t* pos, int32_t n_rows,
+                     int32_t* row_pos, void* stream);
+
+/*
+ * gva_append_rows -- gva_append_kv (bf16 or fp32 caches) with the row apart
+ * from the position, for a cache that rows have been evicted from: arguments
+ * and rules as for gva_q4_append_kv, caches and new rows as for gva_append_kv.
+ */
+int gva_append_rows(const gva_dims* dims, void* v_cache, void* kr_cache, const void* v_new, const void* kr_new,
+                    const int32_t* seq, const int32_t* row, const int32_t* pos, int32_t n_rows, int32_t* row_pos,
+                    void* stream);
+
+/*
+ * gva_q4_unpack_kv -- the values of rows 0 .. lens[b]-1 of a 4-bit cache, into
+ * a bf16 v_cache in the tiled layout.  Later rows of v_cache are left as they
+ * were.  For a prompt over a 4-bit cache: gva_q4_append_kv its rows, unpack,
+ * then gva_prefill on the unpacked values and the same kr_cache (after an
+ * eviction gva_prefill_absorb with `seen` for its lens and a t_max of at least
+ * that, and gva_prefill_attention).
+ */
+int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_scale, const int32_t* lens,
+                     void* v_cache, void* stream);
+
+/*
+ * gva_q4_decode_workspace_size, gva_q4_decode_step -- gva_decode_step on a
+ * 4-bit cache that holds the current token's row already (gva_q4_append_kv):
+ * o and lse as there, with x_t over the values that the codes stand for and the
+ * query rotated at position seen[b] - 1.  d_c a multiple of 32 (32 .. 512), H/G
+ * in {1, 2, 4, 8}.  The caches are read only.  workspace: a caller-owned device
+ * buffer of at least the bytes reported for the same dims, num_splits and
+ * split_rows on the current device, 256-byte aligned, scratch.
+ * gva_q4_pick_splits -- gva_pick_splits for this step: a row has fewer
+ * bytes, so fewer and longer splits pay.
+ */
+int gva_q4_pick_splits(const gva_dims* dims, int32_t max_len, int64_t total_len, int32_t n_cu, int32_t* split_rows);
+int gva_q4_decode_workspace_size(const gva_dims* dims, int32_t num_splits, int32_t split_rows, size_t* bytes);
+int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const void* v4_cache, const void* v4_scale,
+                       const void* kr_cache, const int32_t* lens, const int32_t* seen, int32_t num_splits,
+                       int32_t split_rows, void* workspace, size_t workspace_bytes, float* o, float* lse,
+                       void* stream);
+
+/*
+ * ------------------------------------------------------------- eviction
+ * gva_weights_workspace_size, gva_accumulate_weights -- the attention weight
+ * that each cached row draws from a sequence's last n_new queries, summed over
+ * queries and heads and added to what it had:
+ *   new_weights[b][t] = decay * weights[b][t]
+ *                       + sum_{i < n_new} sum_h exp(x_{i,h,t} - lse[b][i][h]),  t < L_b
+ * with x the scaled score of gva_decode_attention, query i of sequence b at
+ * position seen[b] - n_new + i, seeing rows t <= L_b - n_new + i as in a
+ * prompt.  Rows from L_b on of new_weights are left as they were.  A query with
+ * lse -inf (nothing to see) adds nothing.  decay 0 reads no weights (NULL is
+ * allowed); new_weights may be weights itself, else it must not overlap it.
+ * q [B][n_new][H][d_c + d_r] and M in the storage dtype, lse [B][n_new][H] as
+ * the attention calls return it, weights [B][T] fp32.  n_new == 1 is a decode
+ * step's query, more are a window of a prompt's last ones (1 <= n_new <= T).
+ * v_cache is a bf16 or fp32 cache where v4_scale is NULL, else a 4-bit one.
+ * bf16 and 4-bit caches: d_v in {64, 128}, d_c a multiple of 32, d_r one of 8
+ * (<= 64); fp32: what the tiled layout takes.  Any H/G.  The sums have a
+ * fixed order.
+ */
+int gva_weights_workspace_size(const gva_dims* dims, int32_t n_new, size_t* bytes);
+int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, const void* m, const void* v_cache,
+                           const void* v4_scale, const void* kr_cache, const int32_t* lens, const int32_t* seen,
+                           const float* lse, double decay, const float* weights, float* new_weights, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * gva_evict_workspace_size, gva_evict_rows -- cut every sequence down to its
+ * n_keep rows of the largest weight.  Rows at positions below n_first or from
+ * seen[b] - n_recent on stay before all others (n_first + n_recent <= n_keep);
+ * the others go by weight, NaN last; of equal ones the lower row stays.
+ * new_lens[b] = min(L_b, n_keep).  The order of rows means nothing to the
+ * attention (keys are stored rotated), so the rows that stay in place are not
+ * moved: the k-th row below n_keep that goes is overwritten by the k-th row
+ * from n_keep on that stays, in all groups' values, the positional keys,
+ * weights and positions.  new_weights (and new_row_pos) are written whole: 0
+ * (-1) from new_lens[b] on.  Cache rows from new_lens[b] on keep what they
+ * held, and lens, weights and row_pos are not written: the call can be repeated.
+ * new_lens, new_weights and new_row_pos must not overlap their counterparts;
+ * row_pos and new_row_pos come together (NULL: position = row, as long as
+ * nothing has been evicted).  v_cache, v4_scale as for gva_accumulate_weights;
+ * every shape that the tiled layout (or the 4-bit one) takes.
+ */
+int gva_evict_workspace_size(const gva_dims* dims, size_t* bytes);
+int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_t n_recent, void* v_cache,
+                   void* v4_scale, void* kr_cache, const int32_t* lens, const int32_t* seen, const float* weights,
+                   const int32_t* row_pos, int32_t* new_lens, float* new_weights, int32_t* new_row_pos,
+                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a gva_status value (static storage). */
 const char* gva_status_string(int status);

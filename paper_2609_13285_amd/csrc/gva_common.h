@@ -39,7 +39,9 @@ struct AppendParams {
   const void* v_new;
   const void* kr_new;
   const int32_t* seq;
-  const int32_t* pos;
+  const int32_t* pos;           // the rotation's position
+  const int32_t* row;           // the place in the cache (NULL: pos)
+  int32_t* row_pos;             // optional: the positions of cached rows
   int32_t B, G, t_max, d_v, d_r, n_rows;
   const int32_t* block_table;   // paged caches (NULL: contiguous streams)
   int32_t page_rows, max_pages, n_pages;
@@ -545,6 +547,16 @@ inline int check_cache_layout(const gva_dims* d) {
   const double stream_bytes = (double)d->t_max * (double)(d->d_v > d->d_r ? d->d_v : d->d_r) * elem_size(d);
   if (stream_bytes >= 2147483648.0 - 16777216.0) return GVA_ERR_UNSUPPORTED;
   return GVA_OK;
+}
+
+// The shapes that the calls on a 4-bit cache take: bf16 queries, maps and new
+// rows; whole 32-row tiles; streams within 32-bit buffer offsets.
+inline int check_q4_dims(const gva_dims* d) {
+  const int st = check_dims(d);
+  if (st != GVA_OK) return st;
+  if (d->dtype != GVA_DTYPE_BF16 || (d->d_v != 64 && d->d_v != 128)) return GVA_ERR_UNSUPPORTED;
+  if (d->t_max % kTileRows != 0 || d->d_r % 8 != 0 || d->d_r > 64) return GVA_ERR_UNSUPPORTED;
+  return check_cache_layout(d);
 }
 
 inline void fill_inv_freq(const gva_dims* d, double* out) {

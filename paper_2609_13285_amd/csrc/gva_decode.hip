@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
   const int tid = threadIdx.x;
   const int npc = p.d_v / P;
   const int nvb = append_value_blocks(p.G, npc, KP);
+  const int32_t* const rows = p.row != nullptr ? p.row : p.pos;
   AppendPlace at;
   if ((int)blockIdx.y < nvb) {
     const int lane = tid & 63, n = lane & 15, qd = lane >> 4;
@@ -128,7 +129,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
 #pragma unroll
       for (int k = 0; k < KP; ++k)
         if (c0 + 4 * k < npc) piece[k] = src[c0 + 4 * k];
-      if (!append_place(p, p.seq[r], p.pos[r], at)) return;
+      if (!append_place(p, p.seq[r], rows[r], at)) return;
+      if (p.row_pos != nullptr && g == 0 && c0 == 0) p.row_pos[(int64_t)p.seq[r] * p.t_max + rows[r]] = p.pos[r];
       T* stream = static_cast<T*>(p.v_cache) + at.vstream0 + g * at.vstride + tiled_off<T>(at.row, c0 * P, p.d_v);
       constexpr int kStep = 4 * kLayoutRows * P; // elements between pieces c and c + 4 of a row
 #pragma unroll
@@ -146,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
   const T* kin = static_cast<const T*>(p.kr_new) + (int64_t)r * p.d_r + 2 * i;
   const double k0 = load_elem<T>(kin, 0), k1 = load_elem<T>(kin, 1);
   const int ps = p.pos[r];
-  if (!append_place(p, p.seq[r], ps, at)) return;
+  if (!append_place(p, p.seq[r], rows[r], at)) return;
   double y0, y1;
   rotate_pair(k0, k1, (double)ps * p.inv_freq[i], y0, y1);
   T* kstream = static_cast<T*>(p.kr_cache) + at.kstream0;
@@ -1667,14 +1669,15 @@ int absorb_impl(const gva_dims* dims, int n_per_seq, const void* q, const void* 
 
 int append_impl(const gva_dims* dims, const gva_paging* paging, const int32_t* block_table, void* v_cache,
                 void* kr_cache, const void* v_new, const void* kr_new, const int32_t* seq, const int32_t* pos,
-                int32_t n_rows, void* stream) {
+                int32_t n_rows, void* stream, const int32_t* row = nullptr, int32_t* row_pos = nullptr) {
   int st = check_dims(dims);
   if (st != GVA_OK) return st;
   if (n_rows < 0) return GVA_ERR_INVALID_ARG;
   if (n_rows == 0) return GVA_OK;
   if (!v_cache || !v_new || !seq || !pos) return GVA_ERR_INVALID_ARG;
   if (dims->d_r > 0 && (!kr_cache || !kr_new)) return GVA_ERR_INVALID_ARG;
-  if (!aligned(v_cache, 16) || !aligned(v_new, 16) || !aligned(seq, 4) || !aligned(pos, 4))
+  if (!aligned(v_cache, 16) || !aligned(v_new, 16) || !aligned(seq, 4) || !aligned(pos, 4) || !aligned(row, 4) ||
+      !aligned(row_pos, 4))
     return GVA_ERR_INVALID_ARG;
   if (dims->d_r > 0 && (!aligned(kr_cache, 16) || !aligned(kr_new, 4))) return GVA_ERR_INVALID_ARG;
   st = check_cache_layout(dims);
@@ -1686,6 +1689,8 @@ int append_impl(const gva_dims* dims, const gva_paging* paging, const int32_t* b
   p.kr_new = kr_new;
   p.seq = seq;
   p.pos = pos;
+  p.row = row;
+  p.row_pos = row_pos;
   p.B = dims->batch;
   p.G = dims->n_groups;
   p.t_max = dims->t_max;
@@ -1950,6 +1955,14 @@ int gva_append_kv(const gva_dims* dims, void* v_cache, void* kr_cache, const voi
                   const void* kr_new, const int32_t* seq, const int32_t* pos, int32_t n_rows,
                   void* stream) {
   return append_impl(dims, nullptr, nullptr, v_cache, kr_cache, v_new, kr_new, seq, pos, n_rows, stream);
+}
+
+int gva_append_rows(const gva_dims* dims, void* v_cache, void* kr_cache, const void* v_new, const void* kr_new,
+                    const int32_t* seq, const int32_t* row, const int32_t* pos, int32_t n_rows, int32_t* row_pos,
+                    void* stream) {
+  if (n_rows > 0 && row == nullptr) return GVA_ERR_INVALID_ARG;
+  return append_impl(dims, nullptr, nullptr, v_cache, kr_cache, v_new, kr_new, seq, pos != nullptr ? pos : row, n_rows,
+                     stream, row, row_pos);
 }
 
 int gva_absorb_query(const gva_dims* dims, const void* q, const void* m, const int32_t* lens,

@@ -1,0 +1,574 @@
+// libgva.so -- the attention weight that cached rows have drawn, and eviction
+// of rows by it.
+//
+// A row's weight is the sum, over the queries that saw it and over the heads,
+// of its softmax weight exp(x - lse), x the scaled score that the attention
+// calls use.  The streams of a sequence share one positional key per row and one
+// length, so rows are kept or evicted for all of its heads together.
+
+#include "gva_common.h"
+#include "gva_q4.h"
+
+namespace {
+
+// ========================================================= accumulate
+struct WeightParams {
+  const void* v;
+  const uint8_t* scales;
+  const void* kr;
+  const float* q_abs;     // [B][N][H][d_v], fp32
+  const float* q_rot;
+  const float* lse;       // [B][N][H]
+  const int32_t* lens;
+  const float* weights;   // may be NULL with decay 0
+  float* new_weights;
+  int32_t B, H, G, N, d_v, d_r, t_max, chunk;
+  float scale_log2, decay;
+};
+
+constexpr int kWeightWaves = 8;
+constexpr int kWeightChunk = 512;              // most rows of a workgroup
+
+// The workgroup takes `chunk` rows of one sequence.  Wave w scores group
+// w % GP of a round of GP = min(G, 8) groups (a power of two), every
+// (8 / GP)-th tile of the chunk; a column of the products is one (query, head of
+// the group) pair, its query once as bf16 high parts and once as low parts into
+// the same sums.  A lane adds the weights of its column; the sum over the 16
+// columns of a row goes to the wave's array of row sums, and the arrays are
+// added at the end in the order of the waves: the result does not depend on
+// timing.
+template <int DV, int NRC, bool Q4>
+__global__ void __launch_bounds__(64 * kWeightWaves) weights_bf16_kernel(WeightParams p) {
+  constexpr int NC = DV / 32, NS = DV / kScaleCols;
+  __shared__ float sums[kWeightWaves][kWeightChunk];
+  const int nchunks = (p.t_max + p.chunk - 1) / p.chunk;
+  const int item = xcd_remap(blockIdx.x, p.B * nchunks);
+  const int b = item / nchunks, r0 = item % nchunks * p.chunk;
+  const int L = clamp_len(p.lens, b, p.t_max);
+  if (r0 >= L) return;
+  const int r1 = min(r0 + p.chunk, L);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, qd = lane >> 4;
+  const int hpg = p.H / p.G, cols = p.N * hpg;
+  int GP = 1;
+  while (2 * GP <= min(p.G, kWeightWaves)) GP *= 2;
+  const int TS = kWeightWaves / GP;            // waves that share a group's tiles
+  float* const mine = sums[w];
+  for (int i = lane; i < p.chunk; i += 64) mine[i] = 0.f;
+  const int ntiles = (r1 - r0 + kTileRows - 1) / kTileRows;
+  const bf16x8 zero8 = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
+  const int r1k = (r1 + 15) / 16 * 16, r1c = (r1 + 31) / 32 * 32;
+  const __amdgpu_buffer_rsrc_t kres = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t*>(static_cast<const uint16_t*>(p.kr)) + (int64_t)b * p.t_max * p.d_r, (short)0, r1k * p.d_r * 2,
+      kBufferWord3);
+  for (int g = w % GP; g < p.G; g += GP) {
+    const int64_t stream = (int64_t)b * p.G + g;
+    const uint8_t* vbase = static_cast<const uint8_t*>(p.v) + stream * p.t_max * (Q4 ? DV / 2 : DV * 2);
+    const __amdgpu_buffer_rsrc_t vres = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(vbase), (short)0, Q4 ? r1c * (DV / 2) : r1k * DV * 2, kBufferWord3);
+    const __amdgpu_buffer_rsrc_t sres = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(Q4 ? p.scales + stream * p.t_max * NS : vbase), (short)0, r1c * NS, kBufferWord3);
+    for (int c0 = 0; c0 < cols; c0 += 16) {
+      const int col = c0 + n;
+      const bool active = col < cols;
+      const int qi = active ? col / hpg : 0;
+      const int64_t qrow = ((int64_t)b * p.N + qi) * p.H + g * hpg + (active ? col % hpg : 0);
+      const float ls = active ? p.lse[qrow] : -INFINITY;
+      const bool live = ls != -INFINITY;       // a query with nothing to see adds nothing
+      const int last = L - p.N + qi;           // the last row that the query sees
+      bf16x8 qh[NC], ql[NC], kh[NRC > 0 ? NRC : 1], kl[NRC > 0 ? NRC : 1];
+      const float* qa = p.q_abs + qrow * DV + qd * (Q4 ? DV / 4 : 8);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = active ? qa[(Q4 ? 8 : 32) * c + j] * p.scale_log2 : 0.f;
+        qh[c] = split_hi_lo(x, false);
+        ql[c] = split_hi_lo(x, true);
+      }
+#pragma unroll
+      for (int rc = 0; rc < NRC; ++rc) {
+        const bool in = active && 32 * rc + 8 * qd < p.d_r;
+        const float* qr = p.q_rot + qrow * p.d_r + min(32 * rc + 8 * qd, p.d_r - 8);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = in ? qr[j] * p.scale_log2 : 0.f;
+        kh[rc] = split_hi_lo(x, false);
+        kl[rc] = split_hi_lo(x, true);
+      }
+      const float init = live ? -ls * (float)kLog2e : 0.f;
+      for (int j = w / GP; j < ntiles; j += TS) {
+        const int row0 = r0 + j * kTileRows;
+        float sum[8];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          bf16x8 v[NC], k[NRC > 0 ? NRC : 1];
+          if constexpr (Q4) {
+            const unsigned sc2 = __builtin_amdgcn_raw_buffer_load_b16(sres, (qd * NS / 4 * 16 + n) * 2, row0 * NS, 0);
+            const unsigned byte = hf ? sc2 >> 8 & 255u : sc2 & 255u;
+            const u32x4 cw = __builtin_amdgcn_raw_buffer_load_b128(
+                vres, lane * 16 + (DV == 128 ? hf * kBlockBytes : 0), row0 * (DV / 2), 0);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) v[c] = dequant8(cw[DV == 128 ? c : 2 * hf + c], byte);
+          } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+              v[c] = as_bf16x8(__builtin_amdgcn_raw_buffer_load_b128(vres, qd * 256 + n * 16 + 1024 * c, (row0 + 16 * hf) * DV * 2, 0));
+          }
+#pragma unroll
+          for (int rc = 0; rc < NRC; ++rc)
+            k[rc] = as_bf16x8(__builtin_amdgcn_raw_buffer_load_b128(
+                kres, min(4 * rc + qd, p.d_r / 8 - 1) * 256 + n * 16, (row0 + 16 * hf) * p.d_r * 2, 0));
+          f32x4 sc = {init, init, init, init};
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            sc = mfma16(v[c], ql[c], sc);
+            sc = mfma16(v[c], qh[c], sc);
+          }
+#pragma unroll
+          for (int rc = 0; rc < NRC; ++rc) {
+            sc = mfma16(k[rc], kl[rc], sc);
+            sc = mfma16(k[rc], kh[rc], sc);
+          }
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) {
+            const int row = row0 + 16 * hf + 4 * qd + jj;
+            // (rows past the end may hold anything: they are selected away)
+            sum[4 * hf + jj] = live && row <= last && row < r1 ? __builtin_amdgcn_exp2f(sc[jj]) : 0.f;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] = sum16(sum[k]);
+        if (n == 0) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) mine[j * kTileRows + 16 * (k >> 2) + 4 * qd + (k & 3)] += sum[k];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < r1 - r0; i += 64 * kWeightWaves) {
+    float s = 0.f;
+#pragma unroll
+    for (int ww = 0; ww < kWeightWaves; ++ww) s += sums[ww][i];
+    const int64_t at = (int64_t)b * p.t_max + r0 + i;
+    p.new_weights[at] = p.decay != 0.f ? fmaf(p.decay, p.weights[at], s) : s;
+  }
+}
+
+// fp32 storage: the same on the fp32 products, 16-row tiles, any d_v and d_r
+// that the tiled layout takes.
+__global__ void __launch_bounds__(64 * kWeightWaves) weights_f32_kernel(WeightParams p) {
+  __shared__ float sums[kWeightWaves][kWeightChunk];
+  const int nchunks = (p.t_max + p.chunk - 1) / p.chunk;
+  const int item = xcd_remap(blockIdx.x, p.B * nchunks);
+  const int b = item / nchunks, r0 = item % nchunks * p.chunk;
+  const int L = clamp_len(p.lens, b, p.t_max);
+  if (r0 >= L) return;
+  const int r1 = min(r0 + p.chunk, L);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, qd = lane >> 4;
+  const int hpg = p.H / p.G, cols = p.N * hpg;
+  int GP = 1;
+  while (2 * GP <= min(p.G, kWeightWaves)) GP *= 2;
+  const int TS = kWeightWaves / GP;
+  float* const mine = sums[w];
+  for (int i = lane; i < p.chunk; i += 64) mine[i] = 0.f;
+  const int ntiles = (r1 - r0 + 15) / 16;
+  const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  const float* kr = static_cast<const float*>(p.kr) + (int64_t)b * p.t_max * p.d_r;
+  for (int g = w % GP; g < p.G; g += GP) {
+    const float* v = static_cast<const float*>(p.v) + ((int64_t)b * p.G + g) * p.t_max * p.d_v;
+    for (int c0 = 0; c0 < cols; c0 += 16) {
+      const int col = c0 + n;
+      const bool active = col < cols;
+      const int qi = active ? col / hpg : 0;
+      const int64_t qrow = ((int64_t)b * p.N + qi) * p.H + g * hpg + (active ? col % hpg : 0);
+      const float ls = active ? p.lse[qrow] : -INFINITY;
+      const bool live = ls != -INFINITY;
+      const int last = L - p.N + qi;
+      const float init = live ? -ls * (float)kLog2e : 0.f;
+      for (int j = w / GP; j < ntiles; j += TS) {
+        const int64_t row0 = r0 + j * 16;
+        f32x4 sc = {init, init, init, init};
+        auto add = [&](const float* stream, const float* query, int D) {
+          for (int c = 0; c < D; c += 16) {
+            const bool in = c + 4 * qd < D;
+            const f32x4 x = in ? *reinterpret_cast<const f32x4*>(stream + row0 * D + ((c / 4 + qd) * 16 + n) * 4) : zero4;
+            const f32x4 y = in && active ? *reinterpret_cast<const f32x4*>(query + c + 4 * qd) * p.scale_log2 : zero4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], sc, 0, 0, 0);
+          }
+        };
+        add(v, p.q_abs + qrow * p.d_v, p.d_v);
+        add(kr, p.q_rot + qrow * p.d_r, p.d_r);
+        float sum[4];
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          const int row = (int)row0 + 4 * qd + jj;
+          sum[jj] = sum16(live && row <= last && row < r1 ? __builtin_amdgcn_exp2f(sc[jj]) : 0.f);
+        }
+        if (n == 0) {
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) mine[j * 16 + 4 * qd + jj] += sum[jj];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < r1 - r0; i += 64 * kWeightWaves) {
+    float s = 0.f;
+#pragma unroll
+    for (int ww = 0; ww < kWeightWaves; ++ww) s += sums[ww][i];
+    const int64_t at = (int64_t)b * p.t_max + r0 + i;
+    p.new_weights[at] = p.decay != 0.f ? fmaf(p.decay, p.weights[at], s) : s;
+  }
+}
+
+using WeightFn = void (*)(WeightParams);
+
+template <bool Q4>
+WeightFn pick_weights(int dv, int nrc) {
+  const bool wide = dv == 128;
+  switch (nrc) {
+    case 0: return wide ? weights_bf16_kernel<128, 0, Q4> : weights_bf16_kernel<64, 0, Q4>;
+    case 1: return wide ? weights_bf16_kernel<128, 1, Q4> : weights_bf16_kernel<64, 1, Q4>;
+    case 2: return wide ? weights_bf16_kernel<128, 2, Q4> : weights_bf16_kernel<64, 2, Q4>;
+  }
+  return nullptr;
+}
+
+// =============================================================== evict
+struct EvictParams {
+  const int32_t* lens;
+  const int32_t* seen;
+  const float* weights;
+  const int32_t* row_pos;
+  int32_t* new_lens;
+  float* new_weights;
+  int32_t* new_row_pos;
+  int32_t* count;         // [B]: rows that move
+  int32_t* hole;          // [B][room]: the rows they go to, ascending
+  int32_t* move;          // [B][room]: and come from, ascending
+  int32_t B, t_max, keep, first, recent, room;
+};
+
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+
+// The order of rows: larger keys stay.  Protected rows before all, NaN
+// after all, -0 like +0.
+__device__ __forceinline__ unsigned evict_key(const EvictParams& p, int b, int t, int seen) {
+  const int64_t at = (int64_t)b * p.t_max + t;
+  const int pos = p.row_pos != nullptr ? p.row_pos[at] : t;
+  if (pos < p.first || (int64_t)pos >= (int64_t)seen - p.recent) return 0xFFFFFFFFu;
+  const float x = p.weights[at] + 0.f;
+  const unsigned u = __float_as_uint(x);
+  if (x != x) return 0u;
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// One workgroup per sequence.  Radix selection of the keep-th largest key, then
+// each wave goes over a contiguous segment of the rows.
+__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
+  __shared__ int hist[256];
+  __shared__ int pick_bin, pick_rest;
+  __shared__ int wave_n[2][kEvictWaves];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int L = clamp_len(p.lens, b, p.t_max);
+  const int seen = p.seen != nullptr ? p.seen[b] : L;
+  const int64_t base = (int64_t)b * p.t_max;
+  const int K = p.keep;
+  const int n_new = min(L, K);
+  if (tid == 0) p.new_lens[b] = n_new;
+  for (int t = n_new + tid; t < p.t_max; t += kEvictThreads) {
+    p.new_weights[base + t] = 0.f;
+    if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = -1;
+  }
+  if (L <= K) {
+    for (int t = tid; t < L; t += kEvictThreads) {
+      p.new_weights[base + t] = p.weights[base + t];
+      if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = p.row_pos[base + t];
+    }
+    if (tid == 0) p.count[b] = 0;
+    return;
+  }
+  unsigned prefix = 0u, mask = 0u;
+  int rest = K;                                // of the rows that match the prefix, the rest-th largest is the border
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int t = tid; t < L; t += kEvictThreads) {
+      const unsigned key = evict_key(p, b, t, seen);
+      if ((key & mask) == prefix) atomicAdd(&hist[key >> shift & 255u], 1);
+    }
+    __syncthreads();
+    if (w == 0) {                              // lane l: bins 255 - 4 l down to 252 - 4 l
+      int c[4], sum = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        c[k] = hist[255 - 4 * lane - k];
+        sum += c[k];
+      }
+      int above = wave_incl_scan(sum) - sum;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (above < rest && rest <= above + c[k]) {
+          pick_bin = 255 - 4 * lane - k;
+          pick_rest = rest - above;
+        }
+        above += c[k];
+      }
+    }
+    __syncthreads();
+    prefix |= (unsigned)pick_bin << shift;
+    mask |= 255u << shift;
+    rest = pick_rest;
+  }
+  // rows above the border stay, and the first `rest` of those on it
+  const int seg = ((L + kEvictWaves - 1) / kEvictWaves + 63) / 64 * 64;
+  const int s0 = min(w * seg, L), s1 = min(s0 + seg, L);
+  auto scan_waves = [&](int slot, int n) {     // the sum over the waves before this one
+    if (lane == 0) wave_n[slot][w] = n;
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < w; ++i) before += wave_n[slot][i];
+    return before;
+  };
+  const unsigned long long below = (1ull << lane) - 1ull;
+  int n_eq = 0;
+  for (int t0 = s0; t0 < s1; t0 += 64) {
+    const int t = t0 + lane;
+    n_eq += __popcll(__ballot(t < s1 && evict_key(p, b, t, seen) == prefix));
+  }
+  const int eq0 = scan_waves(0, n_eq);
+  auto kept_mask = [&](int t0, int& eq) {      // which rows t0 .. t0 + 63 stay
+    const int t = t0 + lane;
+    const unsigned key = t < s1 ? evict_key(p, b, t, seen) : 0u;
+    const bool on = t < s1 && key == prefix;
+    const unsigned long long m = __ballot(on);
+    const bool stay = t < s1 && (key > prefix || (on && eq + __popcll(m & below) < rest));
+    eq += __popcll(m);
+    return __ballot(stay);
+  };
+  int n_hole = 0, n_move = 0, eq = eq0;
+  for (int t0 = s0; t0 < s1; t0 += 64) {
+    const unsigned long long stay = kept_mask(t0, eq);
+    const bool in = t0 + lane < s1, low = t0 + lane < K;
+    n_hole += __popcll(__ballot(in && low) & ~stay);
+    n_move += __popcll(stay & __ballot(in && !low));
+  }
+  __syncthreads();
+  int hole0 = scan_waves(0, n_hole);
+  int move0 = scan_waves(1, n_move);
+  if (tid == kEvictThreads - 1) p.count[b] = move0 + n_move;
+  eq = eq0;
+  for (int t0 = s0; t0 < s1; t0 += 64) {
+    const unsigned long long stay = kept_mask(t0, eq);
+    const int t = t0 + lane;
+    const bool in = t < s1, low = t < K, me = stay >> lane & 1ull;
+    const unsigned long long hm = __ballot(in && low && !me), mm = __ballot(me && !low);
+    if (hm >> lane & 1ull) p.hole[(int64_t)b * p.room + hole0 + __popcll(hm & below)] = t;
+    if (mm >> lane & 1ull) p.move[(int64_t)b * p.room + move0 + __popcll(mm & below)] = t;
+    if (me && low) {
+      p.new_weights[base + t] = p.weights[base + t];
+      if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = p.row_pos[base + t];
+    }
+    hole0 += __popcll(hm);
+    move0 += __popcll(mm);
+  }
+}
+
+struct MoveParams {
+  const float* weights;
+  const int32_t* row_pos;
+  float* new_weights;
+  int32_t* new_row_pos;
+  const int32_t* count;
+  const int32_t* hole;
+  const int32_t* move;
+  uint8_t* v;
+  uint8_t* scales;
+  uint8_t* kr;
+  int32_t B, G, t_max, d_v, room;
+  int32_t v_pieces, kr_pieces;   // 16-byte pieces of a row in a tiled stream
+};
+
+// Rows move from at or past the budget to below it, so no row is both read and
+// written and the moves need no order.  A wave takes 16 moves of one stream,
+// lane (n, qd) pieces qd, qd + 4, ... of move n: moves next to each other come
+// from, and go to, nearby rows of a tile, whose pieces lie side by side.
+template <bool Q4>
+__global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
+  const int b = blockIdx.z, g = blockIdx.y;
+  const int lane = threadIdx.x & 63, n = lane & 15, qd = lane >> 4;
+  const int i = ((int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6)) * 16 + n;
+  if (i >= p.count[b]) return;
+  const int to = p.hole[(int64_t)b * p.room + i], from = p.move[(int64_t)b * p.room + i];
+  auto tiled = [&](uint8_t* stream, int pieces) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(stream) + (int64_t)(from / 16) * 16 * pieces + from % 16;
+    u32x4* dst = reinterpret_cast<u32x4*>(stream) + (int64_t)(to / 16) * 16 * pieces + to % 16;
+    for (int c = qd; c < pieces; c += 4) dst[c * 16] = src[c * 16];
+  };
+  if (g == p.G) {                              // what the groups share
+    if (p.kr_pieces > 0) tiled(p.kr + (int64_t)b * p.t_max * p.kr_pieces * 16, p.kr_pieces);
+    if (qd == 0) {
+      const int64_t base = (int64_t)b * p.t_max;
+      p.new_weights[base + to] = p.weights[base + from];
+      if (p.new_row_pos != nullptr) p.new_row_pos[base + to] = p.row_pos[base + from];
+    }
+    return;
+  }
+  const int64_t stream = (int64_t)b * p.G + g;
+  if constexpr (Q4) {
+    uint8_t* codes = p.v + stream * p.t_max * (p.d_v / 2);
+    if (p.d_v == 128)
+      *reinterpret_cast<u32x4*>(codes + code_off(to, qd, 128)) = *reinterpret_cast<const u32x4*>(codes + code_off(from, qd, 128));
+    else
+      *reinterpret_cast<u32x2*>(codes + code_off(to, qd, 64)) = *reinterpret_cast<const u32x2*>(codes + code_off(from, qd, 64));
+    uint8_t* sc = p.scales + stream * p.t_max * (p.d_v / kScaleCols);
+    if (qd < p.d_v / kScaleCols) sc[scale_off(to, qd, p.d_v)] = sc[scale_off(from, qd, p.d_v)];
+  } else {
+    tiled(p.v + stream * p.t_max * p.v_pieces * 16, p.v_pieces);
+  }
+}
+
+struct WeightLayout {
+  size_t q_rot, bytes;
+};
+
+int weight_layout(const gva_dims* d, int32_t n_new, WeightLayout& L) {
+  const int st = check_dims(d);
+  if (st != GVA_OK) return st;
+  if (n_new < 1 || n_new > d->t_max) return GVA_ERR_INVALID_ARG;
+  const size_t rows = (size_t)d->batch * n_new * d->n_heads;
+  L.q_rot = round256(rows * d->d_v * 4);
+  L.bytes = L.q_rot + round256(rows * d->d_r * 4);
+  return GVA_OK;
+}
+
+struct EvictLayout {
+  size_t hole, move, bytes;
+  int room;
+};
+
+int evict_layout(const gva_dims* d, EvictLayout& L) {
+  const int st = check_dims(d);
+  if (st != GVA_OK) return st;
+  L.room = d->t_max / 2 + 1;                   // at most min(keep, t_max - keep) rows move
+  L.hole = round256((size_t)d->batch * 4);
+  L.move = L.hole + round256((size_t)d->batch * L.room * 4);
+  L.bytes = L.move + round256((size_t)d->batch * L.room * 4);
+  return GVA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gva_weights_workspace_size(const gva_dims* dims, int32_t n_new, size_t* bytes) {
+  if (bytes == nullptr) return GVA_ERR_INVALID_ARG;
+  WeightLayout L;
+  const int st = weight_layout(dims, n_new, L);
+  if (st != GVA_OK) return st;
+  *bytes = L.bytes;
+  return GVA_OK;
+}
+
+int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, const void* m, const void* v_cache,
+                           const void* v4_scale, const void* kr_cache, const int32_t* lens, const int32_t* seen,
+                           const float* lse, double decay, const float* weights, float* new_weights, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  WeightLayout L;
+  int st = weight_layout(dims, n_new, L);
+  if (st != GVA_OK) return st;
+  if (!q || !m || !v_cache || !lens || !lse || !new_weights) return GVA_ERR_INVALID_ARG;
+  if (dims->d_r > 0 && !kr_cache) return GVA_ERR_INVALID_ARG;
+  if (!(decay >= 0.0) || !isfinite(decay) || (decay != 0.0 && !weights)) return GVA_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(m, 16) || !aligned(v_cache, 16) || !aligned(v4_scale, 16) || !aligned(lens, 4) ||
+      !aligned(seen, 4) || !aligned(lse, 4) || !aligned(weights, 4) || !aligned(new_weights, 4) ||
+      (dims->d_r > 0 && !aligned(kr_cache, 16)))
+    return GVA_ERR_INVALID_ARG;
+  if (workspace == nullptr || workspace_bytes < L.bytes || !aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
+  const bool q4 = v4_scale != nullptr, f32 = dims->dtype == GVA_DTYPE_F32;
+  st = q4 ? check_q4_dims(dims) : check_cache_layout(dims);
+  if (st != GVA_OK) return st;
+  WeightFn fn = weights_f32_kernel;
+  if (!f32) {
+    if ((dims->d_v != 64 && dims->d_v != 128) || dims->d_r % 8 != 0 || dims->d_r > 64) return GVA_ERR_UNSUPPORTED;
+    const int nrc = (dims->d_r + 31) / 32;
+    fn = q4 ? pick_weights<true>(dims->d_v, nrc) : pick_weights<false>(dims->d_v, nrc);
+  }
+  if ((long long)n_new * (dims->n_heads / dims->n_groups) > 0x7FFFFFF0LL) return GVA_ERR_UNSUPPORTED;
+  // rows per workgroup: few enough for two workgroups per CU, whole tiles
+  int chunk = kWeightChunk;
+  while (chunk > 32 && (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk) < 2LL * device_cu_count()) chunk /= 2;
+  const long long items = (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk);
+  if (items > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
+  float* q_abs = static_cast<float*>(workspace);
+  float* q_rot = dims->d_r > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + L.q_rot) : nullptr;
+  gva_dims at = *dims;                         // the queries' positions count the tokens seen, not the rows left
+  if (seen != nullptr) at.t_max = 0x7FFFFFFF;
+  st = gva_prefill_absorb(&at, n_new, q, m, seen != nullptr ? seen : lens, q_abs, q_rot, stream);
+  if (st != GVA_OK) return st;
+  WeightParams p{v_cache, static_cast<const uint8_t*>(v4_scale), kr_cache, q_abs, q_rot, lse, lens, weights, new_weights,
+                 dims->batch, dims->n_heads, dims->n_groups, n_new, dims->d_v, dims->d_r, dims->t_max, chunk,
+                 scale_log2(dims), (float)decay};
+  hipLaunchKernelGGL(fn, dim3((unsigned)items), dim3(64 * kWeightWaves), 0, static_cast<hipStream_t>(stream), p);
+  return launch_status();
+}
+
+int gva_evict_workspace_size(const gva_dims* dims, size_t* bytes) {
+  if (bytes == nullptr) return GVA_ERR_INVALID_ARG;
+  EvictLayout L;
+  const int st = evict_layout(dims, L);
+  if (st != GVA_OK) return st;
+  *bytes = L.bytes;
+  return GVA_OK;
+}
+
+int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_t n_recent, void* v_cache,
+                   void* v4_scale, void* kr_cache, const int32_t* lens, const int32_t* seen, const float* weights,
+                   const int32_t* row_pos, int32_t* new_lens, float* new_weights, int32_t* new_row_pos,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  EvictLayout L;
+  int st = evict_layout(dims, L);
+  if (st != GVA_OK) return st;
+  if (n_keep < 1 || n_first < 0 || n_recent < 0 || (long long)n_first + n_recent > n_keep) return GVA_ERR_INVALID_ARG;
+  if (!v_cache || !lens || !weights || !new_lens || !new_weights) return GVA_ERR_INVALID_ARG;
+  if (dims->d_r > 0 && !kr_cache) return GVA_ERR_INVALID_ARG;
+  if ((row_pos == nullptr) != (new_row_pos == nullptr)) return GVA_ERR_INVALID_ARG;
+  if (!aligned(v_cache, 16) || !aligned(v4_scale, 16) || !aligned(lens, 4) || !aligned(seen, 4) || !aligned(weights, 4) ||
+      !aligned(row_pos, 4) || !aligned(new_lens, 4) || !aligned(new_weights, 4) || !aligned(new_row_pos, 4) ||
+      (dims->d_r > 0 && !aligned(kr_cache, 16)))
+    return GVA_ERR_INVALID_ARG;
+  if (new_lens == lens || new_weights == weights || (row_pos != nullptr && new_row_pos == row_pos))
+    return GVA_ERR_INVALID_ARG;
+  if (workspace == nullptr || workspace_bytes < L.bytes || !aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
+  const bool q4 = v4_scale != nullptr;
+  st = q4 ? check_q4_dims(dims) : check_cache_layout(dims);
+  if (st != GVA_OK) return st;
+  if (dims->batch > 65535 || dims->n_groups >= 65535) return GVA_ERR_UNSUPPORTED;
+  char* ws = static_cast<char*>(workspace);
+  int32_t* count = reinterpret_cast<int32_t*>(ws);
+  int32_t* hole = reinterpret_cast<int32_t*>(ws + L.hole);
+  int32_t* move = reinterpret_cast<int32_t*>(ws + L.move);
+  const EvictParams p{lens, seen, weights, row_pos, new_lens, new_weights, new_row_pos, count, hole, move,
+                      dims->batch, dims->t_max, n_keep, n_first, n_recent, L.room};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(evict_select_kernel, dim3(dims->batch), dim3(kEvictThreads), 0, s, p);
+  st = launch_status();
+  const int most = n_keep < dims->t_max - n_keep ? n_keep : dims->t_max - n_keep;   // rows of a sequence that can move
+  if (st != GVA_OK || most <= 0) return st;
+  const int piece = (int)(16 / elem_size(dims));
+  const MoveParams mp{weights, row_pos, new_weights, new_row_pos, count, hole, move,
+                      static_cast<uint8_t*>(v_cache), static_cast<uint8_t*>(v4_scale), static_cast<uint8_t*>(kr_cache),
+                      dims->batch, dims->n_groups, dims->t_max, dims->d_v, L.room, dims->d_v / piece, dims->d_r / piece};
+  const dim3 grid((unsigned)((most + 16 * kWaves - 1) / (16 * kWaves)), (unsigned)(dims->n_groups + 1), (unsigned)dims->batch);
+  hipLaunchKernelGGL((q4 ? evict_move_kernel<true> : evict_move_kernel<false>), grid, dim3(kThreads), 0, s, mp);
+  return launch_status();
+}
+
+}  // extern "C"

@@ -26,7 +26,10 @@ EXPORTS = ("gva_append_kv", "gva_absorb_query", "gva_decode_attention", "gva_com
            "gva_gqa_decode_attention", "gva_paged_append_kv", "gva_paged_decode_attention",
            "gva_rope_decode_attention", "gva_prefill_absorb", "gva_prefill_attention",
            "gva_gqa_prefill_attention", "gva_prefill_workspace_size", "gva_prefill", "gva_pick_splits",
-           "gva_prefer_fused", "gva_status_string", "gva_version", "gva_decode_workspace_size", "gva_decode_step", "gva_decode_step_static")
+           "gva_prefer_fused", "gva_status_string", "gva_version", "gva_decode_workspace_size", "gva_decode_step", "gva_decode_step_static",
+           "gva_q4_append_kv", "gva_append_rows", "gva_q4_unpack_kv", "gva_q4_pick_splits",
+           "gva_q4_decode_workspace_size", "gva_q4_decode_step", "gva_weights_workspace_size",
+           "gva_accumulate_weights", "gva_evict_workspace_size", "gva_evict_rows")
 GVA_MAX_PAGES = 4096
 PROBE_EXPORTS = ("gva_probe_read",)      # include/gva_probe.h
 
@@ -88,6 +91,17 @@ def lib() -> ctypes.CDLL:
         L.gva_decode_workspace_size.argtypes = [D, I32, I32, ctypes.POINTER(ctypes.c_size_t)]
         L.gva_decode_step.argtypes = [D, P, P, P, P, P, P, P, I32, I32, P, ctypes.c_size_t, P, P, P]
         L.gva_decode_step_static.argtypes = [D, P, P, P, P, P, P, P, I32, I32, P, P, P]
+        SZ, SZP = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+        L.gva_q4_append_kv.argtypes = [D, P, P, P, P, P, P, P, P, I32, P, P]
+        L.gva_append_rows.argtypes = [D, P, P, P, P, P, P, P, I32, P, P]
+        L.gva_q4_unpack_kv.argtypes = [D, P, P, P, P, P]
+        L.gva_q4_pick_splits.argtypes = [D, I32, ctypes.c_int64, I32, ctypes.POINTER(I32)]
+        L.gva_q4_decode_workspace_size.argtypes = [D, I32, I32, SZP]
+        L.gva_q4_decode_step.argtypes = [D, P, P, P, P, P, P, P, I32, I32, P, SZ, P, P, P]
+        L.gva_weights_workspace_size.argtypes = [D, I32, SZP]
+        L.gva_accumulate_weights.argtypes = [D, I32, P, P, P, P, P, P, P, P, ctypes.c_double, P, P, P, SZ, P]
+        L.gva_evict_workspace_size.argtypes = [D, SZP]
+        L.gva_evict_rows.argtypes = [D, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P]
         L.gva_status_string.argtypes = [ctypes.c_int]
         L.gva_status_string.restype = ctypes.c_char_p
         L.gva_version.argtypes = []
@@ -97,7 +111,10 @@ def lib() -> ctypes.CDLL:
                      "gva_rope_decode_attention", "gva_prefill_absorb", "gva_prefill_attention",
                      "gva_gqa_prefill_attention", "gva_prefill_workspace_size", "gva_prefill",
                      "gva_pick_splits", "gva_version", "gva_probe_read",
-                     "gva_decode_workspace_size", "gva_decode_step", "gva_decode_step_static"):
+                     "gva_decode_workspace_size", "gva_decode_step", "gva_decode_step_static",
+                     "gva_q4_append_kv", "gva_append_rows", "gva_q4_unpack_kv", "gva_q4_pick_splits",
+                     "gva_q4_decode_workspace_size", "gva_q4_decode_step", "gva_weights_workspace_size",
+                     "gva_accumulate_weights", "gva_evict_workspace_size", "gva_evict_rows"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -787,3 +804,233 @@ def paged_decode(dims: GvaDims, paging: GvaPaging, q, m, v_pool, kr_pool, block_
         return bufs.o_part.view(dims.batch, dims.n_heads, dims.d_v), bufs.lse_part.view(dims.batch, dims.n_heads)
     gva_combine(dims, bufs.o_part, bufs.lse_part, S, bufs.o, bufs.lse, stream=stream)
     return bufs.o, bufs.lse
+
+
+# ------------------------------------------------- a cache held in 4 bits
+def q4_cache(dims: GvaDims, device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
+    """An empty 4-bit value cache: codes [B, G, T, d_v / 2] and scale bytes
+    [B, G, T, d_v / 32] (uint8, the layouts of include/gva.h)."""
+    d = dims
+    lead = (d.batch, d.n_groups, d.t_max)
+    return (torch.zeros(*lead, d.d_v // 2, dtype=torch.uint8, device=device),
+            torch.zeros(*lead, d.d_v // 32, dtype=torch.uint8, device=device))
+
+
+def _here(*tensors):
+    """The calls launch on the current device: refuse tensors of another."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.device.type == "cuda" and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _q4_ptrs(d: GvaDims, codes, scales):
+    lead = (d.batch, d.n_groups, d.t_max)
+    return (_ptr(codes, "v4_cache", torch.uint8, (*lead, d.d_v // 2)),
+            _ptr(scales, "v4_scale", torch.uint8, (*lead, d.d_v // 32)))
+
+
+def _values_ptrs(d: GvaDims, v_cache, v4_scale):
+    """A dense value cache (v4_scale None) or a 4-bit one."""
+    if v4_scale is not None:
+        return _q4_ptrs(d, v_cache, v4_scale)
+    return _ptr(v_cache, "v_cache", d.torch_dtype, (d.batch, d.n_groups, d.t_max, d.d_v)), None
+
+
+def _workspace(workspace):
+    if workspace is not None and (workspace.dtype != torch.uint8 or workspace.dim() != 1):
+        raise ValueError("workspace must be a 1-D uint8 tensor")
+    return _ptr(workspace, "workspace"), 0 if workspace is None else workspace.numel()
+
+
+def _bytes(name: str, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(name, getattr(lib(), name)(*args, ctypes.byref(n)))
+    return int(n.value)
+
+
+def _scratch(n: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def gva_q4_append_kv(dims: GvaDims, v4_cache, v4_scale, kr_cache, v_new, kr_new, seq, row, pos=None, row_pos=None,
+                     stream=None):
+    """gva_append_kv into a 4-bit cache: row r goes to row[r] of sequence
+    seq[r], its positional key rotated at pos[r] (None: row[r])."""
+    d, n = dims, seq.numel()
+    _here(v4_cache, v4_scale, kr_cache, v_new, kr_new, seq, row, pos, row_pos)
+    st = lib().gva_q4_append_kv(
+        ctypes.byref(d), *_q4_ptrs(d, v4_cache, v4_scale),
+        _ptr(kr_cache, "kr_cache", torch.bfloat16, (d.batch, d.t_max, d.d_r)),
+        _ptr(v_new, "v_new", torch.bfloat16, (n, d.n_groups, d.d_v)),
+        _ptr(kr_new, "kr_new", torch.bfloat16, (n, d.d_r)),
+        _ptr(seq, "seq", torch.int32, (n,)), _ptr(row, "row", torch.int32, (n,)), _ptr(pos, "pos", torch.int32, (n,)),
+        n, _ptr(row_pos, "row_pos", torch.int32, (d.batch, d.t_max)), _stream(stream))
+    _check("gva_q4_append_kv", st)
+
+
+def gva_append_rows(dims: GvaDims, v_cache, kr_cache, v_new, kr_new, seq, row, pos=None, row_pos=None, stream=None):
+    """gva_append_kv with the row apart from the position, for a cache that
+    rows have been evicted from."""
+    d, n = dims, seq.numel()
+    dt = d.torch_dtype
+    _here(v_cache, kr_cache, v_new, kr_new, seq, row, pos, row_pos)
+    st = lib().gva_append_rows(
+        ctypes.byref(d),
+        _ptr(v_cache, "v_cache", dt, (d.batch, d.n_groups, d.t_max, d.d_v)),
+        _ptr(kr_cache, "kr_cache", dt, (d.batch, d.t_max, d.d_r)),
+        _ptr(v_new, "v_new", dt, (n, d.n_groups, d.d_v)),
+        _ptr(kr_new, "kr_new", dt, (n, d.d_r)),
+        _ptr(seq, "seq", torch.int32, (n,)), _ptr(row, "row", torch.int32, (n,)), _ptr(pos, "pos", torch.int32, (n,)),
+        n, _ptr(row_pos, "row_pos", torch.int32, (d.batch, d.t_max)), _stream(stream))
+    _check("gva_append_rows", st)
+
+
+def gva_q4_unpack_kv(dims: GvaDims, v4_cache, v4_scale, lens, v_cache, stream=None):
+    """The values of a 4-bit cache's rows below lens, into a bf16 cache."""
+    d = dims
+    _here(v4_cache, v4_scale, lens, v_cache)
+    st = lib().gva_q4_unpack_kv(
+        ctypes.byref(d), *_q4_ptrs(d, v4_cache, v4_scale), _ptr(lens, "lens", torch.int32, (d.batch,)),
+        _ptr(v_cache, "v_cache", torch.bfloat16, (d.batch, d.n_groups, d.t_max, d.d_v)), _stream(stream))
+    _check("gva_q4_unpack_kv", st)
+
+
+def gva_q4_pick_splits(dims: GvaDims, max_len: int = 0, total_len: int = 0, n_cu: int = 0,
+                       chunked: bool = True) -> Tuple[int, int]:
+    """gva_pick_splits for gva_q4_decode_step: (num_splits, split_rows)."""
+    rows = ctypes.c_int32(0)
+    S = lib().gva_q4_pick_splits(ctypes.byref(dims), int(max_len), int(total_len), int(n_cu),
+                                 ctypes.byref(rows) if chunked else None)
+    return int(S), int(rows.value)
+
+
+def q4_plan_for(dims: GvaDims, lens: torch.Tensor, n_cu: int = 0, chunked: bool = True) -> Tuple[int, int]:
+    """gva_q4_pick_splits for the lengths in ``lens`` (host copy)."""
+    L = lens.detach().to("cpu", torch.int64).clamp(0, dims.t_max)
+    return gva_q4_pick_splits(dims, int(L.max()) if L.numel() else 0, int(L.sum()), n_cu, chunked)
+
+
+def gva_q4_decode_workspace_size(dims: GvaDims, num_splits: int, split_rows: int = 0) -> int:
+    return _bytes("gva_q4_decode_workspace_size", ctypes.byref(dims), int(num_splits), int(split_rows))
+
+
+def q4_workspace_for(dims: GvaDims, num_splits: int, split_rows: int = 0, device="cuda") -> Optional[torch.Tensor]:
+    """A device buffer for gva_q4_decode_step (None when the plan needs none)."""
+    return _scratch(gva_q4_decode_workspace_size(dims, num_splits, split_rows), device)
+
+
+def gva_q4_decode_step(dims: GvaDims, q, m, v4_cache, v4_scale, kr_cache, lens, num_splits: int, o, lse,
+                       workspace=None, seen=None, split_rows: int = 0, stream=None):
+    """gva_decode_step on a 4-bit cache that holds the current row already."""
+    d = dims
+    _here(q, m, v4_cache, v4_scale, kr_cache, lens, o, lse, workspace, seen)
+    st = lib().gva_q4_decode_step(
+        ctypes.byref(d),
+        _ptr(q, "q", torch.bfloat16, (d.batch, d.n_heads, d.d_c + d.d_r)),
+        _ptr(m, "m", torch.bfloat16, (d.n_heads, d.d_v, d.d_c)),
+        *_q4_ptrs(d, v4_cache, v4_scale),
+        _ptr(kr_cache, "kr_cache", torch.bfloat16, (d.batch, d.t_max, d.d_r)),
+        _ptr(lens, "lens", torch.int32, (d.batch,)), _ptr(seen, "seen", torch.int32, (d.batch,)),
+        int(num_splits), int(split_rows), *_workspace(workspace),
+        _ptr(o, "o", torch.float32, (d.batch, d.n_heads, d.d_v)),
+        _ptr(lse, "lse", torch.float32, (d.batch, d.n_heads)), _stream(stream))
+    _check("gva_q4_decode_step", st)
+
+
+def q4_decode(dims: GvaDims, q, m, v4_cache, v4_scale, kr_cache, lens, seen=None,
+              stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """One decode step on a 4-bit cache, planned for its lengths (which it
+    reads); returns (o, lse) fp32."""
+    d = dims
+    S, rows = q4_plan_for(d, lens)
+    dev = v4_cache.device
+    o = torch.empty(d.batch, d.n_heads, d.d_v, dtype=torch.float32, device=dev)
+    lse = torch.empty(d.batch, d.n_heads, dtype=torch.float32, device=dev)
+    ws = q4_workspace_for(d, S, rows, dev)
+    _in_use_on(stream, o, lse, ws)
+    gva_q4_decode_step(d, q, m, v4_cache, v4_scale, kr_cache if d.d_r > 0 else None, lens, S, o, lse, workspace=ws,
+                       seen=seen, split_rows=rows, stream=stream)
+    return o, lse
+
+
+# ------------------------------------------------------------- eviction
+def gva_weights_workspace_size(dims: GvaDims, n_new: int) -> int:
+    return _bytes("gva_weights_workspace_size", ctypes.byref(dims), int(n_new))
+
+
+def weights_workspace_for(dims: GvaDims, n_new: int, device="cuda") -> Optional[torch.Tensor]:
+    """A device buffer for gva_accumulate_weights."""
+    return _scratch(gva_weights_workspace_size(dims, n_new), device)
+
+
+def gva_accumulate_weights(dims: GvaDims, n_new: int, q, m, v_cache, v4_scale, kr_cache, lens, lse, weights, new_weights,
+                           workspace=None, seen=None, decay: float = 1.0, stream=None):
+    """Add the attention weight that cached rows draw from the last n_new
+    queries (q [B, n_new, H, d_c+d_r], lse [B, n_new, H]) to their weights
+    [B, T].  v_cache is a 4-bit cache's codes where v4_scale is given."""
+    d, N = dims, int(n_new)
+    _here(q, m, v_cache, v4_scale, kr_cache, lens, lse, weights, new_weights, workspace, seen)
+    st = lib().gva_accumulate_weights(
+        ctypes.byref(d), N,
+        _ptr(q, "q", d.torch_dtype, (d.batch, N, d.n_heads, d.d_c + d.d_r)),
+        _ptr(m, "m", d.torch_dtype, (d.n_heads, d.d_v, d.d_c)),
+        *_values_ptrs(d, v_cache, v4_scale),
+        _ptr(kr_cache, "kr_cache", d.torch_dtype, (d.batch, d.t_max, d.d_r)),
+        _ptr(lens, "lens", torch.int32, (d.batch,)), _ptr(seen, "seen", torch.int32, (d.batch,)),
+        _ptr(lse, "lse", torch.float32, (d.batch, N, d.n_heads)), float(decay),
+        _ptr(weights, "weights", torch.float32, (d.batch, d.t_max)),
+        _ptr(new_weights, "new_weights", torch.float32, (d.batch, d.t_max)), *_workspace(workspace), _stream(stream))
+    _check("gva_accumulate_weights", st)
+
+
+def accumulate_weights(dims: GvaDims, q, m, v_cache, kr_cache, lens, lse, weights, v4_scale=None, seen=None,
+                       decay: float = 1.0, stream=None) -> torch.Tensor:
+    """gva_accumulate_weights in place; q [B, N, H, d_c+d_r], or [B, H, ...]
+    for a decode step (lse alike).  Returns weights."""
+    d = dims
+    if q.dim() == 3:
+        q, lse = q.unsqueeze(1), lse.unsqueeze(1)
+    ws = weights_workspace_for(d, q.shape[1], q.device)
+    _in_use_on(stream, ws)
+    gva_accumulate_weights(d, q.shape[1], q, m, v_cache, v4_scale, kr_cache if d.d_r > 0 else None, lens, lse, weights,
+                           weights, workspace=ws, seen=seen, decay=decay, stream=stream)
+    return weights
+
+
+def gva_evict_workspace_size(dims: GvaDims) -> int:
+    return _bytes("gva_evict_workspace_size", ctypes.byref(dims))
+
+
+def evict_workspace_for(dims: GvaDims, device="cuda") -> Optional[torch.Tensor]:
+    """A device buffer for gva_evict_rows."""
+    return _scratch(gva_evict_workspace_size(dims), device)
+
+
+def gva_evict_rows(dims: GvaDims, n_keep: int, n_first: int, n_recent: int, v_cache, v4_scale, kr_cache, lens, weights,
+                   new_lens, new_weights, workspace=None, seen=None, row_pos=None, new_row_pos=None, stream=None):
+    """Cut every sequence down to its n_keep rows of the largest weight, rows
+    at positions below n_first or among the last n_recent before all others."""
+    d = dims
+    _here(v_cache, v4_scale, kr_cache, lens, weights, new_lens, new_weights, workspace, seen, row_pos, new_row_pos)
+    BT = (d.batch, d.t_max)
+    st = lib().gva_evict_rows(
+        ctypes.byref(d), int(n_keep), int(n_first), int(n_recent), *_values_ptrs(d, v_cache, v4_scale),
+        _ptr(kr_cache, "kr_cache", d.torch_dtype, (*BT, d.d_r)),
+        _ptr(lens, "lens", torch.int32, (d.batch,)), _ptr(seen, "seen", torch.int32, (d.batch,)),
+        _ptr(weights, "weights", torch.float32, BT), _ptr(row_pos, "row_pos", torch.int32, BT),
+        _ptr(new_lens, "new_lens", torch.int32, (d.batch,)), _ptr(new_weights, "new_weights", torch.float32, BT),
+        _ptr(new_row_pos, "new_row_pos", torch.int32, BT), *_workspace(workspace), _stream(stream))
+    _check("gva_evict_rows", st)
+
+
+def evict(dims: GvaDims, n_keep: int, v_cache, kr_cache, lens, weights, n_first: int = 0, n_recent: int = 0,
+          v4_scale=None, seen=None, row_pos=None, stream=None):
+    """gva_evict_rows; returns (lens, weights, row_pos) as they are afterwards
+    (row_pos None where none is given)."""
+    d = dims
+    out = torch.empty_like(lens), torch.empty_like(weights), None if row_pos is None else torch.empty_like(row_pos)
+    ws = evict_workspace_for(d, v_cache.device)
+    _in_use_on(stream, *out, ws)
+    gva_evict_rows(d, n_keep, n_first, n_recent, v_cache, v4_scale, kr_cache if d.d_r > 0 else None, lens, weights, out[0],
+                   out[1], workspace=ws, seen=seen, row_pos=row_pos, new_row_pos=out[2], stream=stream)
+    return out

@@ -1,0 +1,725 @@
+"""The 4-bit cache (append, unpack, decode step), the accumulated attention
+weights and the eviction: against 64-bit references on the GPU, and their
+refusals on the CPU."""
+
+import ctypes
+import math
+
+import pytest
+import torch
+
+import q4_ref as ref
+from gpu_helpers import note
+from paper_2609_13285_amd import gva
+
+A = 0x10000      # an aligned address that a refused call never reads
+gpu = pytest.mark.gpu
+
+
+def dims(**kw):
+    base = dict(batch=2, n_heads=8, n_groups=2, d_v=128, d_c=128, d_r=16, t_max=64, dtype="bf16")
+    base.update(kw)
+    return gva.make_dims(**base)
+
+
+# ---------------------------------------------------------------- refusals
+def append_status(d, c=A, s=A, k=A, v=A, kn=A, seq=A, row=A, pos=None, n=4, rp=None):
+    return gva.lib().gva_q4_append_kv(ctypes.byref(d), c, s, k, v, kn, seq, row, pos, n, rp, None)
+
+
+def rows_status(d, v=A, k=A, vn=A, kn=A, seq=A, row=A, pos=None, n=4, rp=None):
+    return gva.lib().gva_append_rows(ctypes.byref(d), v, k, vn, kn, seq, row, pos, n, rp, None)
+
+
+def unpack_status(d, c=A, s=A, lens=A, v=A):
+    return gva.lib().gva_q4_unpack_kv(ctypes.byref(d), c, s, lens, v, None)
+
+
+def step_status(d, q=A, m=A, c=A, s=A, k=A, lens=A, seen=None, S=2, rows=0, ws=A, n=1 << 40, o=A, lse=A):
+    return gva.lib().gva_q4_decode_step(ctypes.byref(d), q, m, c, s, k, lens, seen, S, rows, ws, n, o, lse, None)
+
+
+def weights_status(d, N=1, q=A, m=A, v=A, s=None, k=A, lens=A, seen=None, lse=A, decay=1.0, w=A, nw=A, ws=A, n=1 << 40):
+    return gva.lib().gva_accumulate_weights(ctypes.byref(d), N, q, m, v, s, k, lens, seen, lse, decay, w, nw, ws, n, None)
+
+
+def evict_status(d, keep=16, first=0, recent=0, v=A, s=None, k=A, lens=A, seen=None, w=A, rp=None, nl=A + 256, nw=A + 512,
+                 nrp=None, ws=A, n=1 << 40):
+    return gva.lib().gva_evict_rows(ctypes.byref(d), keep, first, recent, v, s, k, lens, seen, w, rp, nl, nw, nrp, ws, n,
+                                    None)
+
+
+Q4_CALLS = [append_status, unpack_status, step_status]
+ALL_CALLS = Q4_CALLS + [rows_status, weights_status, evict_status]
+
+
+@pytest.mark.parametrize("call", ALL_CALLS)
+@pytest.mark.parametrize("kw", [dict(batch=0), dict(n_groups=3), dict(d_r=-2), dict(d_v=0), dict(dtype=5), dict(t_max=0)])
+def test_bad_dims_refused(call, kw):
+    assert call(dims(**kw)) == gva.GVA_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("call", ALL_CALLS)
+def test_no_dims_refused(call):
+    d = ctypes.POINTER(gva.GvaDims)()
+    assert gva.lib().gva_q4_unpack_kv(d, A, A, A, A, None) == gva.GVA_ERR_INVALID_ARG
+    assert gva.lib().gva_evict_workspace_size(d, ctypes.byref(ctypes.c_size_t())) == gva.GVA_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("call", Q4_CALLS)
+@pytest.mark.parametrize("kw", [dict(dtype="f32"), dict(d_v=32), dict(d_v=256), dict(t_max=48), dict(d_r=12), dict(d_r=72),
+                                dict(t_max=1 << 25)])
+def test_unsupported_q4_shapes(call, kw):
+    assert call(dims(**kw)) == gva.GVA_ERR_UNSUPPORTED
+
+
+def test_append_refusals():
+    for call in (append_status, rows_status):
+        d = dims()
+        assert call(d, n=-1) == gva.GVA_ERR_INVALID_ARG
+        assert call(d, n=0) == gva.GVA_OK
+        for kw in (dict(seq=None), dict(row=None), dict(k=None), dict(kn=None), dict(seq=A + 2), dict(row=A + 1),
+                   dict(pos=A + 2), dict(rp=A + 2), dict(k=A + 8), dict(kn=A + 2)):
+            assert call(d, **kw) == gva.GVA_ERR_INVALID_ARG, kw
+    for kw in (dict(c=None), dict(s=None), dict(v=None), dict(c=A + 8), dict(s=A + 4), dict(v=A + 2)):
+        assert append_status(dims(), **kw) == gva.GVA_ERR_INVALID_ARG, kw
+    assert rows_status(dims(t_max=40)) == gva.GVA_ERR_UNSUPPORTED
+
+
+def test_unpack_refusals():
+    for kw in (dict(c=None), dict(s=None), dict(lens=None), dict(v=None), dict(c=A + 8), dict(s=A + 2), dict(lens=A + 1),
+               dict(v=A + 2)):
+        assert unpack_status(dims(), **kw) == gva.GVA_ERR_INVALID_ARG, kw
+
+
+def test_step_refusals():
+    d = dims()
+    for kw in (dict(q=None), dict(m=None), dict(c=None), dict(s=None), dict(k=None), dict(lens=None), dict(o=None),
+               dict(lse=None), dict(q=A + 8), dict(c=A + 8), dict(seen=A + 2), dict(S=0), dict(S=257), dict(rows=-32),
+               dict(rows=40), dict(ws=None), dict(ws=A + 128), dict(n=256), dict(o=A + 4), dict(lse=A + 2)):
+        assert step_status(d, **kw) == gva.GVA_ERR_INVALID_ARG, kw
+    for kw in (dict(d_c=48), dict(d_c=0), dict(d_c=544), dict(n_heads=32), dict(n_heads=6)):
+        assert step_status(dims(**kw)) == gva.GVA_ERR_UNSUPPORTED, kw
+    n = ctypes.c_size_t(7)
+    assert gva.lib().gva_q4_decode_workspace_size(ctypes.byref(d), 0, 0, ctypes.byref(n)) == gva.GVA_ERR_INVALID_ARG
+    assert gva.lib().gva_q4_decode_workspace_size(ctypes.byref(d), 1, 0, None) == gva.GVA_ERR_INVALID_ARG
+    assert gva.gva_q4_decode_workspace_size(d, 4) % 256 == 0
+
+
+def test_weights_refusals():
+    for d, s in ((dims(), None), (dims(), A), (dims(dtype="f32"), None)):
+        for kw in (dict(q=None), dict(m=None), dict(v=None), dict(k=None), dict(lens=None), dict(lse=None), dict(nw=None),
+                   dict(N=0), dict(N=65), dict(decay=-0.5), dict(decay=math.nan), dict(decay=math.inf), dict(w=None),
+                   dict(v=A + 8), dict(lse=A + 2), dict(w=A + 2), dict(nw=A + 1), dict(seen=A + 2), dict(ws=None),
+                   dict(ws=A + 64), dict(n=512)):
+            assert weights_status(d, s=s, **kw) == gva.GVA_ERR_INVALID_ARG, kw
+    assert weights_status(dims(dtype="f32"), s=A) == gva.GVA_ERR_UNSUPPORTED
+    assert weights_status(dims(d_v=96)) == gva.GVA_ERR_UNSUPPORTED
+    assert weights_status(dims(d_r=12)) == gva.GVA_ERR_UNSUPPORTED
+    assert weights_status(dims(t_max=40)) == gva.GVA_ERR_UNSUPPORTED
+    assert weights_status(dims(t_max=48), s=A) == gva.GVA_ERR_UNSUPPORTED
+    assert weights_status(dims(d_c=40)) == gva.GVA_ERR_UNSUPPORTED
+
+
+def test_evict_refusals():
+    for d, s in ((dims(), None), (dims(), A), (dims(dtype="f32"), None)):
+        for kw in (dict(keep=0), dict(keep=-1), dict(first=-1), dict(recent=-1), dict(first=9, recent=8), dict(v=None),
+                   dict(k=None), dict(lens=None), dict(w=None), dict(nl=None), dict(nw=None), dict(rp=A), dict(nrp=A),
+                   dict(nl=A), dict(nw=A), dict(rp=A, nrp=A), dict(v=A + 8), dict(nl=A + 2), dict(ws=None), dict(ws=A + 64),
+                   dict(n=16)):
+            assert evict_status(d, s=s, **kw) == gva.GVA_ERR_INVALID_ARG, kw
+    assert evict_status(dims(dtype="f32"), s=A) == gva.GVA_ERR_UNSUPPORTED
+    assert evict_status(dims(t_max=48), s=A) == gva.GVA_ERR_UNSUPPORTED
+    assert evict_status(dims(t_max=40)) == gva.GVA_ERR_UNSUPPORTED
+
+
+def test_binding_refuses_cpu_tensors_and_wrong_shapes():
+    d = dims()
+    c, s = gva.q4_cache(d, device="cpu")
+    assert tuple(c.shape) == (2, 2, 64, 64) and tuple(s.shape) == (2, 2, 64, 4)
+    lens = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        gva.gva_q4_unpack_kv(d, c, s, lens, torch.zeros(2, 2, 64, 128, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        gva.gva_evict_rows(d, 8, 0, 0, c, s, None, lens, torch.zeros(2, 64), lens, torch.zeros(2, 64))
+
+
+# ------------------------------------------------------- the references
+@pytest.mark.parametrize("d", [64, 128])
+def test_reference_layout_is_a_permutation(d):
+    g = torch.Generator().manual_seed(d)
+    code = torch.randint(0, 16, (2, 96, d), generator=g, dtype=torch.int32).to(torch.uint8)
+    byte = torch.randint(0, 256, (2, 96, d // 32), generator=g, dtype=torch.int32).to(torch.uint8)
+    c, s = ref.unpack(*ref.pack(code, byte))
+    assert torch.equal(c, code) and torch.equal(s, byte)
+
+
+def test_reference_scale_bounds_the_error():
+    # off by at most 2^e, and at most half the gap between levels below 6 * 2^e
+    x = torch.randn(64, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    code, byte = ref.quantize(x)
+    err = (ref.values(code, byte) - x.double()).abs().unflatten(-1, (-1, 32))
+    assert bool((err <= torch.exp2(byte.double() - 127).unsqueeze(-1)).all())
+
+
+# --------------------------------------------------------------- append
+def bf16(bits):
+    return bits.to(torch.int32).to(torch.int16).view(torch.bfloat16)
+
+
+@gpu
+@pytest.mark.parametrize("d_v", [64, 128])
+def test_append_every_bf16(d_v):
+    """Every bf16 number, in blocks of its own binade, and under larger ones."""
+    bits = torch.arange(65536)
+    own = bits.reshape(-1, 32)
+    g = torch.Generator().manual_seed(3)
+    mixed = own[torch.randperm(2048, generator=g)].clone()
+    shift = torch.randint(0, 5, (2048, 1), generator=g) * 128          # the first element up to four binades up
+    mixed[:, :1] = (mixed[:, :1] & 0x7FFF) + shift
+    mixed[:, :1].clamp_(max=0x7F7F)
+    x = bf16(torch.cat((own, mixed)).reshape(-1, 1, d_v))              # [rows, 1, d_v]
+    n = x.shape[0]
+    d = dims(batch=1, n_heads=1, n_groups=1, d_v=d_v, d_r=0, t_max=n)
+    note(f"q4 append every bf16 d_v={d_v} rows={n}")
+    c, s = gva.q4_cache(d)
+    row = torch.arange(n, dtype=torch.int32).cuda()
+    gva.gva_q4_append_kv(d, c, s, None, x.cuda(), None, torch.zeros_like(row), row)
+    code, byte = ref.quantize(x.transpose(0, 1).unsqueeze(0))
+    got_c, got_s = ref.unpack(c.cpu(), s.cpu())
+    assert torch.equal(got_s, byte)
+    assert torch.equal(got_c, code)
+
+
+@gpu
+@pytest.mark.parametrize("d_v,G,d_r,n", [(64, 1, 0, 1), (64, 3, 8, 37), (128, 5, 64, 70), (128, 8, 16, 16), (64, 9, 24, 33)])
+def test_append_scatters_rotates_and_skips(orc, d_v, G, d_r, n):
+    B, T = 3, 96
+    d = dims(batch=B, n_heads=G, n_groups=G, d_v=d_v, d_r=d_r, t_max=T)
+    g = torch.Generator().manual_seed(n)
+    v = torch.randn(n, G, d_v, generator=g).to(torch.bfloat16)
+    kn = torch.randn(n, d_r, generator=g).to(torch.bfloat16)
+    place = torch.randperm(B * T, generator=g)[:n]
+    seq, row = (place // T).to(torch.int32), (place % T).to(torch.int32)
+    pos = torch.randint(0, 500, (n,), generator=g, dtype=torch.int32)
+    out = (torch.arange(n) % 7 == 3)
+    bad_seq, bad_row = seq.clone(), row.clone()
+    bad_seq[out] = torch.where(torch.arange(int(out.sum())) % 2 == 0, -1, B).to(torch.int32)
+    bad_row[(torch.arange(n) % 7 == 5)] = T
+    out |= torch.arange(n) % 7 == 5
+    note(f"q4 append d_v={d_v} G={G} d_r={d_r} n={n}")
+    c, s = gva.q4_cache(d)
+    c.fill_(0x5A), s.fill_(0x81)
+    kr = torch.full((B, T, d_r), 7.0, dtype=torch.bfloat16, device="cuda")
+    rp = torch.full((B, T), -9, dtype=torch.int32, device="cuda")
+    for _ in range(2):                                   # the same rows twice: the same cache
+        gva.gva_q4_append_kv(d, c, s, kr if d_r else None, v.cuda(), kn.cuda() if d_r else None, bad_seq.cuda(),
+                             bad_row.cuda(), pos=pos.cuda(), row_pos=rp)
+    code = torch.full((B, G, T, d_v), 0, dtype=torch.uint8)
+    byte = torch.full((B, G, T, d_v // 32), 0x81, dtype=torch.uint8)
+    code[..., 0::2], code[..., 1::2] = 0xA, 0x5
+    wc, ws = ref.quantize(v)
+    v_ref = torch.zeros(1, G, 512, d_v, dtype=torch.bfloat16)
+    want_k = torch.full((B, T, d_r), 7.0, dtype=torch.bfloat16)
+    want_p = torch.full((B, T), -9, dtype=torch.int32)
+    for r in range(n):
+        if out[r]:
+            continue
+        b, t = int(seq[r]), int(row[r])
+        code[b, :, t], byte[b, :, t] = wc[r], ws[r]
+        want_p[b, t] = pos[r]
+        if d_r:
+            k_ref = torch.zeros(1, 512, d_r, dtype=torch.bfloat16)
+            orc.append(v_ref, k_ref, v[r:r + 1], kn[r:r + 1], torch.zeros(1), pos[r:r + 1])
+            want_k[b, t] = k_ref[0, int(pos[r])]
+    got_c, got_s = ref.unpack(c.cpu(), s.cpu())
+    assert torch.equal(got_c, code) and torch.equal(got_s, byte)
+    assert torch.equal(rp.cpu(), want_p)
+    if d_r:
+        assert torch.equal(gva.untiled(kr.cpu()), want_k)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,d_v,d_r", [("bf16", 128, 16), ("f32", 64, 8), ("f32", 20, 0)])
+def test_append_rows_is_append_kv_elsewhere(dtype, d_v, d_r):
+    """A row stored at `row` equals gva_append_kv's at `pos`."""
+    B, G, T, n = 2, 3, 512, 50
+    d = dims(batch=B, n_heads=G, n_groups=G, d_v=d_v, d_r=d_r, t_max=T, dtype=dtype)
+    g = torch.Generator().manual_seed(9)
+    v = torch.randn(n, G, d_v, generator=g).to(d.torch_dtype).cuda()
+    kn = torch.randn(n, d_r, generator=g).to(d.torch_dtype).cuda()
+    place = torch.randperm(B * T, generator=g)[:n]
+    seq, pos = (place // T).to(torch.int32).cuda(), (place % T).to(torch.int32).cuda()
+    row = ((pos + 77) % T).to(torch.int32)
+    new = lambda *shape: torch.zeros(*shape, dtype=d.torch_dtype, device="cuda")     # noqa: E731
+    note(f"append_rows {dtype} d_v={d_v} d_r={d_r}")
+    v0, k0, v1, k1 = new(B, G, T, d_v), new(B, T, d_r), new(B, G, T, d_v), new(B, T, d_r)
+    rp = torch.full((B, T), -1, dtype=torch.int32, device="cuda")
+    gva.gva_append_kv(d, v0, k0, v, kn, seq, pos)
+    gva.gva_append_rows(d, v1, k1, v, kn, seq, row, pos=pos, row_pos=rp)
+    assert torch.equal(gva.untiled(v1.cpu()).roll(-77, 2), gva.untiled(v0.cpu()))
+    if d_r:
+        assert torch.equal(gva.untiled(k1.cpu()).roll(-77, 1), gva.untiled(k0.cpu()))
+    want = torch.full((B, T), -1, dtype=torch.int32)
+    want[seq.cpu().long(), row.cpu().long()] = pos.cpu()
+    assert torch.equal(rp.cpu(), want)
+    v2, k2 = new(B, G, T, d_v), new(B, T, d_r)
+    gva.gva_append_rows(d, v2, k2, v, kn, seq, pos)     # without positions: gva_append_kv
+    assert torch.equal(v2, v0) and torch.equal(k2, k0)
+
+
+# --------------------------------------------------------------- unpack
+@gpu
+@pytest.mark.parametrize("d_v,G,T", [(64, 1, 32), (64, 3, 160), (128, 2, 96), (128, 7, 544)])
+def test_unpack(d_v, G, T):
+    B = 5
+    d = dims(batch=B, n_heads=G, n_groups=G, d_v=d_v, d_r=0, t_max=T)
+    g = torch.Generator().manual_seed(T)
+    code = torch.randint(0, 16, (B, G, T, d_v), generator=g, dtype=torch.int32).to(torch.uint8)
+    byte = torch.randint(8, 253, (B, G, T, d_v // 32), generator=g, dtype=torch.int32).to(torch.uint8)
+    byte[torch.rand(byte.shape, generator=g) < 0.05] = 255
+    lens = torch.tensor([0, 1, T, T // 2 + 3, T + 5], dtype=torch.int32)
+    note(f"q4 unpack d_v={d_v} G={G} T={T}")
+    c, s = ref.pack(code, byte)
+    out = torch.full((B, G, T, d_v), 3.0, dtype=torch.bfloat16, device="cuda")
+    gva.gva_q4_unpack_kv(d, c.cuda(), s.cuda(), lens.cuda(), out)
+    want = ref.values(code, byte)
+    got = gva.untiled(out.cpu()).double()
+    for b in range(B):
+        L = min(int(lens[b]), T)
+        assert torch.equal(torch.isnan(got[b, :, :L]), torch.isnan(want[b, :, :L]))
+        assert torch.equal(torch.nan_to_num(got[b, :, :L]), torch.nan_to_num(want[b, :, :L]))
+        assert bool((got[b, :, L:] == 3.0).all())
+
+
+# --------------------------------------------------------------- decode
+def problem(B, T, H, G, d_v, d_c, d_r, lens, N=1, extra=0, cache="q4", seed=0, q_std=1.0):
+    """Seeded inputs: device tensors for the calls and the fp64 rows they stand for."""
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=d_c, d_r=d_r, t_max=T, dtype="f32" if cache == "f32" else "bf16")
+    g = torch.Generator().manual_seed(seed)
+    dt = d.torch_dtype
+    x = {"d": d, "G": G, "lens": torch.tensor(lens, dtype=torch.int32), "q": (q_std * torch.randn(B, N, H, d_c + d_r, generator=g)).to(dt),
+         "m": (torch.randn(H, d_v, d_c, generator=g) / math.sqrt(d_v)).to(dt)}
+    x["seen"] = x["lens"].clamp(0, T) + extra
+    rows, kr = torch.randn(B, G, T, d_v, generator=g).to(dt), torch.randn(B, T, d_r, generator=g).to(dt)
+    dead = torch.arange(T) >= x["lens"].clamp(0, T).unsqueeze(1)
+    if cache == "q4":
+        code, byte = ref.quantize(rows)
+        x["v"] = ref.values(code, byte)
+        byte = torch.where(dead[:, None, :, None], torch.full_like(byte, 255), byte)      # never-written rows read as NaN
+        x["vc"], x["sc"] = (t.cuda() for t in ref.pack(code, byte))
+    else:
+        x["v"] = rows.double()
+        x["vc"], x["sc"] = gva.tiled(rows.masked_fill(dead[:, None, :, None], math.nan)).cuda(), None
+    x["kr"] = kr.double()
+    x["kc"] = gva.tiled(kr.masked_fill(dead[..., None], math.nan)).cuda() if d_r else None
+    return x
+
+
+def step(x, S=1, rows=0, stream=None):
+    d = x["d"]
+    o = torch.full((d.batch, d.n_heads, d.d_v), math.nan, device="cuda")
+    lse = torch.full((d.batch, d.n_heads), math.nan, device="cuda")
+    ws = gva.q4_workspace_for(d, S, rows)
+    if ws is not None:
+        ws.fill_(0xFF)                                   # whatever the workspace holds
+    gva.gva_q4_decode_step(d, x["q"][:, 0].contiguous().cuda(), x["m"].cuda(), x["vc"], x["sc"], x["kc"], x["lens"].cuda(), S, o,
+                           lse, workspace=ws, seen=x["seen"].cuda(), split_rows=rows, stream=stream)
+    return o, lse
+
+
+def check_step(x, o, lse):
+    """The query and the weights are kept as bf16 high + low parts, each off by
+    at most 2^-18 of its size (two roundings of half a step, 2^-9, one after the
+    other); sums are fp32 over d_v + d_r terms.  So a score is off by at most
+    A (2^-18 + 256 * 2^-24), A its sum of magnitudes (log2(e) and the scale cost
+    a few 2^-24 more), the weights by e^(2 |dx|) - 1 and 2^-17, and o by that
+    times the largest value of its sequence."""
+    sc, size = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], x["G"])
+    ro, rl = ref.attend(sc, x["v"], x["G"])
+    ro, rl = ro[:, 0], rl[:, 0]
+    o, lse = o.cpu().double(), lse.cpu().double()
+    empty = torch.isneginf(rl)
+    assert torch.equal(torch.isneginf(lse), empty)
+    dx = size.amax(-1)[:, 0] * (2.0 ** -18 + 264 * 2.0 ** -24)
+    assert bool(((lse - rl).abs()[~empty] <= (dx + 8e-7 * (1 + rl.abs()))[~empty]).all())
+    top = x["v"].abs().amax((1, 2, 3))[:, None, None]
+    tol = (torch.expm1(2 * dx) + 2.0 ** -16).unsqueeze(-1) * top
+    err = (o - torch.where(empty.unsqueeze(-1), torch.zeros_like(ro), ro)).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@gpu
+@pytest.mark.parametrize("hpg", [1, 2, 4, 8])
+@pytest.mark.parametrize("d_v,d_c,d_r", [(64, 64, 16), (128, 128, 0), (128, 32, 40), (64, 160, 64), (128, 128, 8)])
+@pytest.mark.parametrize("S,rows", [(1, 0), (3, 0), (4, 64)])
+def test_step(hpg, d_v, d_c, d_r, S, rows):
+    T = 224
+    lens = [0, 1, 31, 32, 33, T, 97, T + 40, -3]
+    x = problem(len(lens), T, 2 * hpg, 2, d_v, d_c, d_r, lens, extra=41, seed=hpg * 1000 + d_v + d_r)
+    note(f"q4 step hpg={hpg} d={d_v}/{d_c}/{d_r} S={S} rows={rows}")
+    check_step(x, *step(x, S, rows))
+
+
+@gpu
+@pytest.mark.parametrize("B,T,H,G,d_v,d_r,S,rows", [(1, 4128, 8, 8, 64, 16, 16, 0), (2, 2016, 16, 4, 128, 24, 7, 0),
+                                                    (40, 160, 8, 2, 128, 16, 4, 32), (70, 96, 4, 1, 64, 0, 3, 32),
+                                                    (3, 1024, 32, 8, 128, 32, 1, 0), (1, 8192, 8, 1, 128, 16, 256, 0)])
+def test_step_plans(B, T, H, G, d_v, d_r, S, rows):
+    g = torch.Generator().manual_seed(T)
+    lens = torch.randint(1, T + 1, (B,), generator=g).tolist()
+    lens[0] = T
+    x = problem(B, T, H, G, d_v, d_v, d_r, lens, seed=T)
+    note(f"q4 step B={B} T={T} H={H} G={G} d={d_v}/{d_r} S={S} rows={rows}")
+    one = step(x, S, rows)
+    check_step(x, *one)
+    two = step(x, S, rows)
+    assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+    check_step(x, *step(x, *gva.q4_plan_for(x["d"], x["lens"])))
+
+
+@gpu
+def test_step_sharp_scores_and_far_positions():
+    """Queries six times larger (a few rows take the weight), at positions past 2^20."""
+    x = problem(2, 512, 8, 2, 128, 128, 32, [512, 300], extra=1 << 20, seed=5, q_std=6.0)
+    note("q4 step, sharp scores, far positions")
+    check_step(x, *step(x, 2, 0))
+
+
+@gpu
+def test_step_reads_a_nan_block_as_nan_in_its_group_only():
+    x = problem(1, 64, 4, 2, 64, 64, 0, [40], seed=6)
+    code, byte = ref.unpack(x["vc"].cpu(), x["sc"].cpu())
+    byte[0, 1, 7, 0] = 255
+    x["sc"] = ref.pack(code, byte)[1].cuda()
+    note("q4 step, NaN block")
+    o, lse = step(x)
+    assert bool(torch.isnan(o[0, 2:]).all()) and bool(torch.isfinite(o[0, :2]).all())
+
+
+@gpu
+def test_step_large_stream_offsets():
+    """The longest stream that the calls take (508 MB of codes)."""
+    T = ((1 << 31) - (1 << 24)) // 256 - 32
+    d = dims(batch=1, n_heads=1, n_groups=1, d_v=128, d_c=32, d_r=0, t_max=T)
+    c, s = gva.q4_cache(d)
+    s.fill_(127)                                        # every row zero but the last three
+    v = torch.full((3, 1, 128), 2.0, dtype=torch.bfloat16, device="cuda")
+    row = torch.tensor([T - 1, T - 2, T - 3], dtype=torch.int32, device="cuda")
+    note(f"q4 step, T={T}")
+    gva.gva_q4_append_kv(d, c, s, None, v, None, torch.zeros_like(row), row)
+    q = torch.zeros(1, 1, 32, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 16.0
+    m = torch.zeros(1, 128, 32, dtype=torch.bfloat16, device="cuda")
+    m[..., 0] = 0.125
+    o, lse = gva.q4_decode(d, q, m, c, s, None, torch.tensor([T], dtype=torch.int32, device="cuda"))
+    x = 16 * 0.125 * 2.0 * 128 / math.sqrt(32)          # the three rows' score; the others' is 0
+    p = 3 / (3 + (T - 3) * math.exp(-x))
+    assert bool(((o.cpu().double() - 2.0 * p).abs() <= 2e-5).all())
+    # the scaled query as bf16 high + low parts is off by up to 2^-18 of itself,
+    # which moves the score x = 90.5 by up to 3.5e-4; fp32 sums by x * 2^-22
+    assert abs(float(lse) - (x + math.log(3 / p))) <= x * (2.0 ** -18 + 2.0 ** -22)
+
+
+@gpu
+def test_step_streams_graph_and_guards():
+    """On a side stream; captured, replayed with eager work between; nothing
+    written outside the outputs."""
+    x = problem(3, 256, 16, 4, 128, 128, 16, [256, 17, 130], seed=8)
+    d = x["d"]
+    note("q4 step: streams, graph, guards")
+    base = step(x, 3, 0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step(x, 3, 0)
+    side.synchronize()
+    assert torch.equal(other[0], base[0]) and torch.equal(other[1], base[1])
+    q, m, lens, seen = x["q"][:, 0].contiguous().cuda(), x["m"].cuda(), x["lens"].cuda(), x["seen"].cuda()
+    pad = 4096
+    raw = torch.full((pad + d.batch * d.n_heads * d.d_v + pad,), 123.0, device="cuda")
+    o = raw[pad:-pad].view(d.batch, d.n_heads, d.d_v)
+    rawl = torch.full((pad + d.batch * d.n_heads + pad,), 123.0, device="cuda")
+    lse = rawl[pad:-pad].view(d.batch, d.n_heads)
+    n = gva.gva_q4_decode_workspace_size(d, 3, 0)
+    raww = torch.full((n + 8192,), 0x77, dtype=torch.uint8, device="cuda")
+    ws = raww[4096:4096 + n]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gva.gva_q4_decode_step(d, q, m, x["vc"], x["sc"], x["kc"], lens, 3, o, lse, workspace=ws, seen=seen)
+    for _ in range(4):
+        o.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, base[0]) and torch.equal(lse, base[1])
+        step(x, 2, 0)
+        torch.cuda.synchronize()
+    for r in (raw, rawl):
+        assert bool((r[:pad] == 123.0).all()) and bool((r[-pad:] == 123.0).all())
+    assert bool((raww[:4096] == 0x77).all()) and bool((raww[4096 + n:] == 0x77).all())
+
+
+# -------------------------------------------------------------- weights
+def weights_case(x, N, decay=1.0, in_place=False):
+    """Runs the call; checks it against the 64-bit sums.  A weight is off by
+    its score's error (see check_step; fp32 caches: 2^-24 per term) and the
+    log-sum-exp's, as a factor, and the sum by 2^-24 per term more."""
+    d = x["d"]
+    sc, size = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], x["G"])
+    lse = torch.logsumexp(sc, -1)
+    lse32 = lse.float()
+    g = torch.Generator().manual_seed(99)
+    w = torch.rand(d.batch, d.t_max, generator=g)
+    L = x["lens"].clamp(0, d.t_max)
+    live = torch.arange(d.t_max) < L.unsqueeze(1)
+    w_dev = w.masked_fill(~live, math.nan).cuda()
+    out = w_dev.clone() if in_place else torch.full((d.batch, d.t_max), 55.0, device="cuda")
+    ws = gva.weights_workspace_for(d, N)
+    ws.fill_(0xFF)
+    gva.gva_accumulate_weights(d, N, x["q"].cuda(), x["m"].cuda(), x["vc"], x["sc"], x["kc"], x["lens"].cuda(), lse32.cuda(),
+                               out if in_place else (w_dev if decay else None), out, workspace=ws, seen=x["seen"].cuda(),
+                               decay=decay)
+    finite = torch.isfinite(lse32)
+    p = torch.exp(sc - torch.where(finite, lse32.double(), torch.zeros_like(lse)).unsqueeze(-1)) * finite.unsqueeze(-1)
+    part = 2.0 ** -24 if d.dtype == gva.GVA_DTYPE_F32 else 2.0 ** -18
+    dx = size * (part + 280 * 2.0 ** -24) + 4 * 2.0 ** -24 * (1 + lse.abs().nan_to_num(0, 0, 0).unsqueeze(-1) + size)
+    terms = N * d.n_heads
+    want = p.sum((1, 2)) + decay * w.double()
+    tol = (p * torch.expm1(dx)).sum((1, 2)) + 2.0 ** -23 * (terms + 4) * want + 1e-30
+    got = out.cpu().double()
+    err = (got - want).abs()
+    assert bool((err <= tol)[live].all()), float((err / tol)[live].max())
+    rest = got[~live]
+    assert bool(torch.isnan(rest).all()) if in_place else bool((rest == 55.0).all())
+    return out
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16", "f32"])
+@pytest.mark.parametrize("G,hpg,d_v,d_c,d_r", [(1, 1, 64, 64, 0), (2, 4, 128, 64, 16), (3, 8, 64, 32, 40), (8, 2, 128, 128, 64),
+                                               (11, 3, 64, 64, 8)])
+@pytest.mark.parametrize("N", [1, 7])
+def test_weights(cache, G, hpg, d_v, d_c, d_r, N):
+    T = 160
+    lens = [0, 1, 3, 31, 33, T, 97, T + 40, -3]
+    x = problem(len(lens), T, G * hpg, G, d_v, d_c, d_r, lens, N=N, extra=29, cache=cache, seed=G * 100 + d_r + N)
+    note(f"weights {cache} G={G} hpg={hpg} d={d_v}/{d_c}/{d_r} N={N}")
+    weights_case(x, N)
+    weights_case(x, N, decay=0.0)
+    weights_case(x, N, decay=0.75, in_place=True)
+
+
+@gpu
+@pytest.mark.parametrize("cache,d_v,d_r", [("f32", 20, 4), ("f32", 256, 64), ("f32", 68, 0)])
+def test_weights_fp32_shapes(cache, d_v, d_r):
+    x = problem(2, 96, 6, 2, d_v, 12, d_r, [96, 41], N=3, cache=cache, seed=d_v)
+    note(f"weights fp32 d={d_v}/{d_r}")
+    weights_case(x, 3)
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16"])
+def test_weights_long_window(cache):
+    """More queries than a product has columns, every row of a short prompt."""
+    x = problem(1, 96, 8, 2, 64, 64, 16, [96], N=96, cache=cache, seed=11)
+    note(f"weights window {cache}")
+    one = weights_case(x, 96)
+    assert torch.equal(one, weights_case(x, 96))
+    x = problem(2, 2080, 8, 2, 64, 64, 16, [2080, 1500], N=5, cache=cache, seed=12)
+    weights_case(x, 5)
+
+
+# ------------------------------------------------------------- eviction
+def evict_case(B, T, G, d_v, d_r, cache, lens, keep, first=0, recent=0, with_pos=True, weights=None, seed=0, runs=2):
+    d = dims(batch=B, n_heads=G, n_groups=G, d_v=d_v, d_r=d_r, t_max=T, dtype="f32" if cache == "f32" else "bf16")
+    g = torch.Generator().manual_seed(seed)
+    lens = torch.tensor(lens, dtype=torch.int32)
+    L = lens.clamp(0, T)
+    w = torch.randint(0, 20, (B, T), generator=g).float() / 8 if weights is None else weights   # many alike
+    pos = torch.stack([torch.randperm(2 * T, generator=g)[:T] for _ in range(B)]).to(torch.int32) if with_pos else \
+        torch.arange(T, dtype=torch.int32).expand(B, T).contiguous()
+    seen = torch.full((B,), 2 * T, dtype=torch.int32) if with_pos else L.clone()
+    if cache == "q4":
+        c = torch.randint(0, 256, (B, G, T, d_v // 2), generator=g, dtype=torch.int32).to(torch.uint8)
+        s = torch.randint(0, 256, (B, G, T, d_v // 32), generator=g, dtype=torch.int32).to(torch.uint8)
+        rows = list(ref.unpack(c, s))
+        vc, sc = c.cuda(), s.cuda()
+    else:
+        v = torch.randn(B, G, T, d_v, generator=g).to(d.torch_dtype)
+        rows = [v.clone()]
+        vc, sc = gva.tiled(v).cuda(), None
+    kr = torch.randn(B, T, d_r, generator=g).to(d.torch_dtype)
+    kc = gva.tiled(kr).cuda() if d_r else None
+    new_l = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    new_w = torch.full((B, T), 9.0, device="cuda")
+    new_p = torch.full((B, T), 9, dtype=torch.int32, device="cuda") if with_pos else None
+    ws = gva.evict_workspace_for(d)
+    ws.fill_(0xFF)
+    wd, pd, ld, sd = w.cuda(), pos.cuda() if with_pos else None, lens.cuda(), seen.cuda()
+    for _ in range(runs):                                # a call can be repeated
+        gva.gva_evict_rows(d, keep, first, recent, vc, sc, kc, ld, wd, new_l, new_w, workspace=ws,
+                           seen=sd if with_pos else None, row_pos=pd, new_row_pos=new_p)
+    want_w, want_p = torch.zeros(B, T), torch.full((B, T), -1, dtype=torch.int32)
+    plan = ref.evict(w, L, pos, seen, keep, first, recent)
+    for b, (n, moves, src) in enumerate(plan):
+        assert int(new_l[b]) == n
+        for to, of in moves:
+            for x in rows:
+                x[b, :, to] = x[b, :, of]
+            kr[b, to] = kr[b, of]
+        for to, of in src.items():
+            want_w[b, to], want_p[b, to] = w[b, of], pos[b, of]
+    assert torch.equal(new_w.cpu().view(torch.int32), want_w.view(torch.int32))
+    if with_pos:
+        assert torch.equal(new_p.cpu(), want_p)
+    got = list(ref.unpack(vc.cpu(), sc.cpu())) if cache == "q4" else [gva.untiled(vc.cpu())]
+    for x, y in zip(got, rows):
+        assert torch.equal(x, y)
+    if d_r:
+        assert torch.equal(gva.untiled(kc.cpu()), kr)
+
+
+@gpu
+@pytest.mark.parametrize("cache,G,d_v,d_r", [("q4", 2, 64, 16), ("q4", 3, 128, 0), ("bf16", 2, 128, 24), ("bf16", 1, 72, 8),
+                                             ("f32", 3, 20, 4)])
+@pytest.mark.parametrize("keep,first,recent", [(1, 0, 0), (40, 0, 0), (64, 4, 60), (100, 3, 20), (159, 0, 9), (160, 0, 0), (500, 1, 1)])
+def test_evict(cache, G, d_v, d_r, keep, first, recent):
+    T = 160
+    lens = [0, 1, 40, 41, 64, 65, 100, T, T + 9, -2]
+    note(f"evict {cache} G={G} d={d_v}/{d_r} keep={keep} {first} {recent}")
+    evict_case(len(lens), T, G, d_v, d_r, cache, lens, keep, first, recent, seed=keep)
+    evict_case(len(lens), T, G, d_v, d_r, cache, lens, keep, first, recent, with_pos=False, seed=keep + 1)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["equal", "special", "close", "increasing", "decreasing"])
+def test_evict_orders(kind):
+    B, T, keep = 2, 2112, 1000
+    g = torch.Generator().manual_seed(4)
+    if kind == "equal":
+        w = torch.full((B, T), 0.5)
+    elif kind == "special":
+        few = torch.tensor([0.0, -0.0, math.nan, math.inf, -math.inf, -1.0, 1e-40, -1e-40, 3.0, 3.4e38])
+        w = few[torch.randint(0, 10, (B, T), generator=g)]
+    elif kind == "close":                               # one binade, then next to each other
+        w = torch.cat((1.0 + torch.rand(1, T, generator=g) * 1e-4, 1.0 + torch.randint(0, 300, (1, T), generator=g) * 2.0 ** -23))
+    else:
+        w = torch.arange(T).float().expand(B, T).contiguous()
+        w = -w if kind == "decreasing" else w
+    note(f"evict order {kind}")
+    evict_case(B, T, 1, 64, 8, "q4", [T, T - 1], keep, 2, 30, weights=w, seed=5)
+
+
+@gpu
+@pytest.mark.parametrize("T,L,keep", [(16416, 16400, 9000), (70016, 70016, 20000), (131072, 131000, 130999), (4128, 4097, 4096)])
+def test_evict_long(T, L, keep):
+    w = torch.randn(1, T, generator=torch.Generator().manual_seed(T)).mul(1.5).exp()
+    note(f"evict long T={T} keep={keep}")
+    evict_case(1, T, 1, 64, 0, "q4", [L], keep, 4, 64, weights=w, seed=6)
+
+
+# ------------------------------------------------------------- together
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16"])
+def test_generation_with_eviction(cache):
+    """A prompt, then decode steps that append, attend, add up weights and
+    evict at a budget: each step against a 64-bit attention over the rows that
+    a plain simulation keeps."""
+    B, T, H, G, dv, dr, budget, steps = 2, 160, 8, 2, 64, 16, 60, 40
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=dv, d_c=dv, d_r=dr, t_max=T)
+    g = torch.Generator().manual_seed(21)
+    m = (torch.randn(H, dv, dv, generator=g) / 8).to(torch.bfloat16)
+    note(f"generation with eviction, {cache}")
+    new = [70, 33]                                      # prompt lengths
+    lens = torch.zeros(B, dtype=torch.int32)
+    seen = torch.zeros(B, dtype=torch.int32)
+    if cache == "q4":
+        vc, sc = gva.q4_cache(d)
+    else:
+        vc, sc = torch.zeros(B, G, T, dv, dtype=torch.bfloat16, device="cuda"), None
+    kc = torch.zeros(B, T, dr, dtype=torch.bfloat16, device="cuda")
+    rp = torch.full((B, T), -1, dtype=torch.int32, device="cuda")
+    weights = torch.zeros(B, T, device="cuda")
+    held = [[] for _ in range(B)]                       # the simulation: (position, value rows, rotated key, weight)
+
+    def append(counts):
+        nonlocal lens, seen
+        n = sum(counts)
+        v, k = torch.randn(n, G, dv, generator=g).to(torch.bfloat16), torch.randn(n, dr, generator=g).to(torch.bfloat16)
+        seq = torch.cat([torch.full((c,), b) for b, c in enumerate(counts)]).to(torch.int32)
+        row = torch.cat([int(lens[b]) + torch.arange(c) for b, c in enumerate(counts)]).to(torch.int32)
+        pos = torch.cat([int(seen[b]) + torch.arange(c) for b, c in enumerate(counts)]).to(torch.int32)
+        call = (gva.gva_q4_append_kv, (d, vc, sc)) if cache == "q4" else (gva.gva_append_rows, (d, vc))
+        call[0](*call[1], kc, v.cuda(), k.cuda(), seq.cuda(), row.cuda(), pos=pos.cuda(), row_pos=rp)
+        for r in range(n):
+            val = ref.values(*ref.quantize(v[r])) if cache == "q4" else v[r].double()
+            held[int(seq[r])].append([int(pos[r]), val, ref.rotate(k[r], int(pos[r])).to(torch.bfloat16).double(), 0.0])
+        step_by = torch.tensor(counts, dtype=torch.int32)
+        lens, seen = lens + step_by, seen + step_by
+
+    append(new)
+    for i in range(steps):
+        if i:
+            append([1, 1])
+        q = torch.randn(B, H, dv + dr, generator=g).to(torch.bfloat16)
+        ld, sd = lens.cuda(), seen.cuda()
+        if cache == "q4":
+            o, lse = gva.q4_decode(d, q.cuda(), m.cuda(), vc, sc, kc, ld, seen=sd)
+        else:
+            far = gva.make_dims(B, H, G, dv, dv, dr, 1 << 20, "bf16")
+            qa, qr = torch.empty(B, H, dv, device="cuda"), torch.empty(B, H, dr, device="cuda")
+            gva.gva_absorb_query(far, q.cuda(), m.cuda(), sd, qa, qr)
+            op, lp = torch.empty(B, H, 1, dv, device="cuda"), torch.empty(B, H, 1, device="cuda")
+            gva.gva_decode_attention(d, vc, kc, ld, 1, op, lp, q_abs=qa, q_rot=qr)
+            o, lse = op[:, :, 0], lp[:, :, 0].contiguous()
+        gva.accumulate_weights(d, q.cuda(), m.cuda(), vc, kc, ld, lse, weights, v4_scale=sc, seen=sd)
+        got_w, got_p = weights.cpu().double(), rp.cpu()
+        for b in range(B):
+            n = int(lens[b])
+            v = torch.stack([h[1] for h in held[b]], 1).unsqueeze(0)
+            k = torch.stack([h[2] for h in held[b]]).unsqueeze(0)
+            x, _ = ref.scores(q[b:b + 1].unsqueeze(1), m, v, k, [n], [int(seen[b])], G)
+            ro, rl = ref.attend(x, v, G)
+            # values up to 6; scores off by under 1e-4 as in check_step
+            assert float((o[b].cpu().double() - ro[0, 0]).abs().max()) <= 6e-4
+            p = torch.exp(x - rl.unsqueeze(-1)).sum((0, 1, 2))
+            for t in range(n):
+                held[b][t][3] += float(p[t])
+                assert abs(held[b][t][3] - float(got_w[b, t])) <= 1e-4 * (1 + held[b][t][3])
+                assert held[b][t][0] == int(got_p[b, t])
+        new_l, weights, rp = gva.evict(d, budget, vc, kc, ld, weights, n_first=2, n_recent=8, v4_scale=sc, seen=sd, row_pos=rp)
+        # the same choice from the same weights (the device's, so that rounding decides nothing)
+        pos = torch.full((B, T), -1, dtype=torch.int32)
+        for b in range(B):
+            pos[b, :len(held[b])] = torch.tensor([h[0] for h in held[b]])
+        for b, (n, moves, _) in enumerate(ref.evict(got_w.float(), lens, pos, seen, budget, 2, 8)):
+            for to, of in moves:
+                held[b][to] = held[b][of]
+            del held[b][n:]
+        lens = new_l.cpu()
+        assert [len(h) for h in held] == lens.tolist()
+    assert lens.tolist() == [budget, budget]
+
+
+@gpu
+def test_prompt_over_a_4_bit_cache():
+    """Append a prompt, unpack, prefill; then the step at its last token agrees
+    with the prompt's last row."""
+    B, T, H, G, dv, dr, N = 2, 256, 8, 2, 128, 16, 100
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=dv, d_c=dv, d_r=dr, t_max=T)
+    x = problem(B, T, H, G, dv, dv, dr, [180, 256], N=N, seed=31)
+    note("prompt over a 4-bit cache")
+    values = torch.full((B, G, T, dv), math.nan, dtype=torch.bfloat16, device="cuda")
+    lens = x["lens"].cuda()
+    gva.gva_q4_unpack_kv(d, x["vc"], x["sc"], lens, values)
+    o, lse = gva.prefill(d, x["q"].cuda(), x["m"].cuda(), values, x["kc"], lens)
+    sc, _ = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], G)
+    ro, rl = ref.attend(sc, x["v"], G)
+    assert float((o.cpu().double() - ro).abs().max()) <= 2e-3      # the prompt kernels' fp16 weights
+    so, sl = gva.q4_decode(d, x["q"][:, -1].contiguous().cuda(), x["m"].cuda(), x["vc"], x["sc"], x["kc"], lens)
+    assert float((so - o[:, -1]).abs().max()) <= 2e-3
+    w = torch.zeros(B, T, device="cuda")
+    gva.accumulate_weights(d, x["q"].cuda(), x["m"].cuda(), x["vc"], x["kc"], lens, lse, w, v4_scale=x["sc"])
+    # every query's weights sum to one over the rows it sees
+    assert float((w.sum(-1).cpu().double() - N * H).abs().max()) <= 1e-3 * N * H
