@@ -35,8 +35,7 @@ __device__ __forceinline__ bf16x8 dequant8(unsigned w, unsigned byte) {
   bf16x8 out;
   out[0] = a[0]; out[1] = a[1]; out[2] = b[0]; out[3] = b[1];
   out[4] = c[0]; out[5] = c[1]; out[6] = d[0]; out[7] = d[1];
-  if (byte == kScaleNaN) out = as_bf16x8(u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u});
-  return out;
+  return out;                                  // (byte 255 is an infinite scale here, and the converter gives NaN)
 }
 
 inline size_t round256(size_t x) { return (x + 255) / 256 * 256; }

@@ -155,6 +155,28 @@ __global__ void __launch_bounds__(kThreads) q4_unpack_kernel(Q4UnpackParams p) {
 struct Q4DecodeParams {
   DecodeArgs a;                                // a.v: the codes
   const uint8_t* scales;
+  double inv_freq[kMaxPairs];
+};
+
+// The leading scalar arguments, in registers before a wave starts (see
+// GVA_DECODE_HEAD_ARGS): what the first memory requests need.  head_q, head_m:
+// the raw query and the maps, or the absorbed and the rotated query.  head_seen:
+// NULL, or the tokens that each sequence has had.
+#define GVA_Q4_HEAD_ARGS                                                                                       \
+  const int32_t *head_lens, const int32_t *head_seen, const void *head_q, const void *head_m, void *head_codes, \
+      int32_t head_dims, int32_t head_B, int32_t head_G, int32_t head_split_rows
+
+constexpr int kQ4Waves = 8;
+
+template <int HPG, int DV, int NRC, int NW>
+struct Q4Cfg {
+  static constexpr int DEPTH = 2, OCC = 2;
+  // absorption: loads of four map rows (of 128 columns) per round, so that the
+  // heads' maps are one round over the waves where registers allow it
+  static constexpr int AR0 = DV * HPG / (4 * NW);
+  static constexpr int AR = AR0 < 4 ? 4 : (AR0 > 16 ? 16 : AR0);
+  static constexpr int QS = DV + 4, QR = 32 * NRC + 4;   // padded rows of the query in LDS (floats)
+  static constexpr int PITCH = DV * 2 + 16;    // bytes of a row of the wave's tile in LDS
 };
 
 template <int DV, int NRC>
@@ -164,16 +186,43 @@ struct Q4Tile {
   bf16x8 k[2][NRC > 0 ? NRC : 1];
 };
 
+// Eight bf16 of column n of an LDS tile: four rows at p and four at p + step.
+// Within 16 lanes ds_read_b64_tr_b16 takes four values from each lane's address,
+// lanes 4 r .. 4 r + 3 a row of 16, and hands lane n column n of the four rows.
+__device__ __forceinline__ bf16x8 read_transposed(const uint8_t* p, int step) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* Lds;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + step));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
 // One (sequence, group, split) per workgroup; its waves take interleaved tiles
 // of 32 rows.  As in the bf16 kernel a head has two columns of the products, its
-// absorbed query (and its softmax weights) as bf16 high and low parts.
-template <int HPG, int DV, int NRC>
-__global__ void __launch_bounds__(kThreads) q4_decode_kernel(Q4DecodeParams p) {
-  const DecodeArgs& a = p.a;
-  constexpr int NC = DV / 32, NB = DV / 16, NS = DV / kScaleCols, DEPTH = 4, NW = kWaves;
-  constexpr int RS = DV + 2;
+// absorbed query (and its softmax weights) as bf16 high and low parts, and with
+// FUSED the workgroup absorbs its heads' queries itself while its first tiles
+// are on their way.
+template <int HPG, int DV, int NRC, int NW, bool FUSED>
+__global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_decode_kernel(GVA_Q4_HEAD_ARGS,
+                                                                                            Q4DecodeParams p) {
+  using Cfg = Q4Cfg<HPG, DV, NRC, NW>;
   using TileT = Q4Tile<DV, NRC>;
-  __shared__ __attribute__((aligned(16))) float red[NW * HPG * RS];
+  constexpr int NC = DV / 32, NB = DV / 16, NS = DV / kScaleCols, DEPTH = Cfg::DEPTH, NT = 64 * NW;
+  constexpr int RS = DV + 2, PITCH = Cfg::PITCH, AR = Cfg::AR, QS = Cfg::QS, QR = Cfg::QR;
+  constexpr int LDS_TR = NW * 32 * PITCH, LDS_RED = NW * HPG * RS * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[LDS_TR > LDS_RED ? LDS_TR : LDS_RED];
+  __shared__ __attribute__((aligned(16))) float qlds[FUSED ? HPG * (QS + QR) : 1];
+  DecodeArgs a = p.a;
+  a.lens = head_lens;
+  a.v = head_codes;
+  a.d_c = head_dims & 1023;
+  a.d_r = head_dims >> 10 & 127;
+  a.S = head_dims >> 17 & 511;
+  a.B = head_B;
+  a.G = head_G;
+  a.H = head_G * HPG;
+  a.split_rows = head_split_rows;
+
   int b, s, g;
   bool empty_slot;
   if (!work_item(a, b, s, g, empty_slot)) return;
@@ -183,12 +232,66 @@ __global__ void __launch_bounds__(kThreads) q4_decode_kernel(Q4DecodeParams p) {
   const int h0 = g * HPG;
   const bool active = n < 2 * HPG;
   const bool is_lo = n >= HPG;
-  const int hq = h0 + (!active ? 0 : (is_lo ? 2 * HPG - 1 - n : n));
+  const int col_head = !active ? 0 : (is_lo ? 2 * HPG - 1 - n : n);
   const bf16x8 zero8 = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
-  const int L = clamp_len(a.lens, b, a.t_max);
+  const int len_b = *(const __attribute__((address_space(4))) int32_t*)(head_lens + b);
+  const int32_t* const seen_at = head_seen != nullptr ? head_seen : head_lens;
+  const int seen_b = *(const __attribute__((address_space(4))) int32_t*)(seen_at + b);
+  if (empty_slot && s > 0) {                   // bounded chunks: a split with no rows
+    if (tid < HPG) a.lse_part[((int64_t)b * a.H + h0 + tid) * a.S + s] = -INFINITY;
+    return;
+  }
+
+  // ---- the query's loads, which need no length.  Absorption, q~[i] = sum_k
+  // q[k] M_h[i][k]: a job is 4 AR rows of a head's map, wave w taking jobs w, w +
+  // NW, ...; a load covers four whole rows of 128 columns (16 lanes of 16 bytes).
+  constexpr int ARB = DV / 4 / AR, NJOB = HPG * ARB;
+  const int W = a.d_c + a.d_r;
+  const int a_row = lane >> 4, a_col = 8 * (lane & 15);
+  u32x4 am[FUSED ? AR : 1], xq = {0u, 0u, 0u, 0u};
+  f32x4 xa[FUSED ? 1 : NC][2], xr[NRC > 0 ? NRC : 1][2];
+  const int npair = a.d_r / 2, ptid = NT - 1 - tid;
+  const bool has_pair = FUSED && ptid < HPG * npair;
+  const int pair_h = npair > 0 ? ptid / npair : 0, pair_i = npair > 0 ? ptid % npair : 0;
+  uint32_t rq_bits = 0u;
+  double qfreq = 0.0;
+  auto load_round = [&](int job, int seg) {    // columns past d_c: a valid piece, against zeros of the query
+    const int h = h0 + job / ARB, i0 = (job % ARB) * 4 * AR + a_row, col = min(128 * seg + a_col, a.d_c - 8);
+    const uint16_t* mh = static_cast<const uint16_t*>(head_m) + ((int64_t)h * DV + i0) * a.d_c + col;
+    xq = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(head_q) + ((int64_t)b * a.H + h) * W + col);
+#pragma unroll
+    for (int r = 0; r < AR; ++r) am[r] = *reinterpret_cast<const u32x4*>(mh + (int64_t)(4 * r) * a.d_c);
+  };
+  if constexpr (FUSED) {
+    if (has_pair) {
+      rq_bits = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(head_q) +
+                                                   ((int64_t)b * a.H + h0 + pair_h) * W + a.d_c + 2 * pair_i);
+      qfreq = p.inv_freq[pair_i];
+    }
+    if (w < NJOB) load_round(w, 0);
+  } else {
+    const int hq = h0 + col_head;
+    const float* qa = static_cast<const float*>(head_q) + ((int64_t)b * a.H + hq) * DV + qd * (DV / 4);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      xa[c][0] = *reinterpret_cast<const f32x4*>(qa + 8 * c);
+      xa[c][1] = *reinterpret_cast<const f32x4*>(qa + 8 * c + 4);
+    }
+#pragma unroll
+    for (int rc = 0; rc < NRC; ++rc) {
+      const float* qr = static_cast<const float*>(head_m) + ((int64_t)b * a.H + hq) * a.d_r + min(32 * rc + 8 * qd, a.d_r - 8);
+      xr[rc][0] = *reinterpret_cast<const f32x4*>(qr);
+      xr[rc][1] = *reinterpret_cast<const f32x4*>(qr + 4);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  request_args(a);
+  asm volatile("" ::"s"(p.scales) : "memory");
+
+  const int L = len_b < 0 ? 0 : (len_b > a.t_max ? a.t_max : len_b);
   int r0, r1;
   split_rows(L, a.S, a.split_rows, s, r0, r1);
-  if ((empty_slot || r0 >= r1) && s > 0) {
+  if (r0 >= r1 && s > 0) {                     // an empty split past the first: lse only
     if (tid < HPG) a.lse_part[((int64_t)b * a.H + h0 + tid) * a.S + s] = -INFINITY;
     return;
   }
@@ -227,110 +330,168 @@ __global__ void __launch_bounds__(kThreads) q4_decode_kernel(Q4DecodeParams p) {
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // the query operands, columns in the codes' order
+  // ---- the query operands, scaled, columns in the codes' order
   bf16x8 bq[NC], bk[NRC > 0 ? NRC : 1];
-  {
-    const float* qa = a.q_abs + ((int64_t)b * a.H + hq) * DV + qd * (DV / 4);
+  if constexpr (FUSED) {
+    float* const qs = qlds;                    // [HPG][QS]
+    float* const qrs = qlds + HPG * QS;        // [HPG][QR]
+    const int nseg = (a.d_c + 127) / 128;
+    auto absorb_job = [&](int job, bool loaded) {
+      float v[AR];
+#pragma unroll
+      for (int r = 0; r < AR; ++r) v[r] = 0.f;
+      for (int seg = 0; seg < nseg; ++seg) {
+        if (!(loaded && seg == 0)) load_round(job, seg);
+        const u32x4 qv = 128 * seg + a_col < a.d_c ? xq : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < AR; ++r) v[r] += dot8_bf16(am[r], qv);
+      }
+      float* dst = qs + job / ARB * QS + (job % ARB) * 4 * AR + a_row;
+#pragma unroll
+      for (int r = 0; r < AR; ++r) dst[4 * r] = sum16(v[r]) * a.scale_log2;   // every lane of a row the same value
+    };
+    if (w < NJOB) absorb_job(w, true);
+    for (int job = w + NW; job < NJOB; job += NW) absorb_job(job, false);
+    if (has_pair) {                            // the positional slice at the token's position
+      const int at = head_seen != nullptr ? seen_b : L;
+      float y0, y1;
+      rotate_query_pair(bf16_bits_to_f32(rq_bits & 0xFFFFu), bf16_bits_to_f32(rq_bits >> 16),
+                        (double)(at > 0 ? at - 1 : 0) * qfreq, a.scale_log2, y0, y1);
+      qrs[pair_h * QR + 2 * pair_i] = y0;
+      qrs[pair_h * QR + 2 * pair_i + 1] = y1;
+    }
+    if constexpr (NRC > 0) {
+      for (int i = tid; i < HPG * 32 * NRC; i += NT)
+        if (i % (32 * NRC) >= a.d_r) qrs[i / (32 * NRC) * QR + i % (32 * NRC)] = 0.f;
+    }
+    __syncthreads();
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+      const float* src = qs + col_head * QS + qd * (DV / 4) + 8 * c;
       float x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = qa[8 * c + j] * a.scale_log2;
+      for (int j = 0; j < 8; ++j) x[j] = src[j];
       bq[c] = active ? split_hi_lo(x, is_lo) : zero8;
     }
 #pragma unroll
     for (int rc = 0; rc < NRC; ++rc) {
-      const bool in_range = 32 * rc + 8 * qd < a.d_r;
-      const float* qr = a.q_rot + ((int64_t)b * a.H + hq) * a.d_r + min(32 * rc + 8 * qd, a.d_r - 8);
+      const float* src = qrs + col_head * QR + 32 * rc + 8 * qd;
       float x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = qr[j] * a.scale_log2;
-      bk[rc] = (active && in_range) ? split_hi_lo(x, is_lo) : zero8;
+      for (int j = 0; j < 8; ++j) x[j] = src[j];
+      bk[rc] = active ? split_hi_lo(x, is_lo) : zero8;
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = xa[c][j >> 2][j & 3] * a.scale_log2;
+      bq[c] = active ? split_hi_lo(x, is_lo) : zero8;
+    }
+#pragma unroll
+    for (int rc = 0; rc < NRC; ++rc) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = xr[rc][j >> 2][j & 3] * a.scale_log2;
+      bk[rc] = active && 32 * rc + 8 * qd < a.d_r ? split_hi_lo(x, is_lo) : zero8;
     }
   }
-  // identity selectors for the V transpose
-  bf16x8 esel[2];
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    u32x4 u = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (8 * qd + j == n + 16 * half) u[j >> 1] |= 0x3F80u << (16 * (j & 1));
-    esel[half] = as_bf16x8(u);
-  }
+  // the wave's tile: where the lane writes its pieces, and where it reads V^T
+  uint8_t* const tr = lds + w * 32 * PITCH;
+  uint8_t* const tr_put = tr + n * PITCH + qd * (DV / 2);
+  // The transposing LDS read hands lane (n, qd) column n of rows 4 qd .. 4 qd +
+  // 3 (and 16 more), the order in which the score product returns the weights.
+  const uint8_t* const tr_get = tr + (4 * qd + (n >> 2)) * PITCH + 8 * (n & 3);
 
-  float m_run = -__FLT_MAX__, l_run = 0.f;
+  // no tile before the first: rows and weights of 0
+  for (int i = lane * 16; i < 32 * PITCH; i += 64 * 16) *reinterpret_cast<u32x4*>(tr + i) = u32x4{0u, 0u, 0u, 0u};
+  bf16x8 bp = zero8;
+  float m_run = -__FLT_MAX__;
+  f32x4 l_run = {0.f, 0.f, 0.f, 0.f};          // the sum of a column's weights, four times
+  const bf16x8 ones = as_bf16x8(u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+  const uint32_t lo_mask = is_lo ? 0xFFFF0000u : 0u;
   f32x4 acc[NB];
 #pragma unroll
   for (int ib = 0; ib < NB; ++ib) acc[ib] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   auto compute_tile = [&](TileT& t, int row0) {
-    bf16x8 v[2][NC];
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const unsigned byte = hf ? t.s >> 8 & 255u : t.s & 255u;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) v[hf][c] = dequant8(t.w[DV == 128 ? hf : 0][DV == 128 ? c : 2 * hf + c], byte);
-    }
     const bool tail = row0 + kTileRows > r1;
-    if (tail) {                                // rows past the end may hold anything
+    unsigned scales = t.s;
+    if (tail) {
+      // Rows past the end may hold anything.  Codes are finite under a finite
+      // scale, and those rows' weights are 0, so only the scales are replaced
+      // (the key's NaN would reach only the row's own scores).
+      __builtin_amdgcn_sched_barrier(0);
+      if (row0 + n >= r1) scales = scales & ~255u | 127u;
+      if (row0 + 16 + n >= r1) scales = scales & 255u | 127u << 8;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // V^T of the tile before; its P.V products go between this tile's
+    // conversions and score products
+    bf16x8 vt[NB];
+#pragma unroll
+    for (int ib = 0; ib < NB; ++ib) vt[ib] = read_transposed(tr_get + 32 * ib, 16 * PITCH);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();           // this tile is written after those reads
+    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int rc = 0; rc < NRC; ++rc)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16(t.k[hf][rc], bk[rc], sc[hf]);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const bool dead = row0 + 16 * hf + n >= r1;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) v[hf][c] = dead ? zero8 : v[hf][c];
-#pragma unroll
-        for (int rc = 0; rc < NRC; ++rc) t.k[hf][rc] = dead ? zero8 : t.k[hf][rc];
+        const bf16x8 v = dequant8(t.w[DV == 128 ? hf : 0][DV == 128 ? c : 2 * hf + c], hf ? scales >> 8 : scales & 255u);
+        *reinterpret_cast<bf16x8*>(tr_put + 16 * hf * PITCH + 16 * c) = v;
+        sc[hf] = mfma16(v, bq[c], sc[hf]);
+        acc[2 * c + hf] = mfma16(vt[2 * c + hf], bp, acc[2 * c + hf]);
       }
-    }
+    l_run = mfma16(ones, bp, l_run);
     float x[8];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+    for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-      for (int c = 0; c < NC; ++c) sc = mfma16(v[hf][c], bq[c], sc);
+      for (int jj = 0; jj < 4; ++jj) x[4 * hf + jj] = sc[hf][jj] + mirror<HPG>(sc[hf][jj]);
+    if (tail) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int rc = 0; rc < NRC; ++rc) sc = mfma16(t.k[hf][rc], bk[rc], sc);
-#pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        x[4 * hf + jj] = sc[jj] + mirror<HPG>(sc[jj]);
-        if (tail && row0 + 16 * hf + 4 * qd + jj >= r1) x[4 * hf + jj] = -INFINITY;
-      }
+      for (int k = 0; k < 8; ++k)
+        if (row0 + 16 * (k >> 2) + 4 * qd + (k & 3) >= r1) x[k] = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
     }
-    float mt = x[0];
-#pragma unroll
-    for (int k = 1; k < 8; ++k) mt = fmaxf(mt, x[k]);
-    mt = max_over_rows(mt);
-    const float m_new = fmaxf(m_run, mt);
-    if (__ballot(m_new > m_run) != 0) {
+    // The running maximum of a column moves only when some score passes it by 8
+    // (log2): until then weights stay below 2^8, and most tiles need neither the
+    // maximum over the lanes nor the rescaling.
+    const float mt = fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(x[4], x[5])), fmaxf(x[6], x[7]));
+    if (__ballot(mt > m_run + 8.f) != 0) {
+      const float m_new = fmaxf(m_run, max_over_rows(mt));
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
 #pragma unroll
       for (int ib = 0; ib < NB; ++ib) acc[ib] *= alpha;
       m_run = m_new;
     }
-    float pr[8];
+    // Weights as bf16 parts: the high columns take the upper half of the fp32
+    // number, the low columns that of what it leaves (off by less than 2^-15;
+    // the sum of the weights is taken from the same parts by a product with
+    // ones, so what truncation loses on average cancels in o).
+    u32x4 parts;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      pr[k] = __builtin_amdgcn_exp2f(x[k] - m_run);
-      l_run += pr[k];
-    }
-    const bf16x8 bp = active ? split_hi_lo(pr, is_lo) : zero8;
+    for (int k = 0; k < 8; k += 2) {
+      float y[2];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-        const f32x4 t0 = mfma16(v[0][c], esel[half], z);
-        const f32x4 t1 = mfma16(v[1][c], esel[half], z);
-        bf16x8 at;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          at[j] = (__bf16)t0[j];
-          at[4 + j] = (__bf16)t1[j];
-        }
-        acc[2 * c + half] = mfma16(at, bp, acc[2 * c + half]);
+      for (int j = 0; j < 2; ++j) {
+        const float e = __builtin_amdgcn_exp2f(x[k + j] - m_run);
+        y[j] = e - __uint_as_float(__float_as_uint(e) & lo_mask);
       }
+      parts[k / 2] = __builtin_amdgcn_perm(__float_as_uint(y[1]), __float_as_uint(y[0]), 0x07060302u);
+    }
+    bp = as_bf16x8(parts);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();           // the tile's rows, written by the other lanes
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   };
   for (int jt = 0; jt < my_tiles; jt += DEPTH) {
 #pragma unroll
@@ -342,31 +503,32 @@ __global__ void __launch_bounds__(kThreads) q4_decode_kernel(Q4DecodeParams p) {
       compute_tile(buf[d], tile_row(j));
     }
   }
+#pragma unroll
+  for (int ib = 0; ib < NB; ++ib) acc[ib] = mfma16(read_transposed(tr_get + 32 * ib, 16 * PITCH), bp, acc[ib]);
+  l_run = mfma16(ones, bp, l_run);
 
   // ---- merge the waves and write this split's partial
-  l_run = sum_over_rows(l_run);
-  if (l_run == 0.f) m_run = -INFINITY;         // no row counted
+  const float l_sum = l_run[0] + mirror<HPG>(l_run[0]);
+  if (l_sum == 0.f) m_run = -INFINITY;         // no row counted
 #pragma unroll
   for (int ib = 0; ib < NB; ++ib)
 #pragma unroll
     for (int jj = 0; jj < 4; ++jj) acc[ib][jj] += mirror<HPG>(acc[ib][jj]);
+  __syncthreads();                             // the tiles' LDS holds the records from here on
+  float* const red = reinterpret_cast<float*>(lds);
   if (n < HPG) {
     float* rec = red + (w * HPG + n) * RS;
     if (qd == 0) {
       rec[0] = m_run;
-      rec[1] = l_run;
+      rec[1] = l_sum;
     }
-    // output row k = 4 qd + jj + 16 half of product c is column 8 c + k % 8 of piece k / 8
 #pragma unroll
     for (int ib = 0; ib < NB; ++ib)
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        const int k = 4 * qd + jj + 16 * (ib & 1);
-        rec[2 + (k >> 3) * (DV / 4) + 8 * (ib >> 1) + (k & 7)] = acc[ib][jj];
-      }
+      for (int jj = 0; jj < 4; ++jj) rec[2 + 16 * ib + 4 * qd + jj] = acc[ib][jj];
   }
   __syncthreads();
-  for (int idx = tid; idx < HPG * DV; idx += kThreads) {
+  for (int idx = tid; idx < HPG * DV; idx += 64 * NW) {
     const int hl = idx / DV, i = idx % DV;
     float mx = -INFINITY;
 #pragma unroll
@@ -388,30 +550,41 @@ __global__ void __launch_bounds__(kThreads) q4_decode_kernel(Q4DecodeParams p) {
   }
 }
 
-using Q4DecodeFn = void (*)(Q4DecodeParams);
+using Q4DecodeFn = void (*)(GVA_Q4_HEAD_ARGS, Q4DecodeParams);
 
-template <int HPG, int DV>
+template <int HPG, int DV, bool FUSED>
 Q4DecodeFn pick_q4_nrc(int nrc) {
   switch (nrc) {
-    case 0: return q4_decode_kernel<HPG, DV, 0>;
-    case 1: return q4_decode_kernel<HPG, DV, 1>;
-    case 2: return q4_decode_kernel<HPG, DV, 2>;
+    case 0: return q4_decode_kernel<HPG, DV, 0, kQ4Waves, FUSED>;
+    case 1: return q4_decode_kernel<HPG, DV, 1, kQ4Waves, FUSED>;
+    case 2: return q4_decode_kernel<HPG, DV, 2, kQ4Waves, FUSED>;
   }
   return nullptr;
 }
 
-Q4DecodeFn pick_q4_decode(int hpg, int dv, int nrc) {
-  const bool wide = dv == 128;
+template <int HPG>
+Q4DecodeFn pick_q4_dv(int dv, int nrc, bool fused) {
+  if (dv == 128) return fused ? pick_q4_nrc<HPG, 128, true>(nrc) : pick_q4_nrc<HPG, 128, false>(nrc);
+  return fused ? pick_q4_nrc<HPG, 64, true>(nrc) : pick_q4_nrc<HPG, 64, false>(nrc);
+}
+
+Q4DecodeFn pick_q4_decode(int hpg, int dv, int nrc, bool fused) {
   switch (hpg) {
-    case 1: return wide ? pick_q4_nrc<1, 128>(nrc) : pick_q4_nrc<1, 64>(nrc);
-    case 2: return wide ? pick_q4_nrc<2, 128>(nrc) : pick_q4_nrc<2, 64>(nrc);
-    case 4: return wide ? pick_q4_nrc<4, 128>(nrc) : pick_q4_nrc<4, 64>(nrc);
-    case 8: return wide ? pick_q4_nrc<8, 128>(nrc) : pick_q4_nrc<8, 64>(nrc);
+    case 1: return pick_q4_dv<1>(dv, nrc, fused);
+    case 2: return pick_q4_dv<2>(dv, nrc, fused);
+    case 4: return pick_q4_dv<4>(dv, nrc, fused);
+    case 8: return pick_q4_dv<8>(dv, nrc, fused);
   }
   return nullptr;
+}
+
+// Whether the workgroups absorb their queries themselves.
+bool q4_fused(const gva_dims* d, int num_splits, int split_rows) {
+  return gva_prefer_fused(d, num_splits, split_rows, 0) != 0;
 }
 
 struct Q4StepLayout {
+  bool fused;
   size_t q_abs, q_rot, o_part, lse_part, bytes;   // offsets into the workspace
 };
 
@@ -422,9 +595,12 @@ int q4_step_layout(const gva_dims* d, int32_t num_splits, int32_t split_rows, Q4
     return GVA_ERR_INVALID_ARG;
   const size_t rows = (size_t)d->batch * (size_t)d->n_heads;
   L = Q4StepLayout{};
-  size_t off = round256(rows * (size_t)d->d_v * 4);
-  L.q_rot = off;
-  off += round256(rows * (size_t)d->d_r * 4);
+  L.fused = q4_fused(d, num_splits, split_rows);
+  size_t off = 0;
+  if (!L.fused) {
+    L.q_rot = off = round256(rows * (size_t)d->d_v * 4);
+    off += round256(rows * (size_t)d->d_r * 4);
+  }
   if (num_splits > 1) {
     L.o_part = off;
     off += round256(rows * (size_t)num_splits * (size_t)d->d_v * 4);
@@ -529,37 +705,32 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
     return GVA_ERR_INVALID_ARG;
   if (dims->d_c % 32 != 0 || dims->d_c < 32 || dims->d_c > 512) return GVA_ERR_UNSUPPORTED;
   const int hpg = dims->n_heads / dims->n_groups;
-  const Q4DecodeFn fn = pick_q4_decode(hpg, dims->d_v, (dims->d_r + 31) / 32);
+  const Q4DecodeFn fn = pick_q4_decode(hpg, dims->d_v, (dims->d_r + 31) / 32, L.fused);
   const long long n_items = decode_grid(dims, num_splits, split_rows);
   if (fn == nullptr || n_items > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   char* ws = static_cast<char*>(workspace);
-  float* q_abs = reinterpret_cast<float*>(ws + L.q_abs);
-  float* q_rot = dims->d_r > 0 ? reinterpret_cast<float*>(ws + L.q_rot) : nullptr;
   const int S = num_splits;
-  gva_dims at = *dims;                         // the query's position counts the tokens seen, not the rows left
-  if (seen != nullptr) at.t_max = 0x7FFFFFFF;
-  st = gva_absorb_query(&at, q, m, seen != nullptr ? seen : lens, q_abs, q_rot, stream);
-  if (st != GVA_OK) return st;
+  float *q_abs = nullptr, *q_rot = nullptr;
+  if (!L.fused) {
+    q_abs = reinterpret_cast<float*>(ws + L.q_abs);
+    q_rot = dims->d_r > 0 ? reinterpret_cast<float*>(ws + L.q_rot) : nullptr;
+    gva_dims at = *dims;                       // the query's position counts the tokens seen, not the rows left
+    if (seen != nullptr) at.t_max = 0x7FFFFFFF;
+    st = gva_absorb_query(&at, q, m, seen != nullptr ? seen : lens, q_abs, q_rot, stream);
+    if (st != GVA_OK) return st;
+  }
   Q4DecodeParams p{};
-  p.a.q_abs = q_abs;
-  p.a.q_rot = q_rot;
-  p.a.v = const_cast<void*>(v4_cache);
   p.a.kr = const_cast<void*>(kr_cache);
-  p.a.lens = lens;
   p.a.o_part = S > 1 ? reinterpret_cast<float*>(ws + L.o_part) : o;
   p.a.lse_part = S > 1 ? reinterpret_cast<float*>(ws + L.lse_part) : lse;
-  p.a.B = dims->batch;
-  p.a.H = dims->n_heads;
-  p.a.G = dims->n_groups;
-  p.a.d_v = dims->d_v;
-  p.a.d_c = dims->d_c;
-  p.a.d_r = dims->d_r;
   p.a.t_max = dims->t_max;
-  p.a.S = S;
-  p.a.split_rows = split_rows;
   p.a.scale_log2 = scale_log2(dims);
   p.scales = static_cast<const uint8_t*>(v4_scale);
-  hipLaunchKernelGGL(fn, dim3((unsigned)n_items), dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
+  fill_inv_freq(dims, p.inv_freq);
+  const int packed = dims->d_c | dims->d_r << 10 | S << 17;
+  hipLaunchKernelGGL(fn, dim3((unsigned)n_items), dim3(64 * kQ4Waves), 0, static_cast<hipStream_t>(stream), lens, seen,
+                     L.fused ? q : static_cast<const void*>(q_abs), L.fused ? m : static_cast<const void*>(q_rot),
+                     const_cast<void*>(v4_cache), packed, dims->batch, dims->n_groups, split_rows, p);
   st = launch_status();
   if (st != GVA_OK || S == 1) return st;
   return gva_combine(dims, p.a.o_part, p.a.lse_part, S, o, lse, stream);
