@@ -22,6 +22,7 @@ struct WeightParams {
   const int32_t* lens;
   const float* weights;   // may be NULL with decay 0
   float* new_weights;
+  float* part;            // [G][B][T]: row sums of a group, before they are joined
   int32_t B, H, G, N, d_v, d_r, t_max, chunk;
   float scale_log2, decay;
 };
@@ -29,18 +30,89 @@ struct WeightParams {
 constexpr int kWeightWaves = 8;
 constexpr int kWeightChunk = 512;              // most rows of a workgroup
 
-// The workgroup takes `chunk` rows of one sequence.  Wave w scores group
-// w % GP of a round of GP = min(G, 8) groups (a power of two), every
-// (8 / GP)-th tile of the chunk; a column of the products is one (query, head of
-// the group) pair, its query once as bf16 high parts and once as low parts into
-// the same sums.  A lane adds the weights of its column; the sum over the 16
-// columns of a row goes to the wave's array of row sums, and the arrays are
-// added at the end in the order of the waves: the result does not depend on
-// timing.
+// The cached rows as matrix-core operands: 32 rows, K-chunk c of the products.
 template <int DV, int NRC, bool Q4>
-__global__ void __launch_bounds__(64 * kWeightWaves) weights_bf16_kernel(WeightParams p) {
-  constexpr int NC = DV / 32, NS = DV / kScaleCols;
-  __shared__ float sums[kWeightWaves][kWeightChunk];
+struct WeightRows {
+  u32x4 v[Q4 ? DV / 64 : DV / 16];             // [half][chunk], or codes
+  unsigned s;
+  bf16x8 k[2][NRC > 0 ? NRC : 1];
+};
+
+template <int DV, int NRC, bool Q4>
+struct WeightStream {
+  static constexpr int NC = DV / 32, NS = DV / kScaleCols;
+  __amdgpu_buffer_rsrc_t vres, sres, kres;
+  int k_lane[NRC > 0 ? NRC : 1];
+  int lane, n, qd, d_r;
+
+  // rows [0, r1) of stream (b, g); loads past their last tile read zeros
+  __device__ __forceinline__ WeightStream(const WeightParams& p, int b, int g, int r1, int lane_)
+      : lane(lane_), n(lane_ & 15), qd(lane_ >> 4), d_r(p.d_r) {
+    const int64_t stream = (int64_t)b * p.G + g;
+    const int r1k = (r1 + 15) / 16 * 16, r1c = (r1 + 31) / 32 * 32;
+    const uint8_t* v = static_cast<const uint8_t*>(p.v) + stream * p.t_max * (Q4 ? DV / 2 : DV * 2);
+    const uint8_t* sc = Q4 ? p.scales + stream * p.t_max * NS : v;
+    const uint16_t* k = static_cast<const uint16_t*>(p.kr) + (int64_t)b * p.t_max * p.d_r;
+    vres = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v), (short)0, Q4 ? r1c * (DV / 2) : r1k * DV * 2, kBufferWord3);
+    sres = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(sc), (short)0, Q4 ? r1c * NS : 0, kBufferWord3);
+    kres = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(k), (short)0, r1k * p.d_r * 2, kBufferWord3);
+#pragma unroll
+    for (int rc = 0; rc < NRC; ++rc) k_lane[rc] = min(4 * rc + qd, p.d_r / 8 - 1) * 256 + n * 16;
+  }
+  template <int AUX>
+  __device__ __forceinline__ void load(WeightRows<DV, NRC, Q4>& t, int row0) const {
+    if constexpr (Q4) {
+#pragma unroll
+      for (int u = 0; u < DV / 64; ++u)
+        t.v[u] = __builtin_amdgcn_raw_buffer_load_b128(vres, lane * 16 + u * kBlockBytes, row0 * (DV / 2), AUX);
+      t.s = __builtin_amdgcn_raw_buffer_load_b16(sres, (qd * NS / 4 * 16 + n) * 2, row0 * NS, AUX);
+    } else {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          t.v[hf * NC + c] = __builtin_amdgcn_raw_buffer_load_b128(vres, qd * 256 + n * 16 + 1024 * c, (row0 + 16 * hf) * DV * 2, AUX);
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int rc = 0; rc < NRC; ++rc)
+        t.k[hf][rc] = as_bf16x8(__builtin_amdgcn_raw_buffer_load_b128(kres, k_lane[rc], (row0 + 16 * hf) * d_r * 2, 0));
+  }
+  __device__ __forceinline__ static bf16x8 chunk(const WeightRows<DV, NRC, Q4>& t, int hf, int c) {
+    if constexpr (Q4)
+      return dequant8(t.v[DV == 128 ? hf : 0][DV == 128 ? c : 2 * hf + c], hf ? t.s >> 8 : t.s & 255u);
+    else
+      return as_bf16x8(t.v[hf * NC + c]);
+  }
+  // eight scaled entries of an absorbed query, in the columns of chunk c
+  __device__ __forceinline__ void query(const float* qa, int c, float scale, float* x) const {
+    const f32x4* src = reinterpret_cast<const f32x4*>(qa + (Q4 ? qd * (DV / 4) + 8 * c : 32 * c + 8 * qd));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = src[j >> 2][j & 3] * scale;
+  }
+  __device__ __forceinline__ void query_rot(const float* qr, int rc, float scale, float* x) const {
+    const bool in = 32 * rc + 8 * qd < d_r;
+    const f32x4* src = reinterpret_cast<const f32x4*>(qr + min(32 * rc + 8 * qd, d_r - 8));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = in ? src[j >> 2][j & 3] * scale : 0.f;
+  }
+};
+
+// One query per sequence (a decode step).  The workgroup takes `chunk` rows of
+// one sequence; wave w scores group w % GP of a round of GP = min(G, 8) groups (a
+// power of two), every (8 / GP)-th tile of the chunk.  A head has two columns of
+// the products, its query's bf16 high and low parts; the high column's lanes add
+// the pair for the tile's first 16 rows and the low column's for the others, so
+// that every exponential is taken once.  A wave's sums over the heads go to its
+// group's array of row sums, which are added in order at the end: the result
+// does not depend on timing.  The log-sum-exp is the products' initial value.
+// Bound by HBM as the attention is (B32 T8K H32 G8 d 128/16 in 4 bits: see below).
+template <int HPG, int DV, int NRC, bool Q4>
+__global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) weights_step_kernel(WeightParams p) {
+  using Stream = WeightStream<DV, NRC, Q4>;
+  constexpr int NC = Stream::NC, DEPTH = NRC == 2 ? 2 : 3;
+  __shared__ __attribute__((aligned(16))) float sums[kWeightWaves][kWeightChunk];
   const int nchunks = (p.t_max + p.chunk - 1) / p.chunk;
   const int item = xcd_remap(blockIdx.x, p.B * nchunks);
   const int b = item / nchunks, r0 = item % nchunks * p.chunk;
@@ -50,99 +122,72 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_bf16_kernel(WeightP
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, qd = lane >> 4;
-  const int hpg = p.H / p.G, cols = p.N * hpg;
+  const bool active = n < 2 * HPG, is_lo = n >= HPG;
+  const int head = !active ? 0 : (is_lo ? 2 * HPG - 1 - n : n);
   int GP = 1;
   while (2 * GP <= min(p.G, kWeightWaves)) GP *= 2;
   const int TS = kWeightWaves / GP;            // waves that share a group's tiles
-  float* const mine = sums[w];
-  for (int i = lane; i < p.chunk; i += 64) mine[i] = 0.f;
   const int ntiles = (r1 - r0 + kTileRows - 1) / kTileRows;
+  const int my_tiles = ntiles > w / GP ? (ntiles - w / GP + TS - 1) / TS : 0;
+  auto tile_row = [&](int j) { return r0 + (w / GP + TS * j) * kTileRows; };
   const bf16x8 zero8 = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
-  const int r1k = (r1 + 15) / 16 * 16, r1c = (r1 + 31) / 32 * 32;
-  const __amdgpu_buffer_rsrc_t kres = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t*>(static_cast<const uint16_t*>(p.kr)) + (int64_t)b * p.t_max * p.d_r, (short)0, r1k * p.d_r * 2,
-      kBufferWord3);
+  // the lane that holds a row's sum, and the place of its four rows
+  const bool puts = n == 0 || n == HPG;
+  float* const put = &sums[w % GP][(n == HPG ? 16 : 0) + 4 * qd];
   for (int g = w % GP; g < p.G; g += GP) {
-    const int64_t stream = (int64_t)b * p.G + g;
-    const uint8_t* vbase = static_cast<const uint8_t*>(p.v) + stream * p.t_max * (Q4 ? DV / 2 : DV * 2);
-    const __amdgpu_buffer_rsrc_t vres = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(vbase), (short)0, Q4 ? r1c * (DV / 2) : r1k * DV * 2, kBufferWord3);
-    const __amdgpu_buffer_rsrc_t sres = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(Q4 ? p.scales + stream * p.t_max * NS : vbase), (short)0, r1c * NS, kBufferWord3);
-    for (int c0 = 0; c0 < cols; c0 += 16) {
-      const int col = c0 + n;
-      const bool active = col < cols;
-      const int qi = active ? col / hpg : 0;
-      const int64_t qrow = ((int64_t)b * p.N + qi) * p.H + g * hpg + (active ? col % hpg : 0);
-      const float ls = active ? p.lse[qrow] : -INFINITY;
-      const bool live = ls != -INFINITY;       // a query with nothing to see adds nothing
-      const int last = L - p.N + qi;           // the last row that the query sees
-      bf16x8 qh[NC], ql[NC], kh[NRC > 0 ? NRC : 1], kl[NRC > 0 ? NRC : 1];
-      const float* qa = p.q_abs + qrow * DV + qd * (Q4 ? DV / 4 : 8);
+    const Stream in(p, b, g, r1, lane);
+    WeightRows<DV, NRC, Q4> buf[DEPTH];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float x[8];
+    for (int d = 0; d < DEPTH - 1; ++d) {
+      in.template load<kAuxNT>(buf[d], tile_row(d));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const int64_t qrow = (int64_t)b * p.H + g * HPG + head;
+    const float ls = p.lse[qrow];
+    // -inf: a query with nothing to see, whose weights are 0
+    const float init = is_lo ? 0.f : (ls != -INFINITY ? -ls * (float)kLog2e : -INFINITY);
+    bf16x8 bq[NC], bk[NRC > 0 ? NRC : 1];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = active ? qa[(Q4 ? 8 : 32) * c + j] * p.scale_log2 : 0.f;
-        qh[c] = split_hi_lo(x, false);
-        ql[c] = split_hi_lo(x, true);
-      }
+    for (int c = 0; c < NC; ++c) {
+      float x[8];
+      in.query(p.q_abs + qrow * DV, c, p.scale_log2, x);
+      bq[c] = active ? split_hi_lo(x, is_lo) : zero8;
+    }
 #pragma unroll
-      for (int rc = 0; rc < NRC; ++rc) {
-        const bool in = active && 32 * rc + 8 * qd < p.d_r;
-        const float* qr = p.q_rot + qrow * p.d_r + min(32 * rc + 8 * qd, p.d_r - 8);
-        float x[8];
+    for (int rc = 0; rc < NRC; ++rc) {
+      float x[8];
+      in.query_rot(p.q_rot + qrow * p.d_r, rc, p.scale_log2, x);
+      bk[rc] = active ? split_hi_lo(x, is_lo) : zero8;
+    }
+    const bool first = g < GP;
+    for (int jt = 0; jt < my_tiles; jt += DEPTH) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = in ? qr[j] * p.scale_log2 : 0.f;
-        kh[rc] = split_hi_lo(x, false);
-        kl[rc] = split_hi_lo(x, true);
-      }
-      const float init = live ? -ls * (float)kLog2e : 0.f;
-      for (int j = w / GP; j < ntiles; j += TS) {
-        const int row0 = r0 + j * kTileRows;
-        float sum[8];
+      for (int d = 0; d < DEPTH; ++d) {
+        const int j = jt + d;
+        if (j >= my_tiles) break;
+        in.template load<kAuxNT>(buf[(d + DEPTH - 1) % DEPTH], tile_row(j + DEPTH - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sc[2] = {f32x4{init, init, init, init}, f32x4{init, init, init, init}};
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          bf16x8 v[NC], k[NRC > 0 ? NRC : 1];
-          if constexpr (Q4) {
-            const unsigned sc2 = __builtin_amdgcn_raw_buffer_load_b16(sres, (qd * NS / 4 * 16 + n) * 2, row0 * NS, 0);
-            const unsigned byte = hf ? sc2 >> 8 & 255u : sc2 & 255u;
-            const u32x4 cw = __builtin_amdgcn_raw_buffer_load_b128(
-                vres, lane * 16 + (DV == 128 ? hf * kBlockBytes : 0), row0 * (DV / 2), 0);
+        for (int rc = 0; rc < NRC; ++rc)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) v[c] = dequant8(cw[DV == 128 ? c : 2 * hf + c], byte);
-          } else {
+          for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16(buf[d].k[hf][rc], bk[rc], sc[hf]);
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-              v[c] = as_bf16x8(__builtin_amdgcn_raw_buffer_load_b128(vres, qd * 256 + n * 16 + 1024 * c, (row0 + 16 * hf) * DV * 2, 0));
-          }
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int rc = 0; rc < NRC; ++rc)
-            k[rc] = as_bf16x8(__builtin_amdgcn_raw_buffer_load_b128(
-                kres, min(4 * rc + qd, p.d_r / 8 - 1) * 256 + n * 16, (row0 + 16 * hf) * p.d_r * 2, 0));
-          f32x4 sc = {init, init, init, init};
+          for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16(Stream::chunk(buf[d], hf, c), bq[c], sc[hf]);
+        f32x4 e;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            sc = mfma16(v[c], ql[c], sc);
-            sc = mfma16(v[c], qh[c], sc);
-          }
-#pragma unroll
-          for (int rc = 0; rc < NRC; ++rc) {
-            sc = mfma16(k[rc], kl[rc], sc);
-            sc = mfma16(k[rc], kh[rc], sc);
-          }
-#pragma unroll
-          for (int jj = 0; jj < 4; ++jj) {
-            const int row = row0 + 16 * hf + 4 * qd + jj;
-            // (rows past the end may hold anything: they are selected away)
-            sum[4 * hf + jj] = live && row <= last && row < r1 ? __builtin_amdgcn_exp2f(sc[jj]) : 0.f;
-          }
+        for (int jj = 0; jj < 4; ++jj) {
+          const float mine = is_lo ? sc[1][jj] : sc[0][jj], other = is_lo ? sc[0][jj] : sc[1][jj];
+          e[jj] = __builtin_amdgcn_exp2f(mine + mirror<HPG>(other));
+          if constexpr (HPG >= 2) e[jj] = dpp_add<0xB1>(e[jj]);     // over the heads' lanes
+          if constexpr (HPG >= 4) e[jj] = dpp_add<0x1B>(e[jj]);
+          if constexpr (HPG >= 8) e[jj] = dpp_add<0x141>(e[jj]);
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k] = sum16(sum[k]);
-        if (n == 0) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) mine[j * kTileRows + 16 * (k >> 2) + 4 * qd + (k & 3)] += sum[k];
+        if (puts) {
+          f32x4* at = reinterpret_cast<f32x4*>(put + (tile_row(j) - r0));
+          *at = first ? e : *at + e;
         }
       }
     }
@@ -150,11 +195,122 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_bf16_kernel(WeightP
   __syncthreads();
   for (int i = tid; i < r1 - r0; i += 64 * kWeightWaves) {
     float s = 0.f;
-#pragma unroll
-    for (int ww = 0; ww < kWeightWaves; ++ww) s += sums[ww][i];
+    for (int g = 0; g < GP; ++g) s += sums[g][i];
     const int64_t at = (int64_t)b * p.t_max + r0 + i;
     p.new_weights[at] = p.decay != 0.f ? fmaf(p.decay, p.weights[at], s) : s;
   }
+}
+
+// Many queries, or any number of heads per group.  The workgroup takes one group
+// and kWindowRows rows of one sequence; a column of the products is one (query,
+// head) pair, its query once as bf16 high parts and once as low parts into the
+// same sums, 32 columns a wave.  The waves are dealt first over the columns and
+// then over the tiles.  Sums over the columns go through LDS in a fixed order to
+// the group's row sums in the workspace, which weights_join_kernel adds up.
+constexpr int kWindowRows = 128, kWindowCols = 32;
+
+template <int DV, int NRC, bool Q4>
+__global__ void __launch_bounds__(kThreads, 2) weights_window_kernel(WeightParams p) {
+  using Stream = WeightStream<DV, NRC, Q4>;
+  constexpr int NC = Stream::NC, NK = NC + NRC;
+  __shared__ __attribute__((aligned(16))) float sums[kWaves][kWindowRows];
+  const int nchunks = (p.t_max + kWindowRows - 1) / kWindowRows;
+  const int item = xcd_remap(blockIdx.x, p.B * nchunks * p.G);
+  const int g = item % p.G, b = item / p.G / nchunks, r0 = item / p.G % nchunks * kWindowRows;
+  const int L = clamp_len(p.lens, b, p.t_max);
+  if (r0 >= L) return;
+  const int r1 = min(r0 + kWindowRows, L);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, qd = lane >> 4;
+  const int hpg = p.H / p.G, cols = p.N * hpg;
+  const int nsets = (cols + kWindowCols - 1) / kWindowCols;
+  const int WC = nsets >= 4 ? 4 : (nsets >= 2 ? 2 : 1), WT = kWaves / WC;   // waves over columns, over tiles
+  const int ntiles = (r1 - r0 + kTileRows - 1) / kTileRows;
+  const Stream in(p, b, g, r1, lane);
+  float* const mine = sums[w % WC];
+  for (int set = w % WC; set < nsets; set += WC) {
+    bf16x8 hi[2][NK], lo[2][NK];
+    float init[2];
+    int last[2];                               // the last row that the column's query sees
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb) {
+      const int col = set * kWindowCols + 16 * cb + n;
+      const bool active = col < cols;
+      const int qi = active ? col / hpg : 0;
+      const int64_t qrow = ((int64_t)b * p.N + qi) * p.H + g * hpg + (active ? col % hpg : 0);
+      const float ls = p.lse[qrow];
+      init[cb] = active && ls != -INFINITY ? -ls * (float)kLog2e : -INFINITY;
+      last[cb] = active ? L - p.N + qi : -1;
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        float x[8];
+        if (c < NC)
+          in.query(p.q_abs + qrow * DV, c, p.scale_log2, x);
+        else
+          in.query_rot(p.q_rot + qrow * p.d_r, c - NC, p.scale_log2, x);
+        hi[cb][c] = split_hi_lo(x, false);
+        lo[cb][c] = split_hi_lo(x, true);
+      }
+    }
+    for (int j = w / WC; j < ntiles; j += WT) {
+      const int row0 = r0 + j * kTileRows;
+      WeightRows<DV, NRC, Q4> t;
+      in.template load<0>(t, row0);
+      f32x4 sc[2][2];
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) sc[cb][hf] = f32x4{init[cb], init[cb], init[cb], init[cb]};
+#pragma unroll
+      for (int c = 0; c < NK; ++c)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const bf16x8 a = c < NC ? Stream::chunk(t, hf, c) : t.k[hf][c < NC ? 0 : c - NC];
+#pragma unroll
+          for (int cb = 0; cb < 2; ++cb) sc[cb][hf] = mfma16(a, lo[cb][c], sc[cb][hf]);
+#pragma unroll
+          for (int cb = 0; cb < 2; ++cb) sc[cb][hf] = mfma16(a, hi[cb][c], sc[cb][hf]);
+        }
+      // a tile that some query sees only in part, or that holds rows past the end
+      // (where anything may stand): those rows count as not seen
+      const bool edge = row0 + kTileRows > L - p.N + 1 || cols < (set + 1) * kWindowCols;
+      f32x4 e[2];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          float v[2];
+#pragma unroll
+          for (int cb = 0; cb < 2; ++cb) {
+            v[cb] = __builtin_amdgcn_exp2f(sc[cb][hf][jj]);
+            if (edge) v[cb] = row0 + 16 * hf + 4 * qd + jj <= last[cb] ? v[cb] : 0.f;
+          }
+          e[hf][jj] = sum16(v[0] + v[1]);
+        }
+      if (n < 2) {                             // lane 0: the first 16 rows' sums, lane 1 the others'
+        f32x4* at = reinterpret_cast<f32x4*>(mine + j * kTileRows + 16 * n + 4 * qd);
+        const f32x4 mine4 = n ? e[1] : e[0];
+        *at = set < WC ? mine4 : *at + mine4;
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < r1 - r0; i += kThreads) {
+    float s = 0.f;
+    for (int c = 0; c < WC; ++c) s += sums[c][i];
+    p.part[((int64_t)g * p.B + b) * p.t_max + r0 + i] = s;
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) weights_join_kernel(WeightParams p) {
+  const int b = blockIdx.y, t = blockIdx.x * kThreads + threadIdx.x;
+  if (t >= clamp_len(p.lens, b, p.t_max)) return;
+  const int64_t at = (int64_t)b * p.t_max + t;
+  float s = 0.f;
+#pragma unroll 8
+  for (int g = 0; g < p.G; ++g) s += p.part[(int64_t)g * p.B * p.t_max + at];
+  p.new_weights[at] = p.decay != 0.f ? fmaf(p.decay, p.weights[at], s) : s;
 }
 
 // fp32 storage: the same on the fp32 products, 16-row tiles, any d_v and d_r
@@ -229,16 +385,35 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_f32_kernel(WeightPa
 
 using WeightFn = void (*)(WeightParams);
 
+template <int DV, int NRC, bool Q4>
+WeightFn pick_weights_hpg(int hpg) {           // 0: the window kernel
+  switch (hpg) {
+    case 1: return weights_step_kernel<1, DV, NRC, Q4>;
+    case 2: return weights_step_kernel<2, DV, NRC, Q4>;
+    case 4: return weights_step_kernel<4, DV, NRC, Q4>;
+    case 8: return weights_step_kernel<8, DV, NRC, Q4>;
+  }
+  return weights_window_kernel<DV, NRC, Q4>;
+}
+
 template <bool Q4>
-WeightFn pick_weights(int dv, int nrc) {
+WeightFn pick_weights(int hpg, int dv, int nrc) {
   const bool wide = dv == 128;
   switch (nrc) {
-    case 0: return wide ? weights_bf16_kernel<128, 0, Q4> : weights_bf16_kernel<64, 0, Q4>;
-    case 1: return wide ? weights_bf16_kernel<128, 1, Q4> : weights_bf16_kernel<64, 1, Q4>;
-    case 2: return wide ? weights_bf16_kernel<128, 2, Q4> : weights_bf16_kernel<64, 2, Q4>;
+    case 0: return wide ? pick_weights_hpg<128, 0, Q4>(hpg) : pick_weights_hpg<64, 0, Q4>(hpg);
+    case 1: return wide ? pick_weights_hpg<128, 1, Q4>(hpg) : pick_weights_hpg<64, 1, Q4>(hpg);
+    case 2: return wide ? pick_weights_hpg<128, 2, Q4>(hpg) : pick_weights_hpg<64, 2, Q4>(hpg);
   }
   return nullptr;
 }
+
+// A decode step's query with a supported number of heads per group goes to the
+// step kernel (0 otherwise); fp32 has one kernel.
+int step_heads(const gva_dims* d, int n_new) {
+  const int hpg = d->n_heads / d->n_groups;
+  return n_new == 1 && (hpg == 1 || hpg == 2 || hpg == 4 || hpg == 8) ? hpg : 0;
+}
+bool weights_joined(const gva_dims* d, int n_new) { return d->dtype == GVA_DTYPE_BF16 && step_heads(d, n_new) == 0; }
 
 // =============================================================== evict
 struct EvictParams {
@@ -436,7 +611,7 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
 }
 
 struct WeightLayout {
-  size_t q_rot, bytes;
+  size_t q_rot, part, bytes;
 };
 
 int weight_layout(const gva_dims* d, int32_t n_new, WeightLayout& L) {
@@ -445,7 +620,8 @@ int weight_layout(const gva_dims* d, int32_t n_new, WeightLayout& L) {
   if (n_new < 1 || n_new > d->t_max) return GVA_ERR_INVALID_ARG;
   const size_t rows = (size_t)d->batch * n_new * d->n_heads;
   L.q_rot = round256(rows * d->d_v * 4);
-  L.bytes = L.q_rot + round256(rows * d->d_r * 4);
+  L.part = L.q_rot + round256(rows * d->d_r * 4);
+  L.bytes = L.part + (weights_joined(d, n_new) ? round256((size_t)d->n_groups * d->batch * d->t_max * 4) : 0);
   return GVA_OK;
 }
 
@@ -498,14 +674,16 @@ int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, c
   WeightFn fn = weights_f32_kernel;
   if (!f32) {
     if ((dims->d_v != 64 && dims->d_v != 128) || dims->d_r % 8 != 0 || dims->d_r > 64) return GVA_ERR_UNSUPPORTED;
-    const int nrc = (dims->d_r + 31) / 32;
-    fn = q4 ? pick_weights<true>(dims->d_v, nrc) : pick_weights<false>(dims->d_v, nrc);
+    const int nrc = (dims->d_r + 31) / 32, heads = step_heads(dims, n_new);
+    fn = q4 ? pick_weights<true>(heads, dims->d_v, nrc) : pick_weights<false>(heads, dims->d_v, nrc);
   }
-  if ((long long)n_new * (dims->n_heads / dims->n_groups) > 0x7FFFFFF0LL) return GVA_ERR_UNSUPPORTED;
+  const bool joined = weights_joined(dims, n_new);
+  if ((long long)n_new * (dims->n_heads / dims->n_groups) > 0x7FFFFF00LL || dims->batch > 65535) return GVA_ERR_UNSUPPORTED;
   // rows per workgroup: few enough for two workgroups per CU, whole tiles
   int chunk = kWeightChunk;
   while (chunk > 32 && (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk) < 2LL * device_cu_count()) chunk /= 2;
-  const long long items = (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk);
+  long long items = (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk);
+  if (joined) items = (long long)dims->batch * dims->n_groups * ((dims->t_max + kWindowRows - 1) / kWindowRows);
   if (items > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   float* q_abs = static_cast<float*>(workspace);
   float* q_rot = dims->d_r > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + L.q_rot) : nullptr;
@@ -513,10 +691,16 @@ int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, c
   if (seen != nullptr) at.t_max = 0x7FFFFFFF;
   st = gva_prefill_absorb(&at, n_new, q, m, seen != nullptr ? seen : lens, q_abs, q_rot, stream);
   if (st != GVA_OK) return st;
-  WeightParams p{v_cache, static_cast<const uint8_t*>(v4_scale), kr_cache, q_abs, q_rot, lse, lens, weights, new_weights,
+  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.part);
+  WeightParams p{v_cache, static_cast<const uint8_t*>(v4_scale), kr_cache, q_abs, q_rot, lse, lens, weights, new_weights, part,
                  dims->batch, dims->n_heads, dims->n_groups, n_new, dims->d_v, dims->d_r, dims->t_max, chunk,
                  scale_log2(dims), (float)decay};
-  hipLaunchKernelGGL(fn, dim3((unsigned)items), dim3(64 * kWeightWaves), 0, static_cast<hipStream_t>(stream), p);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(fn, dim3((unsigned)items), dim3(joined ? kThreads : 64 * kWeightWaves), 0, s, p);
+  st = launch_status();
+  if (st != GVA_OK || !joined) return st;
+  hipLaunchKernelGGL(weights_join_kernel, dim3((unsigned)((dims->t_max + kThreads - 1) / kThreads), (unsigned)dims->batch),
+                     dim3(kThreads), 0, s, p);
   return launch_status();
 }
 
