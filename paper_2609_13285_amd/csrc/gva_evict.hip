@@ -85,17 +85,32 @@ struct WeightStream {
     else
       return as_bf16x8(t.v[hf * NC + c]);
   }
-  // eight scaled entries of an absorbed query, in the columns of chunk c
-  __device__ __forceinline__ void query(const float* qa, int c, float scale, float* x) const {
-    const f32x4* src = reinterpret_cast<const f32x4*>(qa + (Q4 ? qd * (DV / 4) + 8 * c : 32 * c + 8 * qd));
+  // The absorbed query at qa and the rotated one at qr in the columns of the
+  // lane: requested (request), then scaled and split as chunk c (NC on: the
+  // positional ones).
+  struct Query {
+    f32x4 x[NC + NRC][2];
+  };
+  __device__ __forceinline__ void request(Query& q, const float* qa, const float* qr) const {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = src[j >> 2][j & 3] * scale;
+    for (int c = 0; c < NC; ++c) {
+      const f32x4* src = reinterpret_cast<const f32x4*>(qa + (Q4 ? qd * (DV / 4) + 8 * c : 32 * c + 8 * qd));
+      q.x[c][0] = src[0];
+      q.x[c][1] = src[1];
+    }
+#pragma unroll
+    for (int rc = 0; rc < NRC; ++rc) {
+      const f32x4* src = reinterpret_cast<const f32x4*>(qr + min(32 * rc + 8 * qd, d_r - 8));
+      q.x[NC + rc][0] = src[0];
+      q.x[NC + rc][1] = src[1];
+    }
   }
-  __device__ __forceinline__ void query_rot(const float* qr, int rc, float scale, float* x) const {
-    const bool in = 32 * rc + 8 * qd < d_r;
-    const f32x4* src = reinterpret_cast<const f32x4*>(qr + min(32 * rc + 8 * qd, d_r - 8));
+  __device__ __forceinline__ bf16x8 part(const Query& q, int c, float scale, bool lo) const {
+    const bool in = c < NC || 32 * (c - NC) + 8 * qd < d_r;
+    float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = in ? src[j >> 2][j & 3] * scale : 0.f;
+    for (int j = 0; j < 8; ++j) x[j] = in ? q.x[c][j >> 2][j & 3] * scale : 0.f;
+    return split_hi_lo(x, lo);
   }
 };
 
@@ -136,29 +151,25 @@ __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) wei
   float* const put = &sums[w % GP][(n == HPG ? 16 : 0) + 4 * qd];
   for (int g = w % GP; g < p.G; g += GP) {
     const Stream in(p, b, g, r1, lane);
+    // the query before the tiles: loads are waited for in the order of their issue
+    const int64_t qrow = (int64_t)b * p.H + g * HPG + head;
+    typename Stream::Query q;
+    in.request(q, p.q_abs + qrow * DV, p.q_rot + qrow * p.d_r);
+    const float ls = p.lse[qrow];
+    __builtin_amdgcn_sched_barrier(0);
     WeightRows<DV, NRC, Q4> buf[DEPTH];
 #pragma unroll
     for (int d = 0; d < DEPTH - 1; ++d) {
       in.template load<kAuxNT>(buf[d], tile_row(d));
       __builtin_amdgcn_sched_barrier(0);
     }
-    const int64_t qrow = (int64_t)b * p.H + g * HPG + head;
-    const float ls = p.lse[qrow];
     // -inf: a query with nothing to see, whose weights are 0
     const float init = is_lo ? 0.f : (ls != -INFINITY ? -ls * (float)kLog2e : -INFINITY);
     bf16x8 bq[NC], bk[NRC > 0 ? NRC : 1];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float x[8];
-      in.query(p.q_abs + qrow * DV, c, p.scale_log2, x);
-      bq[c] = active ? split_hi_lo(x, is_lo) : zero8;
-    }
+    for (int c = 0; c < NC; ++c) bq[c] = active ? in.part(q, c, p.scale_log2, is_lo) : zero8;
 #pragma unroll
-    for (int rc = 0; rc < NRC; ++rc) {
-      float x[8];
-      in.query_rot(p.q_rot + qrow * p.d_r, rc, p.scale_log2, x);
-      bk[rc] = active ? split_hi_lo(x, is_lo) : zero8;
-    }
+    for (int rc = 0; rc < NRC; ++rc) bk[rc] = active ? in.part(q, NC + rc, p.scale_log2, is_lo) : zero8;
     const bool first = g < GP;
     for (int jt = 0; jt < my_tiles; jt += DEPTH) {
 #pragma unroll
@@ -202,24 +213,24 @@ __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) wei
 }
 
 // Many queries, or any number of heads per group.  The workgroup takes one group
-// and kWindowRows rows of one sequence; a column of the products is one (query,
+// and `chunk` rows of one sequence; a column of the products is one (query,
 // head) pair, its query once as bf16 high parts and once as low parts into the
 // same sums, 32 columns a wave.  The waves are dealt first over the columns and
 // then over the tiles.  Sums over the columns go through LDS in a fixed order to
 // the group's row sums in the workspace, which weights_join_kernel adds up.
-constexpr int kWindowRows = 128, kWindowCols = 32;
+constexpr int kWindowRows = 512, kWindowCols = 32;   // most rows of a workgroup; columns of a wave
 
 template <int DV, int NRC, bool Q4>
 __global__ void __launch_bounds__(kThreads, 2) weights_window_kernel(WeightParams p) {
   using Stream = WeightStream<DV, NRC, Q4>;
   constexpr int NC = Stream::NC, NK = NC + NRC;
   __shared__ __attribute__((aligned(16))) float sums[kWaves][kWindowRows];
-  const int nchunks = (p.t_max + kWindowRows - 1) / kWindowRows;
+  const int nchunks = (p.t_max + p.chunk - 1) / p.chunk;
   const int item = xcd_remap(blockIdx.x, p.B * nchunks * p.G);
-  const int g = item % p.G, b = item / p.G / nchunks, r0 = item / p.G % nchunks * kWindowRows;
+  const int g = item % p.G, b = item / p.G / nchunks, r0 = item / p.G % nchunks * p.chunk;
   const int L = clamp_len(p.lens, b, p.t_max);
   if (r0 >= L) return;
-  const int r1 = min(r0 + kWindowRows, L);
+  const int r1 = min(r0 + p.chunk, L);
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, qd = lane >> 4;
@@ -230,8 +241,8 @@ __global__ void __launch_bounds__(kThreads, 2) weights_window_kernel(WeightParam
   const Stream in(p, b, g, r1, lane);
   float* const mine = sums[w % WC];
   for (int set = w % WC; set < nsets; set += WC) {
-    bf16x8 hi[2][NK], lo[2][NK];
-    float init[2];
+    typename Stream::Query q[2];
+    float ls[2];
     int last[2];                               // the last row that the column's query sees
 #pragma unroll
     for (int cb = 0; cb < 2; ++cb) {
@@ -239,24 +250,34 @@ __global__ void __launch_bounds__(kThreads, 2) weights_window_kernel(WeightParam
       const bool active = col < cols;
       const int qi = active ? col / hpg : 0;
       const int64_t qrow = ((int64_t)b * p.N + qi) * p.H + g * hpg + (active ? col % hpg : 0);
-      const float ls = p.lse[qrow];
-      init[cb] = active && ls != -INFINITY ? -ls * (float)kLog2e : -INFINITY;
+      in.request(q[cb], p.q_abs + qrow * DV, p.q_rot + qrow * p.d_r);
+      ls[cb] = active ? p.lse[qrow] : -INFINITY;
       last[cb] = active ? L - p.N + qi : -1;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    WeightRows<DV, NRC, Q4> buf[2];
+    in.template load<0>(buf[0], r0 + w / WC * kTileRows);
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 hi[2][NK], lo[2][NK];
+    float init[2];
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb) {
+      init[cb] = ls[cb] != -INFINITY ? -ls[cb] * (float)kLog2e : -INFINITY;
 #pragma unroll
       for (int c = 0; c < NK; ++c) {
-        float x[8];
-        if (c < NC)
-          in.query(p.q_abs + qrow * DV, c, p.scale_log2, x);
-        else
-          in.query_rot(p.q_rot + qrow * p.d_r, c - NC, p.scale_log2, x);
-        hi[cb][c] = split_hi_lo(x, false);
-        lo[cb][c] = split_hi_lo(x, true);
+        hi[cb][c] = in.part(q[cb], c, p.scale_log2, false);
+        lo[cb][c] = in.part(q[cb], c, p.scale_log2, true);
       }
     }
-    for (int j = w / WC; j < ntiles; j += WT) {
+    for (int j0 = w / WC; j0 < ntiles; j0 += 2 * WT)
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const int j = j0 + d * WT;
+      if (j >= ntiles) break;
       const int row0 = r0 + j * kTileRows;
-      WeightRows<DV, NRC, Q4> t;
-      in.template load<0>(t, row0);
+      const WeightRows<DV, NRC, Q4>& t = buf[d];
+      in.template load<0>(buf[1 - d], row0 + WT * kTileRows);   // (past the last tile: zeros, no traffic)
+      __builtin_amdgcn_sched_barrier(0);
       f32x4 sc[2][2];
 #pragma unroll
       for (int cb = 0; cb < 2; ++cb)
@@ -680,10 +701,11 @@ int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, c
   const bool joined = weights_joined(dims, n_new);
   if ((long long)n_new * (dims->n_heads / dims->n_groups) > 0x7FFFFF00LL || dims->batch > 65535) return GVA_ERR_UNSUPPORTED;
   // rows per workgroup: few enough for two workgroups per CU, whole tiles
-  int chunk = kWeightChunk;
-  while (chunk > 32 && (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk) < 2LL * device_cu_count()) chunk /= 2;
-  long long items = (long long)dims->batch * ((dims->t_max + chunk - 1) / chunk);
-  if (joined) items = (long long)dims->batch * dims->n_groups * ((dims->t_max + kWindowRows - 1) / kWindowRows);
+  const long long streams = (long long)dims->batch * (joined ? dims->n_groups : 1);
+  int chunk = joined ? kWindowRows : kWeightChunk;
+  auto count = [&]() { return streams * ((dims->t_max + chunk - 1) / chunk); };
+  while (chunk > 32 && count() < 2LL * device_cu_count()) chunk /= 2;
+  const long long items = count();
   if (items > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   float* q_abs = static_cast<float*>(workspace);
   float* q_rot = dims->d_r > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + L.q_rot) : nullptr;
