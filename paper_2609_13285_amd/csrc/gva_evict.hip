@@ -452,25 +452,30 @@ struct EvictParams {
 };
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+constexpr int kEvictBins = 8192, kEvictBatch = 8;   // counters; rows of a lane requested at once
 
 // The order of rows: larger keys stay.  Protected rows before all, NaN
 // after all, -0 like +0.
-__device__ __forceinline__ unsigned evict_key(const EvictParams& p, int b, int t, int seen) {
-  const int64_t at = (int64_t)b * p.t_max + t;
-  const int pos = p.row_pos != nullptr ? p.row_pos[at] : t;
-  if (pos < p.first || (int64_t)pos >= (int64_t)seen - p.recent) return 0xFFFFFFFFu;
-  const float x = p.weights[at] + 0.f;
+__device__ __forceinline__ unsigned evict_key(const EvictParams& p, int pos, float weight, int seen) {
+  const float x = weight + 0.f;
   const unsigned u = __float_as_uint(x);
-  if (x != x) return 0u;
-  return u >> 31 ? ~u : u | 0x80000000u;
+  const unsigned order = x != x ? 0u : (u >> 31 ? ~u : u | 0x80000000u);
+  return pos < p.first || (int64_t)pos >= (int64_t)seen - p.recent ? 0xFFFFFFFFu : order;
 }
 
-// One workgroup per sequence.  Radix selection of the keep-th largest key, then
-// each wave goes over a contiguous segment of the rows.
+// One workgroup per sequence; wave w owns rows [w seg, (w + 1) seg).  The
+// border, the keep-th largest key, is found digit by digit (13, 10 and 9 bits:
+// the first takes in the exponent and four bits more, so that keys of like weight
+// spread over a hundred counters), then the rows to leave and those to move into
+// their places are numbered in order.  KPT > 0: every lane keeps the keys of its
+// KPT rows in registers, and the weights are read from memory once.  KPT = 0
+// (longer sequences): keys are computed again in every pass.
+// Bound by the latency of its passes: see kEvictKeys for the times.
+template <int KPT>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
-  __shared__ int hist[256];
+  __shared__ __attribute__((aligned(16))) int hist[kEvictBins];
+  __shared__ int wave_n[3][kEvictWaves];
   __shared__ int pick_bin, pick_rest;
-  __shared__ int wave_n[2][kEvictWaves];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int L = clamp_len(p.lens, b, p.t_max);
@@ -491,41 +496,93 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     if (tid == 0) p.count[b] = 0;
     return;
   }
+  const int seg = KPT > 0 ? 64 * KPT : ((L + kEvictWaves - 1) / kEvictWaves + 63) / 64 * 64;
+  const int s0 = min(w * seg, L), s1 = min(s0 + seg, L);
+  const int steps = KPT > 0 ? KPT : (s1 - s0 + 63) / 64;
+  // A lane's rows are s0 + lane, s0 + lane + 64, ..., taken kEvictBatch at a time
+  // (rows past the segment read its last one and are never counted).
+  const int32_t* const rp = p.row_pos;
+  auto fetch = [&](int i0, float (&wt)[kEvictBatch], int (&pos)[kEvictBatch]) {
+#pragma unroll
+    for (int k = 0; k < kEvictBatch; ++k) {
+      const int t = max(min(s0 + 64 * (i0 + k) + lane, s1 - 1), 0);
+      wt[k] = p.weights[base + t];
+      pos[k] = rp != nullptr ? rp[base + t] : t;
+    }
+  };
+  constexpr int NB = KPT > 0 ? (KPT + kEvictBatch - 1) / kEvictBatch : 1;
+  const int nb = KPT > 0 ? NB : (steps + kEvictBatch - 1) / kEvictBatch;
+  unsigned keys[KPT > 0 ? NB * kEvictBatch : 1];
+  if constexpr (KPT > 0) {
+#pragma unroll
+    for (int i0 = 0; i0 < NB * kEvictBatch; i0 += kEvictBatch) {
+      float wt[kEvictBatch];
+      int pos[kEvictBatch];
+      fetch(i0, wt, pos);
+#pragma unroll
+      for (int k = 0; k < kEvictBatch; ++k) keys[i0 + k] = evict_key(p, pos[k], wt[k], seen);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  auto each = [&](auto&& body) {               // body(step, key)
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) {
+        body(i, keys[i]);
+        if (i % kEvictBatch == kEvictBatch - 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      for (int i0 = 0; i0 < steps; i0 += kEvictBatch) {
+        float wt[kEvictBatch];
+        int pos[kEvictBatch];
+        fetch(i0, wt, pos);
+#pragma unroll
+        for (int k = 0; k < kEvictBatch; ++k) body(i0 + k, evict_key(p, pos[k], wt[k], seen));
+      }
+    }
+  };
+
   unsigned prefix = 0u, mask = 0u;
   int rest = K;                                // of the rows that match the prefix, the rest-th largest is the border
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+#pragma unroll
+  for (int digit = 0; digit < 3; ++digit) {
+    const int bits = digit == 0 ? 13 : (digit == 1 ? 10 : 9), shift = digit == 0 ? 19 : (digit == 1 ? 9 : 0);
+    constexpr int kWide = kEvictBins / kEvictThreads;
+    const int per = digit == 0 ? kWide : 1;    // counters a thread holds
+#pragma unroll
+    for (int k = 0; k < per; ++k) hist[tid + k * kEvictThreads] = 0;
     __syncthreads();
-    for (int t = tid; t < L; t += kEvictThreads) {
-      const unsigned key = evict_key(p, b, t, seen);
-      if ((key & mask) == prefix) atomicAdd(&hist[key >> shift & 255u], 1);
+    each([&](int i, unsigned x) {
+      if (s0 + 64 * i + lane < s1 && (x & mask) == prefix) atomicAdd(&hist[x >> shift & ((1u << bits) - 1u)], 1);
+    });
+    __syncthreads();
+    // the scan runs from the top: thread t holds the t-th `per` counters from there
+    const int first = (per * kEvictThreads - 1) - per * tid;
+    int c[kWide], sum = 0;
+#pragma unroll
+    for (int k = 0; k < per; ++k) {
+      c[k] = hist[first - k];
+      sum += c[k];
     }
+    const int incl = wave_incl_scan(sum);
+    if (lane == 63) wave_n[0][w] = incl;
     __syncthreads();
-    if (w == 0) {                              // lane l: bins 255 - 4 l down to 252 - 4 l
-      int c[4], sum = 0;
+    int above = incl - sum;
+    for (int i = 0; i < w; ++i) above += wave_n[0][i];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        c[k] = hist[255 - 4 * lane - k];
-        sum += c[k];
+    for (int k = 0; k < per; ++k) {
+      if (above < rest && rest <= above + c[k]) {
+        pick_bin = first - k;
+        pick_rest = rest - above;
       }
-      int above = wave_incl_scan(sum) - sum;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (above < rest && rest <= above + c[k]) {
-          pick_bin = 255 - 4 * lane - k;
-          pick_rest = rest - above;
-        }
-        above += c[k];
-      }
+      above += c[k];
     }
     __syncthreads();
     prefix |= (unsigned)pick_bin << shift;
-    mask |= 255u << shift;
+    mask |= ((1u << bits) - 1u) << shift;
     rest = pick_rest;
   }
   // rows above the border stay, and the first `rest` of those on it
-  const int seg = ((L + kEvictWaves - 1) / kEvictWaves + 63) / 64 * 64;
-  const int s0 = min(w * seg, L), s1 = min(s0 + seg, L);
   auto scan_waves = [&](int slot, int n) {     // the sum over the waves before this one
     if (lane == 0) wave_n[slot][w] = n;
     __syncthreads();
@@ -535,45 +592,51 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
   };
   const unsigned long long below = (1ull << lane) - 1ull;
   int n_eq = 0;
-  for (int t0 = s0; t0 < s1; t0 += 64) {
-    const int t = t0 + lane;
-    n_eq += __popcll(__ballot(t < s1 && evict_key(p, b, t, seen) == prefix));
-  }
-  const int eq0 = scan_waves(0, n_eq);
-  auto kept_mask = [&](int t0, int& eq) {      // which rows t0 .. t0 + 63 stay
-    const int t = t0 + lane;
-    const unsigned key = t < s1 ? evict_key(p, b, t, seen) : 0u;
-    const bool on = t < s1 && key == prefix;
-    const unsigned long long m = __ballot(on);
-    const bool stay = t < s1 && (key > prefix || (on && eq + __popcll(m & below) < rest));
+  each([&](int i, unsigned x) { n_eq += __popcll(__ballot(s0 + 64 * i + lane < s1 && x == prefix)); });
+  const int eq0 = scan_waves(1, n_eq);
+  auto stays = [&](int i, unsigned x, int& eq) {   // which rows of step i stay
+    const bool in = s0 + 64 * i + lane < s1;
+    const unsigned long long m = __ballot(in && x == prefix);
+    const bool me = in && (x > prefix || (x == prefix && eq + __popcll(m & below) < rest));
     eq += __popcll(m);
-    return __ballot(stay);
+    return __ballot(me);
   };
   int n_hole = 0, n_move = 0, eq = eq0;
-  for (int t0 = s0; t0 < s1; t0 += 64) {
-    const unsigned long long stay = kept_mask(t0, eq);
-    const bool in = t0 + lane < s1, low = t0 + lane < K;
-    n_hole += __popcll(__ballot(in && low) & ~stay);
-    n_move += __popcll(stay & __ballot(in && !low));
-  }
-  __syncthreads();
-  int hole0 = scan_waves(0, n_hole);
-  int move0 = scan_waves(1, n_move);
+  each([&](int i, unsigned x) {
+    const unsigned long long stay = stays(i, x, eq);
+    const int t = s0 + 64 * i + lane;
+    n_hole += __popcll(__ballot(t < s1 && t < K) & ~stay);
+    n_move += __popcll(stay & __ballot(t >= K));
+  });
+  int hole0 = scan_waves(2, n_hole);
+  int move0 = scan_waves(0, n_move);           // (slot 0 was last read two barriers ago)
   if (tid == kEvictThreads - 1) p.count[b] = move0 + n_move;
   eq = eq0;
-  for (int t0 = s0; t0 < s1; t0 += 64) {
-    const unsigned long long stay = kept_mask(t0, eq);
-    const int t = t0 + lane;
-    const bool in = t < s1, low = t < K, me = stay >> lane & 1ull;
-    const unsigned long long hm = __ballot(in && low && !me), mm = __ballot(me && !low);
+  auto emit = [&](int i, unsigned x, float wt, int pos) {
+    const unsigned long long stay = stays(i, x, eq);
+    const int t = s0 + 64 * i + lane;
+    const bool me = stay >> lane & 1ull;
+    const unsigned long long hm = __ballot(t < s1 && t < K) & ~stay, mm = stay & __ballot(t >= K);
     if (hm >> lane & 1ull) p.hole[(int64_t)b * p.room + hole0 + __popcll(hm & below)] = t;
     if (mm >> lane & 1ull) p.move[(int64_t)b * p.room + move0 + __popcll(mm & below)] = t;
-    if (me && low) {
-      p.new_weights[base + t] = p.weights[base + t];
-      if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = p.row_pos[base + t];
+    if (me && t < K) {
+      p.new_weights[base + t] = wt;
+      if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = pos;
     }
     hole0 += __popcll(hm);
     move0 += __popcll(mm);
+  };
+#pragma unroll
+  for (int q = 0; q < (KPT > 0 ? NB : 1); ++q) {
+    for (int i0 = q * kEvictBatch; i0 < (KPT > 0 ? (q + 1) * kEvictBatch : nb * kEvictBatch); i0 += kEvictBatch) {
+      float wt[kEvictBatch];
+      int pos[kEvictBatch];
+      fetch(i0, wt, pos);
+#pragma unroll
+      for (int k = 0; k < kEvictBatch; ++k)
+        emit(i0 + k, KPT > 0 ? keys[KPT > 0 ? q * kEvictBatch + k : 0] : evict_key(p, pos[k], wt[k], seen), wt[k], pos[k]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
@@ -593,12 +656,14 @@ struct MoveParams {
 };
 
 // Rows move from at or past the budget to below it, so no row is both read and
-// written and the moves need no order.  A wave takes 16 moves of one stream,
-// lane (n, qd) pieces qd, qd + 4, ... of move n: moves next to each other come
-// from, and go to, nearby rows of a tile, whose pieces lie side by side.
+// written and the moves need no order.  A wave takes 16 moves of one stream and
+// 16 of its 16-byte pieces, lane (n, qd) pieces qd, qd + 4, ... of move n, all
+// requested before the first is stored: moves next to each other come from, and
+// go to, nearby rows of a tile, whose pieces lie side by side.
 template <bool Q4>
 __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
-  const int b = blockIdx.z, g = blockIdx.y;
+  const int b = blockIdx.z, nseg = Q4 ? 1 : (p.v_pieces + 15) / 16;
+  const int g = blockIdx.y / nseg, c0 = blockIdx.y % nseg * 16;
   const int lane = threadIdx.x & 63, n = lane & 15, qd = lane >> 4;
   const int i = ((int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6)) * 16 + n;
   if (i >= p.count[b]) return;
@@ -606,9 +671,15 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
   auto tiled = [&](uint8_t* stream, int pieces) {
     const u32x4* src = reinterpret_cast<const u32x4*>(stream) + (int64_t)(from / 16) * 16 * pieces + from % 16;
     u32x4* dst = reinterpret_cast<u32x4*>(stream) + (int64_t)(to / 16) * 16 * pieces + to % 16;
-    for (int c = qd; c < pieces; c += 4) dst[c * 16] = src[c * 16];
+    u32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c0 + qd + 4 * k < pieces) x[k] = src[(c0 + qd + 4 * k) * 16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c0 + qd + 4 * k < pieces) dst[(c0 + qd + 4 * k) * 16] = x[k];
   };
-  if (g == p.G) {                              // what the groups share
+  if (g == p.G) {                              // what the groups share (a positional key has at most 16 pieces)
     if (p.kr_pieces > 0) tiled(p.kr + (int64_t)b * p.t_max * p.kr_pieces * 16, p.kr_pieces);
     if (qd == 0) {
       const int64_t base = (int64_t)b * p.t_max;
@@ -629,6 +700,18 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
   } else {
     tiled(p.v + stream * p.t_max * p.v_pieces * 16, p.v_pieces);
   }
+}
+
+using SelectFn = void (*)(EvictParams);
+
+// The keys a lane holds, by the capacity.
+SelectFn pick_select(int t_max) {
+  if (t_max <= 4 * kEvictThreads) return evict_select_kernel<4>;
+  if (t_max <= 8 * kEvictThreads) return evict_select_kernel<8>;
+  if (t_max <= 16 * kEvictThreads) return evict_select_kernel<16>;
+  if (t_max <= 32 * kEvictThreads) return evict_select_kernel<32>;
+  if (t_max <= 64 * kEvictThreads) return evict_select_kernel<64>;
+  return evict_select_kernel<0>;
 }
 
 struct WeightLayout {
@@ -756,7 +839,8 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
   const bool q4 = v4_scale != nullptr;
   st = q4 ? check_q4_dims(dims) : check_cache_layout(dims);
   if (st != GVA_OK) return st;
-  if (dims->batch > 65535 || dims->n_groups >= 65535) return GVA_ERR_UNSUPPORTED;
+  const long long blocks = q4 ? 1 : ((long long)dims->d_v * (long long)elem_size(dims) / 16 + 15) / 16;
+  if (dims->batch > 65535 || blocks * dims->n_groups >= 65535) return GVA_ERR_UNSUPPORTED;
   char* ws = static_cast<char*>(workspace);
   int32_t* count = reinterpret_cast<int32_t*>(ws);
   int32_t* hole = reinterpret_cast<int32_t*>(ws + L.hole);
@@ -764,15 +848,16 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
   const EvictParams p{lens, seen, weights, row_pos, new_lens, new_weights, new_row_pos, count, hole, move,
                       dims->batch, dims->t_max, n_keep, n_first, n_recent, L.room};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(dims->batch), dim3(kEvictThreads), 0, s, p);
+  hipLaunchKernelGGL(pick_select(dims->t_max), dim3(dims->batch), dim3(kEvictThreads), 0, s, p);
   st = launch_status();
   const int most = n_keep < dims->t_max - n_keep ? n_keep : dims->t_max - n_keep;   // rows of a sequence that can move
   if (st != GVA_OK || most <= 0) return st;
   const int piece = (int)(16 / elem_size(dims));
+  const int nseg = q4 ? 1 : (dims->d_v / piece + 15) / 16;
   const MoveParams mp{weights, row_pos, new_weights, new_row_pos, count, hole, move,
                       static_cast<uint8_t*>(v_cache), static_cast<uint8_t*>(v4_scale), static_cast<uint8_t*>(kr_cache),
                       dims->batch, dims->n_groups, dims->t_max, dims->d_v, L.room, dims->d_v / piece, dims->d_r / piece};
-  const dim3 grid((unsigned)((most + 16 * kWaves - 1) / (16 * kWaves)), (unsigned)(dims->n_groups + 1), (unsigned)dims->batch);
+  const dim3 grid((unsigned)((most + 16 * kWaves - 1) / (16 * kWaves)), (unsigned)(dims->n_groups * nseg + 1), (unsigned)dims->batch);
   hipLaunchKernelGGL((q4 ? evict_move_kernel<true> : evict_move_kernel<false>), grid, dim3(kThreads), 0, s, mp);
   return launch_status();
 }
