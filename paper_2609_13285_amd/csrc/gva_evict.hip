@@ -437,6 +437,11 @@ int step_heads(const gva_dims* d, int n_new) {
 bool weights_joined(const gva_dims* d, int n_new) { return d->dtype == GVA_DTYPE_BF16 && step_heads(d, n_new) == 0; }
 
 // =============================================================== evict
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+constexpr int kEvictRows = 4;                  // rows of a thread
+constexpr int kEvictBlock = kEvictThreads * kEvictRows;
+constexpr int kDigit0 = 12, kDigit12 = 10;     // bits of the key's digits, from the top
+
 struct EvictParams {
   const int32_t* lens;
   const int32_t* seen;
@@ -448,11 +453,13 @@ struct EvictParams {
   int32_t* count;         // [B]: rows that move
   int32_t* hole;          // [B][room]: the rows they go to, ascending
   int32_t* move;          // [B][room]: and come from, ascending
-  int32_t B, t_max, keep, first, recent, room;
+  int32_t* state;         // [B][4]: the border's first digit and the rank left in it; the second and its
+  int32_t* above;         // [2][B][blocks]: keys above the border's first digit; above its second in the first
+  uint16_t* hist0;        // [B][blocks][2^12]: keys by first digit
+  uint16_t* hist1;        // [B][blocks][2^10]: by second digit, of those with the border's first
+  uint16_t* hist2;        // [B][blocks][2^10]: by third digit, of those with the border's first two
+  int32_t B, t_max, keep, first, recent, room, blocks, low;   // low: blocks of the rows below the budget
 };
-
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
-constexpr int kEvictBins = 8192, kEvictBatch = 8;   // counters; rows of a lane requested at once
 
 // The order of rows: larger keys stay.  Protected rows before all, NaN
 // after all, -0 like +0.
@@ -463,180 +470,332 @@ __device__ __forceinline__ unsigned evict_key(const EvictParams& p, int pos, flo
   return pos < p.first || (int64_t)pos >= (int64_t)seen - p.recent ? 0xFFFFFFFFu : order;
 }
 
-// One workgroup per sequence; wave w owns rows [w seg, (w + 1) seg).  The
-// border, the keep-th largest key, is found digit by digit (13, 10 and 9 bits:
-// the first takes in the exponent and four bits more, so that keys of like weight
-// spread over a hundred counters), then the rows to leave and those to move into
-// their places are numbered in order.  KPT > 0: every lane keeps the keys of its
-// KPT rows in registers, and the weights are read from memory once.  KPT = 0
-// (longer sequences): keys are computed again in every pass.
-// Bound by the latency of its passes: see kEvictKeys for the times.
-template <int KPT>
-__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
-  __shared__ __attribute__((aligned(16))) int hist[kEvictBins];
-  __shared__ int wave_n[3][kEvictWaves];
-  __shared__ int pick_bin, pick_rest;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int L = clamp_len(p.lens, b, p.t_max);
+// The selection runs in four launches over blocks of 4096 rows, one workgroup
+// each; the rows below the budget and those from it on have blocks of their own,
+// so that places to fill and rows to move are numbered per block.  Three launches
+// find the border, the keep-th largest key, digit by digit (12, 10 and 10 bits:
+// the first takes in the exponent and three bits more, so that keys of like weight
+// spread over many counters): every block counts its own keys, and the next launch
+// adds up the blocks' counters, each workgroup for itself.  The fourth numbers the
+// rows.  No counter is shared, so nothing has to be cleared.
+template <int N>
+struct EvictRows {
+  int t[N];
+  bool in[N];             // a cached row of the block
+  float weight[N];
+  int pos[N];
+  unsigned key[N];
+};
+
+// Rows t0 .. t1 - 1, N a thread; a wave's are contiguous.
+template <int N>
+__device__ __forceinline__ void evict_rows(const EvictParams& p, int b, int t0, int t1, int L, EvictRows<N>& r) {
   const int seen = p.seen != nullptr ? p.seen[b] : L;
   const int64_t base = (int64_t)b * p.t_max;
-  const int K = p.keep;
-  const int n_new = min(L, K);
-  if (tid == 0) p.new_lens[b] = n_new;
-  for (int t = n_new + tid; t < p.t_max; t += kEvictThreads) {
-    p.new_weights[base + t] = 0.f;
-    if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = -1;
+  const int first = t0 + (int)(threadIdx.x >> 6) * 64 * N + (int)(threadIdx.x & 63);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    r.t[i] = first + 64 * i;
+    r.in[i] = r.t[i] < t1;
+    const int t = r.in[i] ? r.t[i] : 0;
+    r.weight[i] = p.weights[base + t];
+    r.pos[i] = p.row_pos != nullptr ? p.row_pos[base + t] : t;
   }
-  if (L <= K) {
-    for (int t = tid; t < L; t += kEvictThreads) {
-      p.new_weights[base + t] = p.weights[base + t];
-      if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = p.row_pos[base + t];
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.key[i] = evict_key(p, r.pos[i], r.weight[i], seen);
+}
+
+__device__ __forceinline__ void evict_block_rows(const EvictParams& p, int b, int blk, int L, EvictRows<kEvictRows>& r) {
+  const int t0 = blk < p.low ? blk * kEvictBlock : p.keep + (blk - p.low) * kEvictBlock;
+  evict_rows(p, b, t0, min(blk < p.low ? min(t0 + kEvictBlock, p.keep) : t0 + kEvictBlock, L), L, r);
+}
+
+// Sums over the workgroup, each thread receiving those of the threads before it.
+__device__ __forceinline__ int block_before(int v, int* wave_n) {
+  const int incl = wave_incl_scan(v);
+  __syncthreads();                             // wave_n may still be read
+  if ((threadIdx.x & 63) == 63) wave_n[threadIdx.x >> 6] = incl;
+  __syncthreads();
+  int before = incl - v;
+  for (int i = 0; i < (int)(threadIdx.x >> 6); ++i) before += wave_n[i];
+  return before;
+}
+__device__ __forceinline__ int block_sum(int v, int* wave_n) {
+  const int s = wave_sum_int(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = s;
+  __syncthreads();
+  int sum = 0;
+  for (int i = 0; i < kEvictWaves; ++i) sum += wave_n[i];
+  return sum;
+}
+
+// The counter that holds the rest-th key from the top, and the rank left in it:
+// thread t holds the t-th N counters from there (its first one `top`).
+template <int N>
+__device__ __forceinline__ void pick_digit(const int (&c)[N], int top, int& rest, int& bin, int* wave_n, int* picked) {
+  int sum = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum += c[k];
+  int above = block_before(sum, wave_n);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if (above < rest && rest <= above + c[k]) {
+      picked[0] = top - k;
+      picked[1] = rest - above;
     }
-    if (tid == 0) p.count[b] = 0;
+    above += c[k];
+  }
+  __syncthreads();
+  bin = picked[0];
+  rest = picked[1];
+}
+
+// Digit STAGE of the keys that match the border's digits before it.
+template <int STAGE>
+__global__ void __launch_bounds__(kEvictThreads) evict_count_kernel(EvictParams p) {
+  constexpr int BITS = STAGE == 0 ? kDigit0 : kDigit12, SHIFT = STAGE == 0 ? 20 : (STAGE == 1 ? 10 : 0);
+  constexpr int PER = (1 << BITS) / kEvictThreads;
+  __shared__ __attribute__((aligned(16))) int hist[1 << BITS];
+  __shared__ int wave_n[kEvictWaves], picked[2];
+  const int b = blockIdx.y, blk = blockIdx.x, tid = threadIdx.x;
+  const int L = clamp_len(p.lens, b, p.t_max);
+  if (L <= p.keep) return;
+  const int64_t at = (int64_t)b * p.blocks + blk;
+  EvictRows<kEvictRows> r;
+  evict_block_rows(p, b, blk, L, r);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) hist[tid + k * kEvictThreads] = 0;
+  unsigned prefix = 0u;
+  if constexpr (STAGE == 1) {
+    const int top = (1 << kDigit0) - 1 - 4 * tid;
+    int c[4] = {0, 0, 0, 0}, rest = p.keep, bin;
+    const uint16_t* h = p.hist0 + ((int64_t)b * p.blocks << kDigit0) + top - 3;
+#pragma unroll 8
+    for (int i = 0; i < p.blocks; ++i) {
+      const uint64_t x = *reinterpret_cast<const uint64_t*>(h + ((int64_t)i << kDigit0));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] += (int)(x >> (16 * (3 - k)) & 0xFFFFu);
+    }
+    pick_digit(c, top, rest, bin, wave_n, picked);
+    if (blk == 0 && tid == 0) {
+      p.state[4 * b] = bin;
+      p.state[4 * b + 1] = rest;
+    }
+    prefix = (unsigned)bin;
+  }
+  if constexpr (STAGE == 2) {
+    int rest = p.state[4 * b + 1], bin, c[1] = {0};
+    const int top = kEvictThreads - 1 - tid;
+    const uint16_t* h = p.hist1 + ((int64_t)b * p.blocks << kDigit12) + top;
+#pragma unroll 8
+    for (int i = 0; i < p.blocks; ++i) c[0] += h[(int64_t)i << kDigit12];
+    pick_digit(c, top, rest, bin, wave_n, picked);
+    if (blk == 0 && tid == 0) {
+      p.state[4 * b + 2] = bin;
+      p.state[4 * b + 3] = rest;
+    }
+    prefix = (unsigned)p.state[4 * b] << kDigit12 | (unsigned)bin;
+  }
+  __syncthreads();                             // the counters are clear
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < kEvictRows; ++i) {
+    if (!r.in[i]) continue;
+    const unsigned x = r.key[i] >> SHIFT;
+    if (STAGE == 0 || x >> BITS == prefix) atomicAdd(&hist[x & ((1u << BITS) - 1u)], 1);
+    // above the border's last digit known so far, alike in those before it
+    if (STAGE == 1) above += x >> BITS > prefix ? 1 : 0;
+    if (STAGE == 2) above += x >> BITS > prefix && x >> (BITS + kDigit12) == prefix >> kDigit12 ? 1 : 0;
+  }
+  if constexpr (STAGE > 0) {
+    above = block_sum(above, wave_n);
+    if (tid == 0) p.above[(int64_t)(STAGE - 1) * p.B * p.blocks + at] = above;
+  }
+  __syncthreads();
+  if constexpr (STAGE == 0) {
+    uint64_t x = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x |= (uint64_t)hist[4 * tid + k] << (16 * k);
+    *reinterpret_cast<uint64_t*>(p.hist0 + (at << kDigit0) + 4 * tid) = x;
+  } else {
+    (STAGE == 1 ? p.hist1 : p.hist2)[(at << kDigit12) + tid] = (uint16_t)hist[tid];
+  }
+}
+
+__global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams p) {
+  __shared__ int wave_n[kEvictWaves], picked[2], eq_n[2];
+  const int b = blockIdx.y, blk = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int L = clamp_len(p.lens, b, p.t_max), K = p.keep;
+  const int64_t base = (int64_t)b * p.t_max;
+  EvictRows<kEvictRows> r;
+  evict_block_rows(p, b, blk, L, r);
+  if (blk == 0 && tid == 0) p.new_lens[b] = min(L, K);
+  auto store = [&](int i, float weight, int pos) {
+    if (r.t[i] >= (blk < p.low ? min(K, p.t_max) : p.t_max)) return;
+    p.new_weights[base + r.t[i]] = weight;
+    if (p.new_row_pos != nullptr) p.new_row_pos[base + r.t[i]] = pos;
+  };
+  if (L <= K) {                                // every row stays
+    if (blk == 0 && tid == 0) p.count[b] = 0;
+#pragma unroll
+    for (int i = 0; i < kEvictRows; ++i) store(i, r.in[i] ? r.weight[i] : 0.f, r.in[i] ? r.pos[i] : -1);
     return;
   }
-  const int seg = KPT > 0 ? 64 * KPT : ((L + kEvictWaves - 1) / kEvictWaves + 63) / 64 * 64;
-  const int s0 = min(w * seg, L), s1 = min(s0 + seg, L);
-  const int steps = KPT > 0 ? KPT : (s1 - s0 + 63) / 64;
-  // A lane's rows are s0 + lane, s0 + lane + 64, ..., taken kEvictBatch at a time
-  // (rows past the segment read its last one and are never counted).
-  const int32_t* const rp = p.row_pos;
-  auto fetch = [&](int i0, float (&wt)[kEvictBatch], int (&pos)[kEvictBatch]) {
-#pragma unroll
-    for (int k = 0; k < kEvictBatch; ++k) {
-      const int t = max(min(s0 + 64 * (i0 + k) + lane, s1 - 1), 0);
-      wt[k] = p.weights[base + t];
-      pos[k] = rp != nullptr ? rp[base + t] : t;
-    }
-  };
-  constexpr int NB = KPT > 0 ? (KPT + kEvictBatch - 1) / kEvictBatch : 1;
-  const int nb = KPT > 0 ? NB : (steps + kEvictBatch - 1) / kEvictBatch;
-  unsigned keys[KPT > 0 ? NB * kEvictBatch : 1];
-  if constexpr (KPT > 0) {
-#pragma unroll
-    for (int i0 = 0; i0 < NB * kEvictBatch; i0 += kEvictBatch) {
-      float wt[kEvictBatch];
-      int pos[kEvictBatch];
-      fetch(i0, wt, pos);
-#pragma unroll
-      for (int k = 0; k < kEvictBatch; ++k) keys[i0 + k] = evict_key(p, pos[k], wt[k], seen);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  // the third digit; its counters in the blocks before this one, and in those
+  // below the budget
+  int rest = p.state[4 * b + 3], bin, c[1] = {0}, before = 0, low = 0;
+  const int top = kEvictThreads - 1 - tid;
+  const uint16_t* h = p.hist2 + ((int64_t)b * p.blocks << kDigit12) + top;
+#pragma unroll 8
+  for (int i = 0; i < p.blocks; ++i) {
+    const int x = h[(int64_t)i << kDigit12];
+    c[0] += x;
+    before += i < blk ? x : 0;
+    low += i < p.low ? x : 0;
   }
-  auto each = [&](auto&& body) {               // body(step, key)
-    if constexpr (KPT > 0) {
+  pick_digit(c, top, rest, bin, wave_n, picked);
+  const unsigned border = ((unsigned)p.state[4 * b] << kDigit12 | (unsigned)p.state[4 * b + 2]) << kDigit12 | (unsigned)bin;
+  if (top == bin) {
+    eq_n[0] = before;
+    eq_n[1] = low;
+  }
+  int more = 0, more_low = 0;                  // keys above the border's earlier digits: a block's to a thread
+  for (int i = tid; i < p.low || i < blk; i += kEvictThreads) {
+    const int64_t at = (int64_t)b * p.blocks + i;
+    const int x = p.above[at] + p.above[(int64_t)p.B * p.blocks + at];
+    more += i < blk ? x : 0;
+    more_low += i < p.low ? x : 0;
+  }
+  const int gt = block_sum(more + (top > bin ? before : 0), wave_n);
+  const int gt_low = block_sum(more_low + (top > bin ? low : 0), wave_n);
+  // rows above the border stay, and the first `rest` of those on it
+  const int eq = eq_n[0];
+  const int kept_low = gt_low + min(rest, eq_n[1]), kept = gt + min(rest, eq);
+  if (blk == 0 && tid == 0) p.count[b] = K - kept_low;
+  const unsigned long long below = (1ull << lane) - 1ull;
+  // a wave's rows are contiguous: its numbers go on from those of the waves before
+  unsigned long long on[kEvictRows], stay[kEvictRows];
+  int n_on = 0;
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) {
-        body(i, keys[i]);
-        if (i % kEvictBatch == kEvictBatch - 1) __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-      for (int i0 = 0; i0 < steps; i0 += kEvictBatch) {
-        float wt[kEvictBatch];
-        int pos[kEvictBatch];
-        fetch(i0, wt, pos);
+  for (int i = 0; i < kEvictRows; ++i) {
+    on[i] = __ballot(r.in[i] && r.key[i] == border);
+    n_on += __popcll(on[i]);
+  }
+  int at_eq = eq + block_before(lane == 0 ? n_on : 0, wave_n);
+  at_eq = __builtin_amdgcn_readfirstlane(at_eq);
+  int n_stay = 0, n_go = 0;
 #pragma unroll
-        for (int k = 0; k < kEvictBatch; ++k) body(i0 + k, evict_key(p, pos[k], wt[k], seen));
-      }
-    }
-  };
+  for (int i = 0; i < kEvictRows; ++i) {
+    const bool me = r.in[i] && (r.key[i] > border || (r.key[i] == border && at_eq + __popcll(on[i] & below) < rest));
+    at_eq += __popcll(on[i]);
+    stay[i] = __ballot(me);
+    n_stay += __popcll(stay[i]);
+    n_go += __popcll(__ballot(r.in[i]) & ~stay[i]);
+  }
+  const bool is_low = blk < p.low;
+  int at = block_before(lane == 0 ? (is_low ? n_go : n_stay) : 0, wave_n);
+  at = __builtin_amdgcn_readfirstlane(at) + (is_low ? blk * kEvictBlock - kept : kept - kept_low);
+  int32_t* const list = (is_low ? p.hole : p.move) + (int64_t)b * p.room;
+#pragma unroll
+  for (int i = 0; i < kEvictRows; ++i) {
+    const unsigned long long m = is_low ? __ballot(r.in[i]) & ~stay[i] : stay[i];
+    const bool listed = m >> lane & 1ull;
+    if (listed) list[at + __popcll(m & below)] = r.t[i];
+    at += __popcll(m);
+    // a row to fill gets its weight and position with the row that moves there
+    if (!is_low)
+      store(i, 0.f, -1);
+    else if (!listed)
+      store(i, r.weight[i], r.pos[i]);
+  }
+}
 
-  unsigned prefix = 0u, mask = 0u;
-  int rest = K;                                // of the rows that match the prefix, the rest-th largest is the border
+// The whole selection of a sequence in one workgroup, N rows a thread: up to 8K
+// rows it takes less than the four launches above (4K rows, B = 32: 13 us against
+// 23; 32K rows, whose keys do not fit the registers beside the rest: 84 against 23).
+template <int N>
+__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
+  __shared__ __attribute__((aligned(16))) int hist[1 << kDigit0];
+  __shared__ int wave_n[kEvictWaves], picked[2];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int L = clamp_len(p.lens, b, p.t_max), K = p.keep;
+  const int64_t base = (int64_t)b * p.t_max;
+  EvictRows<N> r;
+  evict_rows(p, b, 0, L, L, r);
+  auto store = [&](int i, float weight, int pos) {
+    if (r.t[i] >= p.t_max) return;
+    p.new_weights[base + r.t[i]] = weight;
+    if (p.new_row_pos != nullptr) p.new_row_pos[base + r.t[i]] = pos;
+  };
+  if (tid == 0) p.new_lens[b] = min(L, K);
+  if (L <= K) {                                // every row stays
+    if (tid == 0) p.count[b] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) store(i, r.in[i] ? r.weight[i] : 0.f, r.in[i] ? r.pos[i] : -1);
+    return;
+  }
+  unsigned border = 0u;
+  int rest = K;
 #pragma unroll
   for (int digit = 0; digit < 3; ++digit) {
-    const int bits = digit == 0 ? 13 : (digit == 1 ? 10 : 9), shift = digit == 0 ? 19 : (digit == 1 ? 9 : 0);
-    constexpr int kWide = kEvictBins / kEvictThreads;
-    const int per = digit == 0 ? kWide : 1;    // counters a thread holds
+    const int bits = digit == 0 ? kDigit0 : kDigit12, shift = digit == 0 ? 20 : (digit == 1 ? 10 : 0);
+    const int per = digit == 0 ? 4 : 1;
 #pragma unroll
     for (int k = 0; k < per; ++k) hist[tid + k * kEvictThreads] = 0;
     __syncthreads();
-    each([&](int i, unsigned x) {
-      if (s0 + 64 * i + lane < s1 && (x & mask) == prefix) atomicAdd(&hist[x >> shift & ((1u << bits) - 1u)], 1);
-    });
-    __syncthreads();
-    // the scan runs from the top: thread t holds the t-th `per` counters from there
-    const int first = (per * kEvictThreads - 1) - per * tid;
-    int c[kWide], sum = 0;
 #pragma unroll
-    for (int k = 0; k < per; ++k) {
-      c[k] = hist[first - k];
-      sum += c[k];
-    }
-    const int incl = wave_incl_scan(sum);
-    if (lane == 63) wave_n[0][w] = incl;
-    __syncthreads();
-    int above = incl - sum;
-    for (int i = 0; i < w; ++i) above += wave_n[0][i];
-#pragma unroll
-    for (int k = 0; k < per; ++k) {
-      if (above < rest && rest <= above + c[k]) {
-        pick_bin = first - k;
-        pick_rest = rest - above;
-      }
-      above += c[k];
+    for (int i = 0; i < N; ++i) {
+      const unsigned x = r.key[i] >> shift;
+      if (r.in[i] && (digit == 0 || x >> bits == border)) atomicAdd(&hist[x & ((1u << bits) - 1u)], 1);
     }
     __syncthreads();
-    prefix |= (unsigned)pick_bin << shift;
-    mask |= ((1u << bits) - 1u) << shift;
-    rest = pick_rest;
+    int bin;
+    const int top = (1 << bits) - 1 - per * tid;
+    if (digit == 0) {
+      int c[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] = hist[top - k];
+      pick_digit(c, top, rest, bin, wave_n, picked);
+    } else {
+      const int c[1] = {hist[top]};
+      pick_digit(c, top, rest, bin, wave_n, picked);
+    }
+    border = border << bits | (unsigned)bin;
   }
   // rows above the border stay, and the first `rest` of those on it
-  auto scan_waves = [&](int slot, int n) {     // the sum over the waves before this one
-    if (lane == 0) wave_n[slot][w] = n;
-    __syncthreads();
-    int before = 0;
-    for (int i = 0; i < w; ++i) before += wave_n[slot][i];
-    return before;
-  };
   const unsigned long long below = (1ull << lane) - 1ull;
-  int n_eq = 0;
-  each([&](int i, unsigned x) { n_eq += __popcll(__ballot(s0 + 64 * i + lane < s1 && x == prefix)); });
-  const int eq0 = scan_waves(1, n_eq);
-  auto stays = [&](int i, unsigned x, int& eq) {   // which rows of step i stay
-    const bool in = s0 + 64 * i + lane < s1;
-    const unsigned long long m = __ballot(in && x == prefix);
-    const bool me = in && (x > prefix || (x == prefix && eq + __popcll(m & below) < rest));
-    eq += __popcll(m);
-    return __ballot(me);
-  };
-  int n_hole = 0, n_move = 0, eq = eq0;
-  each([&](int i, unsigned x) {
-    const unsigned long long stay = stays(i, x, eq);
-    const int t = s0 + 64 * i + lane;
-    n_hole += __popcll(__ballot(t < s1 && t < K) & ~stay);
-    n_move += __popcll(stay & __ballot(t >= K));
-  });
-  int hole0 = scan_waves(2, n_hole);
-  int move0 = scan_waves(0, n_move);           // (slot 0 was last read two barriers ago)
-  if (tid == kEvictThreads - 1) p.count[b] = move0 + n_move;
-  eq = eq0;
-  auto emit = [&](int i, unsigned x, float wt, int pos) {
-    const unsigned long long stay = stays(i, x, eq);
-    const int t = s0 + 64 * i + lane;
-    const bool me = stay >> lane & 1ull;
-    const unsigned long long hm = __ballot(t < s1 && t < K) & ~stay, mm = stay & __ballot(t >= K);
-    if (hm >> lane & 1ull) p.hole[(int64_t)b * p.room + hole0 + __popcll(hm & below)] = t;
-    if (mm >> lane & 1ull) p.move[(int64_t)b * p.room + move0 + __popcll(mm & below)] = t;
-    if (me && t < K) {
-      p.new_weights[base + t] = wt;
-      if (p.new_row_pos != nullptr) p.new_row_pos[base + t] = pos;
-    }
-    hole0 += __popcll(hm);
-    move0 += __popcll(mm);
-  };
+  unsigned long long on[N], stay[N];
+  int n_on = 0, n_hole = 0, n_move = 0;
 #pragma unroll
-  for (int q = 0; q < (KPT > 0 ? NB : 1); ++q) {
-    for (int i0 = q * kEvictBatch; i0 < (KPT > 0 ? (q + 1) * kEvictBatch : nb * kEvictBatch); i0 += kEvictBatch) {
-      float wt[kEvictBatch];
-      int pos[kEvictBatch];
-      fetch(i0, wt, pos);
+  for (int i = 0; i < N; ++i) {
+    on[i] = __ballot(r.in[i] && r.key[i] == border);
+    n_on += __popcll(on[i]);
+  }
+  int at_eq = __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_on : 0, wave_n));
 #pragma unroll
-      for (int k = 0; k < kEvictBatch; ++k)
-        emit(i0 + k, KPT > 0 ? keys[KPT > 0 ? q * kEvictBatch + k : 0] : evict_key(p, pos[k], wt[k], seen), wt[k], pos[k]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  for (int i = 0; i < N; ++i) {
+    stay[i] = __ballot(r.in[i] && (r.key[i] > border || (r.key[i] == border && at_eq + __popcll(on[i] & below) < rest)));
+    at_eq += __popcll(on[i]);
+    n_hole += __popcll(__ballot(r.in[i] && r.t[i] < K) & ~stay[i]);
+    n_move += __popcll(stay[i] & __ballot(r.t[i] >= K));
+  }
+  // both numbers in one scan (each below 2^14)
+  const int both = __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_hole << 16 | n_move : 0, wave_n));
+  int hole = both >> 16, move = both & 0xFFFF;
+  if (tid == kEvictThreads - 1) p.count[b] = move + n_move;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const unsigned long long hm = __ballot(r.in[i] && r.t[i] < K) & ~stay[i], mm = stay[i] & __ballot(r.t[i] >= K);
+    if (hm >> lane & 1ull) p.hole[(int64_t)b * p.room + hole + __popcll(hm & below)] = r.t[i];
+    if (mm >> lane & 1ull) p.move[(int64_t)b * p.room + move + __popcll(mm & below)] = r.t[i];
+    hole += __popcll(hm);
+    move += __popcll(mm);
+    // a row to fill gets its weight and position with the row that moves there
+    if (r.t[i] >= K)
+      store(i, 0.f, -1);
+    else if (stay[i] >> lane & 1ull)
+      store(i, r.weight[i], r.pos[i]);
   }
 }
 
@@ -674,10 +833,10 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
     u32x4 x[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (c0 + qd + 4 * k < pieces) x[k] = src[(c0 + qd + 4 * k) * 16];
+      if (c0 + qd + 4 * k < pieces) x[k] = __builtin_nontemporal_load(src + (c0 + qd + 4 * k) * 16);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (c0 + qd + 4 * k < pieces) dst[(c0 + qd + 4 * k) * 16] = x[k];
+      if (c0 + qd + 4 * k < pieces) __builtin_nontemporal_store(x[k], dst + (c0 + qd + 4 * k) * 16);
   };
   if (g == p.G) {                              // what the groups share (a positional key has at most 16 pieces)
     if (p.kr_pieces > 0) tiled(p.kr + (int64_t)b * p.t_max * p.kr_pieces * 16, p.kr_pieces);
@@ -702,18 +861,6 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
   }
 }
 
-using SelectFn = void (*)(EvictParams);
-
-// The keys a lane holds, by the capacity.
-SelectFn pick_select(int t_max) {
-  if (t_max <= 4 * kEvictThreads) return evict_select_kernel<4>;
-  if (t_max <= 8 * kEvictThreads) return evict_select_kernel<8>;
-  if (t_max <= 16 * kEvictThreads) return evict_select_kernel<16>;
-  if (t_max <= 32 * kEvictThreads) return evict_select_kernel<32>;
-  if (t_max <= 64 * kEvictThreads) return evict_select_kernel<64>;
-  return evict_select_kernel<0>;
-}
-
 struct WeightLayout {
   size_t q_rot, part, bytes;
 };
@@ -730,17 +877,33 @@ int weight_layout(const gva_dims* d, int32_t n_new, WeightLayout& L) {
 }
 
 struct EvictLayout {
-  size_t hole, move, bytes;
-  int room;
+  size_t hole, move, state, above, hist0, hist1, hist2, bytes;
+  int room, blocks;
 };
 
+// The workspace for any budget: at most min(keep, t_max - keep) rows move, and
+// the rows below the budget and from it on make at most one block more.
 int evict_layout(const gva_dims* d, EvictLayout& L) {
   const int st = check_dims(d);
   if (st != GVA_OK) return st;
-  L.room = d->t_max / 2 + 1;                   // at most min(keep, t_max - keep) rows move
-  L.hole = round256((size_t)d->batch * 4);
-  L.move = L.hole + round256((size_t)d->batch * L.room * 4);
-  L.bytes = L.move + round256((size_t)d->batch * L.room * 4);
+  L.room = d->t_max / 2 + 1;
+  L.blocks = (d->t_max + kEvictBlock - 1) / kEvictBlock + 1;
+  const size_t B = (size_t)d->batch, n = B * (size_t)L.blocks;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += round256(bytes);
+    return at;
+  };
+  take(B * 4);                                 // count, at 0
+  L.hole = take(B * L.room * 4);
+  L.move = take(B * L.room * 4);
+  L.state = take(B * 16);
+  L.above = take(2 * n * 4);
+  L.hist0 = take(n << (kDigit0 + 1));
+  L.hist1 = take(n << (kDigit12 + 1));
+  L.hist2 = take(n << (kDigit12 + 1));
+  L.bytes = off;
   return GVA_OK;
 }
 
@@ -839,16 +1002,28 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
   const bool q4 = v4_scale != nullptr;
   st = q4 ? check_q4_dims(dims) : check_cache_layout(dims);
   if (st != GVA_OK) return st;
-  const long long blocks = q4 ? 1 : ((long long)dims->d_v * (long long)elem_size(dims) / 16 + 15) / 16;
-  if (dims->batch > 65535 || blocks * dims->n_groups >= 65535) return GVA_ERR_UNSUPPORTED;
+  const long long segs = q4 ? 1 : ((long long)dims->d_v * (long long)elem_size(dims) / 16 + 15) / 16;
+  if (dims->batch > 65535 || segs * dims->n_groups >= 65535) return GVA_ERR_UNSUPPORTED;
   char* ws = static_cast<char*>(workspace);
-  int32_t* count = reinterpret_cast<int32_t*>(ws);
-  int32_t* hole = reinterpret_cast<int32_t*>(ws + L.hole);
-  int32_t* move = reinterpret_cast<int32_t*>(ws + L.move);
+  auto ints = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
+  auto shorts = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
+  int32_t *count = ints(0), *hole = ints(L.hole), *move = ints(L.move);
+  const int low = ((n_keep < dims->t_max ? n_keep : dims->t_max) + kEvictBlock - 1) / kEvictBlock;
+  const int high = n_keep < dims->t_max ? (dims->t_max - n_keep + kEvictBlock - 1) / kEvictBlock : 0;
   const EvictParams p{lens, seen, weights, row_pos, new_lens, new_weights, new_row_pos, count, hole, move,
-                      dims->batch, dims->t_max, n_keep, n_first, n_recent, L.room};
+                      ints(L.state), ints(L.above), shorts(L.hist0), shorts(L.hist1), shorts(L.hist2),
+                      dims->batch, dims->t_max, n_keep, n_first, n_recent, L.room, low + high, low};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(pick_select(dims->t_max), dim3(dims->batch), dim3(kEvictThreads), 0, s, p);
+  const dim3 blocks((unsigned)(low + high), (unsigned)dims->batch);
+  if (dims->t_max <= 2 * kEvictBlock) {
+    hipLaunchKernelGGL((dims->t_max <= kEvictBlock ? evict_select_kernel<4> : evict_select_kernel<8>),
+                       dim3((unsigned)dims->batch), dim3(kEvictThreads), 0, s, p);
+  } else {
+    hipLaunchKernelGGL(evict_count_kernel<0>, blocks, dim3(kEvictThreads), 0, s, p);
+    hipLaunchKernelGGL(evict_count_kernel<1>, blocks, dim3(kEvictThreads), 0, s, p);
+    hipLaunchKernelGGL(evict_count_kernel<2>, blocks, dim3(kEvictThreads), 0, s, p);
+    hipLaunchKernelGGL(evict_number_kernel, blocks, dim3(kEvictThreads), 0, s, p);
+  }
   st = launch_status();
   const int most = n_keep < dims->t_max - n_keep ? n_keep : dims->t_max - n_keep;   // rows of a sequence that can move
   if (st != GVA_OK || most <= 0) return st;
