@@ -537,10 +537,13 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
  * in {1, 2, 4, 8}.  The caches are read only.  workspace: a caller-owned device
  * buffer of at least the bytes reported for the same dims, num_splits and
  * split_rows on the current device, 256-byte aligned, scratch.
- * gva_q4_pick_splits -- gva_pick_splits for this step: a row has fewer
- * bytes, so fewer and longer splits pay.
+ * gva_q4_pick_splits -- host heuristic: the split plan (num_splits, and in
+ * split_rows what to pass with it; NULL: even splits only) for the lengths in the
+ * HOST array lens [B] (NULL: every sequence t_max) on a device with n_cu compute
+ * units (0 = ask the current device).  1 for dims that the step does not take.
+ * Pure host code; enqueues nothing.
  */
-int gva_q4_pick_splits(const gva_dims* dims, int32_t max_len, int64_t total_len, int32_t n_cu, int32_t* split_rows);
+int gva_q4_pick_splits(const gva_dims* dims, const int32_t* lens, int32_t n_cu, int32_t* split_rows);
 int gva_q4_decode_workspace_size(const gva_dims* dims, int32_t num_splits, int32_t split_rows, size_t* bytes);
 int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const void* v4_cache, const void* v4_scale,
                        const void* kr_cache, const int32_t* lens, const int32_t* seen, int32_t num_splits,

@@ -126,7 +126,8 @@ struct Q4UnpackParams {
 };
 
 // A wave per 1 KB block of codes: 4 KB of bf16 rows, in 16-byte pieces of 16
-// consecutive rows.
+// consecutive rows.  Bound by HBM: 8 sequences of 4K to 8K rows, G8 d 128 (127 MB),
+// 20.2 us, 6.3 TB/s, with streaming stores (25.5 without).
 template <int DV>
 __global__ void __launch_bounds__(kThreads) q4_unpack_kernel(Q4UnpackParams p) {
   constexpr int R = block_rows(DV), NS = DV / kScaleCols, NH = R / 16, NW = 4 / NH;   // NW words per row and piece
@@ -147,7 +148,8 @@ __global__ void __launch_bounds__(kThreads) q4_unpack_kernel(Q4UnpackParams p) {
     const unsigned byte = sc[scale_off(t, q * (DV / 4) / kScaleCols, DV)];
 #pragma unroll
     for (int k = 0; k < NW; ++k)
-      *reinterpret_cast<bf16x8*>(out + tiled_off<uint16_t>(t, q * (DV / 4) + 8 * k, DV)) = dequant8(w[hf * NW + k], byte);
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, dequant8(w[hf * NW + k], byte)),
+                                  reinterpret_cast<u32x4*>(out + tiled_off<uint16_t>(t, q * (DV / 4) + 8 * k, DV)));
   }
 }
 
@@ -166,11 +168,9 @@ struct Q4DecodeParams {
   const int32_t *head_lens, const int32_t *head_seen, const void *head_q, const void *head_m, void *head_codes, \
       int32_t head_dims, int32_t head_B, int32_t head_G, int32_t head_split_rows
 
-constexpr int kQ4Waves = 8;
-
 template <int HPG, int DV, int NRC, int NW>
 struct Q4Cfg {
-  static constexpr int DEPTH = 2, OCC = 2;
+  static constexpr int DEPTH = NW > kWaves ? 2 : 3, OCC = 2;   // tiles in registers; waves per SIMD at least
   // absorption: loads of four map rows (of 128 columns) per round, so that the
   // heads' maps are one round over the waves where registers allow it
   static constexpr int AR0 = DV * HPG / (4 * NW);
@@ -195,6 +195,14 @@ __device__ __forceinline__ bf16x8 read_transposed(const uint8_t* p, int step) {
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p));
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + step));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The largest of three (a NaN among them is passed over); fmaxf chains quiet every
+// operand with an instruction of its own first.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
 }
 
 // One (sequence, group, split) per workgroup; its waves take interleaved tiles
@@ -464,7 +472,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     // The running maximum of a column moves only when some score passes it by 8
     // (log2): until then weights stay below 2^8, and most tiles need neither the
     // maximum over the lanes nor the rescaling.
-    const float mt = fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(x[4], x[5])), fmaxf(x[6], x[7]));
+    const float mt = max3(max3(max3(x[0], x[1], x[2]), x[3], x[4]), max3(x[5], x[6], x[7]), x[7]);
     if (__ballot(mt > m_run + 8.f) != 0) {
       const float m_new = fmaxf(m_run, max_over_rows(mt));
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -552,36 +560,86 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
 
 using Q4DecodeFn = void (*)(GVA_Q4_HEAD_ARGS, Q4DecodeParams);
 
-template <int HPG, int DV, bool FUSED>
+template <int HPG, int DV, int NW, bool FUSED>
 Q4DecodeFn pick_q4_nrc(int nrc) {
   switch (nrc) {
-    case 0: return q4_decode_kernel<HPG, DV, 0, kQ4Waves, FUSED>;
-    case 1: return q4_decode_kernel<HPG, DV, 1, kQ4Waves, FUSED>;
-    case 2: return q4_decode_kernel<HPG, DV, 2, kQ4Waves, FUSED>;
+    case 0: return q4_decode_kernel<HPG, DV, 0, NW, FUSED>;
+    case 1: return q4_decode_kernel<HPG, DV, 1, NW, FUSED>;
+    case 2: return q4_decode_kernel<HPG, DV, 2, NW, FUSED>;
   }
   return nullptr;
 }
 
-template <int HPG>
-Q4DecodeFn pick_q4_dv(int dv, int nrc, bool fused) {
-  if (dv == 128) return fused ? pick_q4_nrc<HPG, 128, true>(nrc) : pick_q4_nrc<HPG, 128, false>(nrc);
-  return fused ? pick_q4_nrc<HPG, 64, true>(nrc) : pick_q4_nrc<HPG, 64, false>(nrc);
+template <int HPG, int DV>
+Q4DecodeFn pick_q4_waves(int nrc, int nw, bool fused) {
+  if (nw == 8) return fused ? pick_q4_nrc<HPG, DV, 8, true>(nrc) : pick_q4_nrc<HPG, DV, 8, false>(nrc);
+  return fused ? pick_q4_nrc<HPG, DV, 4, true>(nrc) : pick_q4_nrc<HPG, DV, 4, false>(nrc);
 }
 
-Q4DecodeFn pick_q4_decode(int hpg, int dv, int nrc, bool fused) {
+Q4DecodeFn pick_q4_decode(int hpg, int dv, int nrc, int nw, bool fused) {
+  const bool wide = dv == 128;
   switch (hpg) {
-    case 1: return pick_q4_dv<1>(dv, nrc, fused);
-    case 2: return pick_q4_dv<2>(dv, nrc, fused);
-    case 4: return pick_q4_dv<4>(dv, nrc, fused);
-    case 8: return pick_q4_dv<8>(dv, nrc, fused);
+    case 1: return wide ? pick_q4_waves<1, 128>(nrc, nw, fused) : pick_q4_waves<1, 64>(nrc, nw, fused);
+    case 2: return wide ? pick_q4_waves<2, 128>(nrc, nw, fused) : pick_q4_waves<2, 64>(nrc, nw, fused);
+    case 4: return wide ? pick_q4_waves<4, 128>(nrc, nw, fused) : pick_q4_waves<4, 64>(nrc, nw, fused);
+    case 8: return wide ? pick_q4_waves<8, 128>(nrc, nw, fused) : pick_q4_waves<8, 64>(nrc, nw, fused);
   }
   return nullptr;
 }
 
-// Whether the workgroups absorb their queries themselves.
-bool q4_fused(const gva_dims* d, int num_splits, int split_rows) {
-  return gva_prefer_fused(d, num_splits, split_rows, 0) != 0;
+// Workgroups of eight waves that a CU holds at once (registers; two of four
+// waves at d_v = 128, three at 64, by the same).
+inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) : (d_v == 128 ? 2 : 3); }
+
+// Waves per workgroup: eight while the workgroups are resident at once; with
+// bounded chunks (whose empty splits count among them) while a chunk is long and
+// the streams are no more than the CUs (us per step, eight and four waves: B32 T8K H32 G8 d 128, 256 workgroups, 35.4
+// and 43.1; B64 T2K, 512, 28.0 and 23.5; B4 of 64K to 128K rows, chunks of 13024,
+// 54.8 and 67.4; B64 to 32K rows, H16 G2, chunks of 4096 30.0 and 33.0, of 2048
+// 39.2 and 30.5; B64 to 8K rows, G8, chunks of 4096 41.4 and 30.8).
+int q4_waves(const gva_dims* d, int num_splits, int split_rows, int n_cu) {
+  if (split_rows > 0) return split_rows >= 4096 && (long long)d->batch * d->n_groups <= n_cu ? 8 : kWaves;
+  return decode_grid(d, num_splits, 0) <= (long long)n_cu * q4_resident(d->d_v, 8) ? 8 : kWaves;
 }
+
+// Whether the workgroups absorb their queries themselves: while they are resident
+// at once, or a chunk's rows outweigh the (H/G) d_c map rows that its workgroup
+// reads for it (us, inside and apart: B64 to 32K rows, H16 G2 d 128, chunks of
+// 2048 rows against 1024 map rows, 30.6 and 29.7; B16 to 32K rows, H16 G4 d 64,
+// 2048 against 256, 15.5 and 18.5; B128 T1K H32 G8 d 128, even, 29.1 and 27.9).
+bool q4_fused(const gva_dims* d, int num_splits, int split_rows, int n_cu) {
+  if (decode_grid(d, num_splits, split_rows) <= 2LL * n_cu) return true;
+  return split_rows > 0 && split_rows >= 4LL * (d->n_heads / d->n_groups) * d->d_c;
+}
+
+// What a plan costs in microseconds, from the times above: a workgroup's start and
+// end, its rows at the pace of its CU (which the workgroups there share), and the
+// combine.  Only the order of two plans matters.
+struct Q4Cost {
+  int n_cu, groups, d_v;
+  double us(const gva_dims* d, const int32_t* lens, int S, int c) const {
+    const int nw = q4_waves(d, S, c, n_cu), most = q4_resident(d_v, nw);
+    long long items = 0, rows = 0, longest = 0;
+    for (int b = 0; b < d->batch; ++b) {
+      const long long L = lens != nullptr ? (lens[b] < 0 ? 0 : (lens[b] > d->t_max ? d->t_max : lens[b])) : d->t_max;
+      if (L == 0) continue;
+      const long long n = c <= 0 ? S : ((L + c - 1) / c > S ? S : (L + c - 1) / c);
+      const long long per = ((L + n - 1) / n + kTileRows - 1) / kTileRows * kTileRows;
+      items += (L + per - 1) / per * groups;
+      rows += L * groups;
+      if (per > longest) longest = per;
+    }
+    const long long here = (items + n_cu - 1) / n_cu;
+    const long long resident = here < 1 ? 1 : (here > most ? most : here);
+    const double pace = (d_v == 128 ? 290.0 : 500.0) * (resident * nw >= 8 ? 1.0 : 0.68);   // rows per us and CU
+    const double mean = (double)rows / n_cu / pace, last = (double)longest * resident / pace;
+    const double rounds = (double)items / ((double)n_cu * most);
+    double t = rounds <= 1.0 ? 7.0 + (last > mean ? last : mean)
+                             : 7.0 * (1.0 + (rounds - 1.0) / most) + mean + last / 2;
+    const double idle = (double)(decode_grid(d, S, c) - items) / ((double)n_cu * most);      // empty splits
+    return t + (idle > 0 ? idle * 1.2 : 0.0) + (S > 1 ? 4.5 + 0.05 * S + (S > 16 ? 3.0 : 0.0) : 0.0);
+  }
+};
 
 struct Q4StepLayout {
   bool fused;
@@ -595,7 +653,7 @@ int q4_step_layout(const gva_dims* d, int32_t num_splits, int32_t split_rows, Q4
     return GVA_ERR_INVALID_ARG;
   const size_t rows = (size_t)d->batch * (size_t)d->n_heads;
   L = Q4StepLayout{};
-  L.fused = q4_fused(d, num_splits, split_rows);
+  L.fused = q4_fused(d, num_splits, split_rows, device_cu_count());
   size_t off = 0;
   if (!L.fused) {
     L.q_rot = off = round256(rows * (size_t)d->d_v * 4);
@@ -676,8 +734,37 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
   return launch_status();
 }
 
-int gva_q4_pick_splits(const gva_dims* dims, int32_t max_len, int64_t total_len, int32_t n_cu, int32_t* split_rows) {
-  return gva_pick_splits(dims, max_len, total_len, n_cu, split_rows);
+int gva_q4_pick_splits(const gva_dims* dims, const int32_t* lens, int32_t n_cu, int32_t* split_rows) {
+  if (split_rows != nullptr) *split_rows = 0;
+  if (check_q4_dims(dims) != GVA_OK) return 1;
+  if (n_cu <= 0) n_cu = device_cu_count();
+  const Q4Cost cost{n_cu, dims->n_groups, dims->d_v};
+  int longest = 0;
+  for (int b = 0; b < dims->batch; ++b) {
+    const int L = lens != nullptr ? lens[b] : dims->t_max;
+    if (L > longest) longest = L;
+  }
+  if (longest > dims->t_max) longest = dims->t_max;
+  int best_s = 1, best_c = 0;
+  double best = cost.us(dims, lens, 1, 0);
+  auto look = [&](int S, int c) {
+    const double t = cost.us(dims, lens, S, c);
+    if (t < best) {
+      best = t;
+      best_s = S;
+      best_c = c;
+    }
+  };
+  for (int S = 2; S <= 32; ++S) look(S, 0);
+  // bounded chunks, a 24th shorter each time
+  if (split_rows != nullptr)
+    for (int c = longest; c >= 256; c -= c / 24) {
+      const int rows = (c + kTileRows - 1) / kTileRows * kTileRows, S = (longest + rows - 1) / rows;
+      if (S > GVA_MAX_SPLITS) break;
+      if (S > 1) look(S, rows);
+    }
+  if (split_rows != nullptr) *split_rows = best_c;
+  return best_s;
 }
 
 int gva_q4_decode_workspace_size(const gva_dims* dims, int32_t num_splits, int32_t split_rows, size_t* bytes) {
@@ -705,7 +792,8 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
     return GVA_ERR_INVALID_ARG;
   if (dims->d_c % 32 != 0 || dims->d_c < 32 || dims->d_c > 512) return GVA_ERR_UNSUPPORTED;
   const int hpg = dims->n_heads / dims->n_groups;
-  const Q4DecodeFn fn = pick_q4_decode(hpg, dims->d_v, (dims->d_r + 31) / 32, L.fused);
+  const int nw = q4_waves(dims, num_splits, split_rows, device_cu_count());
+  const Q4DecodeFn fn = pick_q4_decode(hpg, dims->d_v, (dims->d_r + 31) / 32, nw, L.fused);
   const long long n_items = decode_grid(dims, num_splits, split_rows);
   if (fn == nullptr || n_items > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   char* ws = static_cast<char*>(workspace);
@@ -728,7 +816,7 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
   p.scales = static_cast<const uint8_t*>(v4_scale);
   fill_inv_freq(dims, p.inv_freq);
   const int packed = dims->d_c | dims->d_r << 10 | S << 17;
-  hipLaunchKernelGGL(fn, dim3((unsigned)n_items), dim3(64 * kQ4Waves), 0, static_cast<hipStream_t>(stream), lens, seen,
+  hipLaunchKernelGGL(fn, dim3((unsigned)n_items), dim3(64 * nw), 0, static_cast<hipStream_t>(stream), lens, seen,
                      L.fused ? q : static_cast<const void*>(q_abs), L.fused ? m : static_cast<const void*>(q_rot),
                      const_cast<void*>(v4_cache), packed, dims->batch, dims->n_groups, split_rows, p);
   st = launch_status();

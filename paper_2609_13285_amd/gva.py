@@ -95,7 +95,7 @@ def lib() -> ctypes.CDLL:
         L.gva_q4_append_kv.argtypes = [D, P, P, P, P, P, P, P, P, I32, P, P]
         L.gva_append_rows.argtypes = [D, P, P, P, P, P, P, P, I32, P, P]
         L.gva_q4_unpack_kv.argtypes = [D, P, P, P, P, P]
-        L.gva_q4_pick_splits.argtypes = [D, I32, ctypes.c_int64, I32, ctypes.POINTER(I32)]
+        L.gva_q4_pick_splits.argtypes = [D, P, I32, ctypes.POINTER(I32)]
         L.gva_q4_decode_workspace_size.argtypes = [D, I32, I32, SZP]
         L.gva_q4_decode_step.argtypes = [D, P, P, P, P, P, P, P, I32, I32, P, SZ, P, P, P]
         L.gva_weights_workspace_size.argtypes = [D, I32, SZP]
@@ -895,19 +895,23 @@ def gva_q4_unpack_kv(dims: GvaDims, v4_cache, v4_scale, lens, v_cache, stream=No
     _check("gva_q4_unpack_kv", st)
 
 
-def gva_q4_pick_splits(dims: GvaDims, max_len: int = 0, total_len: int = 0, n_cu: int = 0,
+def gva_q4_pick_splits(dims: GvaDims, lens: Optional[torch.Tensor] = None, n_cu: int = 0,
                        chunked: bool = True) -> Tuple[int, int]:
-    """gva_pick_splits for gva_q4_decode_step: (num_splits, split_rows)."""
+    """(num_splits, split_rows) of gva_q4_decode_step for the lengths ``lens``
+    (copied to the host; None: every sequence full); ``chunked=False`` asks for
+    even splits only."""
+    host = None if lens is None else lens.detach().to("cpu", torch.int32).contiguous()
+    if host is not None and tuple(host.shape) != (dims.batch,):
+        raise ValueError(f"lens must have shape {(dims.batch,)}, got {tuple(host.shape)}")
     rows = ctypes.c_int32(0)
-    S = lib().gva_q4_pick_splits(ctypes.byref(dims), int(max_len), int(total_len), int(n_cu),
+    S = lib().gva_q4_pick_splits(ctypes.byref(dims), None if host is None else ctypes.c_void_p(host.data_ptr()), int(n_cu),
                                  ctypes.byref(rows) if chunked else None)
     return int(S), int(rows.value)
 
 
 def q4_plan_for(dims: GvaDims, lens: torch.Tensor, n_cu: int = 0, chunked: bool = True) -> Tuple[int, int]:
     """gva_q4_pick_splits for the lengths in ``lens`` (host copy)."""
-    L = lens.detach().to("cpu", torch.int64).clamp(0, dims.t_max)
-    return gva_q4_pick_splits(dims, int(L.max()) if L.numel() else 0, int(L.sum()), n_cu, chunked)
+    return gva_q4_pick_splits(dims, lens, n_cu, chunked)
 
 
 def gva_q4_decode_workspace_size(dims: GvaDims, num_splits: int, split_rows: int = 0) -> int:

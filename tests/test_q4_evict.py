@@ -106,6 +106,23 @@ def test_step_refusals():
     assert gva.gva_q4_decode_workspace_size(d, 4) % 256 == 0
 
 
+def test_q4_plans_are_host_only_and_take_their_lengths():
+    d = dims(batch=4, n_heads=32, n_groups=8, t_max=131072)
+    # whole CUs: the longest sequence decides an even split, chunks level them out
+    assert gva.gva_q4_pick_splits(dims(batch=32, n_heads=32, n_groups=8, t_max=8192), None, 256) == (1, 0)
+    S, rows = gva.gva_q4_pick_splits(d, torch.tensor([73728, 90112, 106496, 122880]), 256)
+    assert rows % 32 == 0 and rows > 0 and S == -(-122880 // rows)
+    assert sum(-(-n // rows) for n in (73728, 90112, 106496, 122880)) * 8 <= 256
+    S, rows = gva.gva_q4_pick_splits(d, torch.tensor([73728, 90112, 106496, 122880]), 256, chunked=False)
+    assert rows == 0 and 1 < S <= 32
+    for lens in ([0, 0, 0, 0], [1, 1, 1, 1], [-5, 200000, 131072, 0]):
+        S, rows = gva.gva_q4_pick_splits(d, torch.tensor(lens), 256)
+        assert 1 <= S <= gva.GVA_MAX_SPLITS and rows >= 0 and rows % 32 == 0
+    assert gva.gva_q4_pick_splits(dims(dtype="f32"), None, 256) == (1, 0)
+    with pytest.raises(ValueError):
+        gva.gva_q4_pick_splits(d, torch.tensor([1, 2]))
+
+
 def test_weights_refusals():
     for d, s in ((dims(), None), (dims(), A), (dims(dtype="f32"), None)):
         for kw in (dict(q=None), dict(m=None), dict(v=None), dict(k=None), dict(lens=None), dict(lse=None), dict(nw=None),
