@@ -415,10 +415,10 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
   // no tile before the first: rows and weights of 0
   for (int i = lane * 16; i < 32 * PITCH; i += 64 * 16) *reinterpret_cast<u32x4*>(tr + i) = u32x4{0u, 0u, 0u, 0u};
   bf16x8 bp = zero8;
-  float m_run = -__FLT_MAX__;
+  float m_run = 0.f, m_limit = -INFINITY;      // no maximum yet: any score sets it
+  f32x4 start = {0.f, 0.f, 0.f, 0.f};          // of the score products: -m_run in the high columns
   f32x4 l_run = {0.f, 0.f, 0.f, 0.f};          // the sum of a column's weights, four times
   const bf16x8 ones = as_bf16x8(u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
-  const uint32_t lo_mask = is_lo ? 0xFFFF0000u : 0u;
   f32x4 acc[NB];
 #pragma unroll
   for (int ib = 0; ib < NB; ++ib) acc[ib] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     for (int ib = 0; ib < NB; ++ib) vt[ib] = read_transposed(tr_get + 32 * ib, 16 * PITCH);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();           // this tile is written after those reads
-    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    f32x4 sc[2] = {start, start};
 #pragma unroll
     for (int rc = 0; rc < NRC; ++rc)
 #pragma unroll
@@ -457,44 +457,58 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
         acc[2 * c + hf] = mfma16(vt[2 * c + hf], bp, acc[2 * c + hf]);
       }
     l_run = mfma16(ones, bp, l_run);
-    float x[8];
+    // Each of a head's two lanes takes the sum of the parts, and the exponential,
+    // for one half of the rows: the high column's lane the first 16.
+    float x[4];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int jj = 0; jj < 4; ++jj) x[4 * hf + jj] = sc[hf][jj] + mirror<HPG>(sc[hf][jj]);
+    for (int j = 0; j < 4; ++j) x[j] = (is_lo ? sc[1][j] : sc[0][j]) + mirror<HPG>(is_lo ? sc[0][j] : sc[1][j]);
     if (tail) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (row0 + 16 * (k >> 2) + 4 * qd + (k & 3) >= r1) x[k] = -INFINITY;
+      for (int j = 0; j < 4; ++j)
+        if (row0 + (is_lo ? 16 : 0) + 4 * qd + j >= r1) x[j] = -INFINITY;
       __builtin_amdgcn_sched_barrier(0);
     }
-    // The running maximum of a column moves only when some score passes it by 8
-    // (log2): until then weights stay below 2^8, and most tiles need neither the
+    // The scores come less the running maximum (the products start from it), which
+    // moves only when a column's score passes it by 8 (log2), or its first one
+    // comes: until then weights stay below 2^8, and most tiles need neither the
     // maximum over the lanes nor the rescaling.
-    const float mt = max3(max3(max3(x[0], x[1], x[2]), x[3], x[4]), max3(x[5], x[6], x[7]), x[7]);
-    if (__ballot(mt > m_run + 8.f) != 0) {
-      const float m_new = fmaxf(m_run, max_over_rows(mt));
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    const float mt = max3(max3(x[0], x[1], x[2]), x[3], x[3]);
+    if (__ballot(mt > m_limit) != 0) {
+      const float top = max_over_rows(fmaxf(mt, mirror<HPG>(mt)));
+      const bool moves = top > m_limit;
+      const float by = moves ? top : 0.f;
+      const float alpha = moves && m_limit != -INFINITY ? __builtin_amdgcn_exp2f(-by) : 1.f;
       l_run *= alpha;
 #pragma unroll
       for (int ib = 0; ib < NB; ++ib) acc[ib] *= alpha;
-      m_run = m_new;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] -= by;
+      m_run += by;
+      m_limit = moves ? 8.f : m_limit;
+      const float s0 = is_lo ? 0.f : -m_run;
+      start = f32x4{s0, s0, s0, s0};
     }
-    // Weights as bf16 parts: the high columns take the upper half of the fp32
-    // number, the low columns that of what it leaves (off by less than 2^-15;
-    // the sum of the weights is taken from the same parts by a product with
-    // ones, so what truncation loses on average cancels in o).
+    // Weights as bf16 parts, each rounded to nearest: the high columns' own, and
+    // in the low columns that of what the high part leaves (together off by at
+    // most 2^-18; a single bf16 weight, 2^-9, would show in o at 1e-3).  The two
+    // lanes exchange what the other needs.  The sum of the weights is a product
+    // with ones.
+    uint32_t keep[2], got[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const f32x2 e = {__builtin_amdgcn_exp2f(x[2 * j]), __builtin_amdgcn_exp2f(x[2 * j + 1])};
+      const bf16x2 h = __builtin_convertvector(e, bf16x2);
+      const bf16x2 l = __builtin_convertvector(e - __builtin_convertvector(h, f32x2), bf16x2);
+      const uint32_t hb = __builtin_bit_cast(uint32_t, h), lb = __builtin_bit_cast(uint32_t, l);
+      keep[j] = is_lo ? lb : hb;
+      got[j] = __float_as_uint(mirror<HPG>(__uint_as_float(is_lo ? hb : lb)));
+    }
     u32x4 parts;
 #pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-      float y[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float e = __builtin_amdgcn_exp2f(x[k + j] - m_run);
-        y[j] = e - __uint_as_float(__float_as_uint(e) & lo_mask);
-      }
-      parts[k / 2] = __builtin_amdgcn_perm(__float_as_uint(y[1]), __float_as_uint(y[0]), 0x07060302u);
+    for (int j = 0; j < 2; ++j) {
+      parts[j] = is_lo ? got[j] : keep[j];
+      parts[2 + j] = is_lo ? keep[j] : got[j];
     }
     bp = as_bf16x8(parts);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
