@@ -533,7 +533,9 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
  * gva_q4_decode_workspace_size, gva_q4_decode_step -- gva_decode_step on a
  * 4-bit cache that holds the current token's row already (gva_q4_append_kv):
  * o and lse as there, with x_t over the values that the codes stand for and the
- * query rotated at position seen[b] - 1.  d_c a multiple of 32 (32 .. 512), H/G
+ * query rotated at position seen[b] - 1.  The query enters the products as a
+ * bf16 high and a low part, so cached positional keys must be finite (their
+ * lowest value hides a row as -inf would).  d_c a multiple of 32 (32 .. 512), H/G
  * in {1, 2, 4, 8}.  The caches are read only.  workspace: a caller-owned device
  * buffer of at least the bytes reported for the same dims, num_splits and
  * split_rows on the current device, 256-byte aligned, scratch.
@@ -560,15 +562,15 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
  * with x the scaled score of gva_decode_attention, query i of sequence b at
  * position seen[b] - n_new + i, seeing rows t <= L_b - n_new + i as in a
  * prompt.  Rows from L_b on of new_weights are left as they were.  A query with
- * lse -inf (nothing to see) adds nothing.  decay 0 reads no weights (NULL is
- * allowed); new_weights may be weights itself, else it must not overlap it.
+ * lse -inf (nothing to see) adds nothing.  decay (>= 0) of 0 reads no weights (NULL
+ * is allowed); new_weights may be weights itself, else it must not overlap it.
  * q [B][n_new][H][d_c + d_r] and M in the storage dtype, lse [B][n_new][H] as
  * the attention calls return it, weights [B][T] fp32.  n_new == 1 is a decode
  * step's query, more are a window of a prompt's last ones (1 <= n_new <= T).
  * v_cache is a bf16 or fp32 cache where v4_scale is NULL, else a 4-bit one.
  * bf16 and 4-bit caches: d_v in {64, 128}, d_c a multiple of 32, d_r one of 8
- * (<= 64); fp32: what the tiled layout takes.  Any H/G.  The sums have a
- * fixed order.
+ * (<= 64), positional keys finite as for gva_q4_decode_step; fp32: what the
+ * tiled layout takes.  Any H/G, batch <= 65535.  The sums have a fixed order.
  */
 int gva_weights_workspace_size(const gva_dims* dims, int32_t n_new, size_t* bytes);
 int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, const void* m, const void* v_cache,
@@ -591,7 +593,7 @@ int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, c
  * new_lens, new_weights and new_row_pos must not overlap their counterparts;
  * row_pos and new_row_pos come together (NULL: position = row, as long as
  * nothing has been evicted).  v_cache, v4_scale as for gva_accumulate_weights;
- * every shape that the tiled layout (or the 4-bit one) takes.
+ * every shape that the tiled layout (or the 4-bit one) takes, batch <= 65535.
  */
 int gva_evict_workspace_size(const gva_dims* dims, size_t* bytes);
 int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_t n_recent, void* v_cache,

@@ -938,7 +938,7 @@ int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, c
   if (st != GVA_OK) return st;
   if (!q || !m || !v_cache || !lens || !lse || !new_weights) return GVA_ERR_INVALID_ARG;
   if (dims->d_r > 0 && !kr_cache) return GVA_ERR_INVALID_ARG;
-  if (!(decay >= 0.0) || !isfinite(decay) || (decay != 0.0 && !weights)) return GVA_ERR_INVALID_ARG;
+  if (!(decay >= 0.0) || !isfinite((float)decay) || (decay != 0.0 && !weights)) return GVA_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(m, 16) || !aligned(v_cache, 16) || !aligned(v4_scale, 16) || !aligned(lens, 4) ||
       !aligned(seen, 4) || !aligned(lse, 4) || !aligned(weights, 4) || !aligned(new_weights, 4) ||
       (dims->d_r > 0 && !aligned(kr_cache, 16)))

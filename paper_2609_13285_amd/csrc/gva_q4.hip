@@ -131,10 +131,11 @@ struct Q4UnpackParams {
 template <int DV>
 __global__ void __launch_bounds__(kThreads) q4_unpack_kernel(Q4UnpackParams p) {
   constexpr int R = block_rows(DV), NS = DV / kScaleCols, NH = R / 16, NW = 4 / NH;   // NW words per row and piece
-  const int stream = blockIdx.y;
+  const int per = (p.t_max / R + kWaves - 1) / kWaves;   // workgroups of a stream
+  const int stream = blockIdx.x / per;
   const int b = stream / p.G;
   const int lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-  const int blk = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int blk = blockIdx.x % per * kWaves + (threadIdx.x >> 6);
   const int t0 = blk * R;
   const int L = clamp_len(p.lens, b, p.t_max);
   if (t0 >= L) return;
@@ -737,13 +738,12 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
     return GVA_ERR_INVALID_ARG;
   st = check_q4_dims(dims);
   if (st != GVA_OK) return st;
-  const long long streams = (long long)dims->batch * dims->n_groups;
-  if (streams > 65535) return GVA_ERR_UNSUPPORTED;
+  const int R = block_rows(dims->d_v);
+  const long long grid = (long long)dims->batch * dims->n_groups * ((dims->t_max / R + kWaves - 1) / kWaves);
+  if (grid > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   Q4UnpackParams p{static_cast<const uint8_t*>(v4_cache), static_cast<const uint8_t*>(v4_scale), lens,
                    static_cast<uint16_t*>(v_cache), dims->batch, dims->n_groups, dims->t_max};
-  const int blocks = dims->t_max / block_rows(dims->d_v);
-  const dim3 grid((unsigned)((blocks + kWaves - 1) / kWaves), (unsigned)streams);
-  hipLaunchKernelGGL((dims->d_v == 128 ? q4_unpack_kernel<128> : q4_unpack_kernel<64>), grid, dim3(kThreads), 0,
+  hipLaunchKernelGGL((dims->d_v == 128 ? q4_unpack_kernel<128> : q4_unpack_kernel<64>), dim3((unsigned)grid), dim3(kThreads), 0,
                      static_cast<hipStream_t>(stream), p);
   return launch_status();
 }

@@ -126,7 +126,7 @@ def test_q4_plans_are_host_only_and_take_their_lengths():
 def test_weights_refusals():
     for d, s in ((dims(), None), (dims(), A), (dims(dtype="f32"), None)):
         for kw in (dict(q=None), dict(m=None), dict(v=None), dict(k=None), dict(lens=None), dict(lse=None), dict(nw=None),
-                   dict(N=0), dict(N=65), dict(decay=-0.5), dict(decay=math.nan), dict(decay=math.inf), dict(w=None),
+                   dict(N=0), dict(N=65), dict(decay=-0.5), dict(decay=1e39), dict(decay=math.nan), dict(decay=math.inf), dict(w=None),
                    dict(v=A + 8), dict(lse=A + 2), dict(w=A + 2), dict(nw=A + 1), dict(seen=A + 2), dict(ws=None),
                    dict(ws=A + 64), dict(n=512)):
             assert weights_status(d, s=s, **kw) == gva.GVA_ERR_INVALID_ARG, kw
@@ -401,6 +401,54 @@ def test_step_sharp_scores_and_far_positions():
     x = problem(2, 512, 8, 2, 128, 128, 32, [512, 300], extra=1 << 20, seed=5, q_std=6.0)
     note("q4 step, sharp scores, far positions")
     check_step(x, *step(x, 2, 0))
+
+
+def hide_rows(x, rows, d_r, cache="q4"):
+    """Rows hidden from every query by the lowest bf16 in a positional key, the
+    scores of the others near -30 (log2); returns the hidden rows' mask."""
+    T, lowest = x["d"].t_max, float(torch.finfo(torch.bfloat16).min)
+    W = x["q"].shape[-1]
+    x["q"][..., :W - d_r] = 0.0
+    x["q"][..., W - d_r:] = 0.0
+    x["q"][..., W - 2] = 40.0                            # the slowest pair: hardly turned at these positions
+    x["kr"].zero_()
+    x["kr"][..., d_r - 2] = -0.5 * math.sqrt(W)
+    x["kr"][:, rows, d_r - 2] = lowest
+    x["kc"] = gva.tiled(x["kr"].to(torch.bfloat16)).cuda()
+
+
+@gpu
+@pytest.mark.parametrize("hpg,d_v", [(4, 128), (8, 64), (1, 64)])
+@pytest.mark.parametrize("S", [1, 3])
+def test_step_hidden_rows(hpg, d_v, S):
+    """Whole tiles hidden (a wave's first, its only one), single rows, and every
+    row of a sequence: the running maximum starts at the first row that counts."""
+    T = 320
+    x = problem(3, T, 2 * hpg, 2, d_v, 64, 16, [T, 70, 200], seed=hpg)
+    rows = torch.zeros(T, dtype=torch.bool)
+    rows[:64] = rows[128:160] = True
+    rows[5::7] = True
+    hide_rows(x, rows, 16)
+    x["kr"][1, :, 14] = float(torch.finfo(torch.bfloat16).min)       # the second sequence: nothing to see
+    x["kc"] = gva.tiled(x["kr"].to(torch.bfloat16)).cuda()
+    note(f"q4 step, hidden rows hpg={hpg} d_v={d_v} S={S}")
+    o, lse = step(x, S)
+    assert bool((o[1] == 0).all()) and bool(torch.isneginf(lse[1]).all())
+    for b in (0, 2):                                     # equal scores: the mean of the rows that count
+        live = ~rows[:int(x["lens"][b])]
+        mean = x["v"][b, :, :int(x["lens"][b])][:, live].mean(1).repeat_interleave(hpg, 0)
+        # the keys of a sequence are alike, so the weights are alike: only the
+        # sums (fp32) and the weights' two parts (2^-17) are rounded
+        assert float((o[b].cpu().double() - mean).abs().max()) <= 6 * 2.0 ** -16
+    w = torch.zeros(3, T, device="cuda")
+    gva.accumulate_weights(x["d"], x["q"][:, 0].contiguous().cuda(), x["m"].cuda(), x["vc"], x["kc"], x["lens"].cuda(), lse, w,
+                           v4_scale=x["sc"], seen=x["seen"].cuda())
+    assert bool((w[:, rows.cuda()] == 0).all()) and bool((w[1] == 0).all())
+    for b in (0, 2):
+        live = ~rows[:int(x["lens"][b])]
+        got = w[b, :int(x["lens"][b])][live.cuda()].cpu().double()
+        # a score near -21 (-30 in log2) and a log-sum-exp as large, each an fp32 number
+        assert float((got * int(live.sum()) / (2 * hpg) - 1).abs().max()) <= 40 * 2.0 ** -22
 
 
 @gpu
