@@ -171,7 +171,10 @@ struct Q4DecodeParams {
 
 template <int HPG, int DV, int NRC, int NW>
 struct Q4Cfg {
-  static constexpr int DEPTH = NW > kWaves ? 2 : 3, OCC = 2;   // tiles in registers; waves per SIMD at least
+  // tiles in registers (two leave room for a third workgroup of four waves on a CU
+  // at d_v = 128: B64 to 8K rows H32 G8, chunks of 2560, 35.5 -> 29.6 us); waves
+  // per SIMD at least
+  static constexpr int DEPTH = NW > kWaves || DV == 128 ? 2 : 3, OCC = 2;
   // absorption: loads of four map rows (of 128 columns) per round, so that the
   // heads' maps are one round over the waves where registers allow it
   static constexpr int AR0 = DV * HPG / (4 * NW);
@@ -602,9 +605,8 @@ Q4DecodeFn pick_q4_decode(int hpg, int dv, int nrc, int nw, bool fused) {
   return nullptr;
 }
 
-// Workgroups of eight waves that a CU holds at once (registers; two of four
-// waves at d_v = 128, three at 64, by the same).
-inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) : (d_v == 128 ? 2 : 3); }
+// Workgroups that a CU holds at once, by their registers.
+inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) : 3; }
 
 // Waves per workgroup: eight while the workgroups are resident at once; with
 // bounded chunks (whose empty splits count among them) while a chunk is long and
@@ -646,11 +648,12 @@ struct Q4Cost {
     }
     const long long here = (items + n_cu - 1) / n_cu;
     const long long resident = here < 1 ? 1 : (here > most ? most : here);
-    const double pace = (d_v == 128 ? 290.0 : 500.0) * (resident * nw >= 8 ? 1.0 : 0.68);   // rows per us and CU
-    const double mean = (double)rows / n_cu / pace, last = (double)longest * resident / pace;
+    const double pace = d_v == 128 ? 290.0 : 500.0;      // rows per us of a CU with eight waves or more, 0.68 with four
+    const double mean = (double)rows / n_cu / (pace * (resident * nw >= 8 ? 1.0 : 0.68));
+    // the longest chunk, whose neighbours on the CU end before it
+    const double last = (double)longest / (pace * (nw == 8 ? 1.0 : 0.68)) * (1.0 + 0.35 * (double)(resident - 1));
     const double rounds = (double)items / ((double)n_cu * most);
-    double t = rounds <= 1.0 ? 7.0 + (last > mean ? last : mean)
-                             : 7.0 * (1.0 + (rounds - 1.0) / most) + mean + last / 2;
+    double t = rounds <= 1.0 ? 7.0 + (last > mean ? last : mean) : 7.0 + 4.0 * (rounds - 1.0) + mean + last / 2;
     const double idle = (double)(decode_grid(d, S, c) - items) / ((double)n_cu * most);      // empty splits
     return t + (idle > 0 ? idle * 1.2 : 0.0) + (S > 1 ? 4.5 + 0.05 * S + (S > 16 ? 3.0 : 0.0) : 0.0);
   }
