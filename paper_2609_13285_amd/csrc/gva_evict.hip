@@ -519,9 +519,22 @@ __device__ __forceinline__ void evict_block_rows(const EvictParams& p, int b, in
   evict_rows(p, b, t0, min(blk < p.low ? min(t0 + kEvictBlock, p.keep) : t0 + kEvictBlock, L), L, r);
 }
 
+// The sum over the lanes up to this one, by shifts within 16 lanes and then the
+// row's and the half's last lane broadcast to those behind (wave_incl_scan goes
+// through LDS six times).
+__device__ __forceinline__ int lane_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);    // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast 15 to rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast 31 to rows 2 and 3
+  return v;
+}
+
 // Sums over the workgroup, each thread receiving those of the threads before it.
 __device__ __forceinline__ int block_before(int v, int* wave_n) {
-  const int incl = wave_incl_scan(v);
+  const int incl = lane_scan(v);
   __syncthreads();                             // wave_n may still be read
   if ((threadIdx.x & 63) == 63) wave_n[threadIdx.x >> 6] = incl;
   __syncthreads();
@@ -530,9 +543,9 @@ __device__ __forceinline__ int block_before(int v, int* wave_n) {
   return before;
 }
 __device__ __forceinline__ int block_sum(int v, int* wave_n) {
-  const int s = wave_sum_int(v);
+  const int s = lane_scan(v);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = s;
+  if ((threadIdx.x & 63) == 63) wave_n[threadIdx.x >> 6] = s;
   __syncthreads();
   int sum = 0;
   for (int i = 0; i < kEvictWaves; ++i) sum += wave_n[i];
@@ -726,7 +739,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
 template <int N>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
   __shared__ __attribute__((aligned(16))) int hist[1 << kDigit0];
-  __shared__ int wave_n[kEvictWaves], picked[2];
+  __shared__ int wave_n[5][kEvictWaves], picked[2];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int L = clamp_len(p.lens, b, p.t_max), K = p.keep;
   const int64_t base = (int64_t)b * p.t_max;
@@ -744,33 +757,52 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     for (int i = 0; i < N; ++i) store(i, r.in[i] ? r.weight[i] : 0.f, r.in[i] ? r.pos[i] : -1);
     return;
   }
+  // (every sum over the waves has a row of wave_n of its own, and the counters of
+  // a digit are cleared while the digit before is being settled: three barriers a
+  // digit)
+  auto before_waves = [&](int row, int incl, int own) {
+    if (lane == 63) wave_n[row][tid >> 6] = incl;
+    __syncthreads();
+    int before = incl - own;
+    for (int i = 0; i < (tid >> 6); ++i) before += wave_n[row][i];
+    return before;
+  };
   unsigned border = 0u;
   int rest = K;
 #pragma unroll
+  for (int k = 0; k < 4; ++k) hist[tid + k * kEvictThreads] = 0;
+  __syncthreads();
+#pragma unroll
   for (int digit = 0; digit < 3; ++digit) {
     const int bits = digit == 0 ? kDigit0 : kDigit12, shift = digit == 0 ? 20 : (digit == 1 ? 10 : 0);
-    const int per = digit == 0 ? 4 : 1;
-#pragma unroll
-    for (int k = 0; k < per; ++k) hist[tid + k * kEvictThreads] = 0;
-    __syncthreads();
+    constexpr int kMost = (1 << kDigit0) / kEvictThreads;
+    const int per = digit == 0 ? kMost : 1;    // counters a thread holds
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const unsigned x = r.key[i] >> shift;
       if (r.in[i] && (digit == 0 || x >> bits == border)) atomicAdd(&hist[x & ((1u << bits) - 1u)], 1);
     }
     __syncthreads();
-    int bin;
     const int top = (1 << bits) - 1 - per * tid;
-    if (digit == 0) {
-      int c[4];
+    int c[kMost], sum = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) c[k] = hist[top - k];
-      pick_digit(c, top, rest, bin, wave_n, picked);
-    } else {
-      const int c[1] = {hist[top]};
-      pick_digit(c, top, rest, bin, wave_n, picked);
+    for (int k = 0; k < per; ++k) {
+      c[k] = hist[top - k];
+      sum += c[k];
     }
-    border = border << bits | (unsigned)bin;
+    int above = before_waves(digit, lane_scan(sum), sum);
+#pragma unroll
+    for (int k = 0; k < per; ++k) {
+      if (above < rest && rest <= above + c[k]) {
+        picked[0] = top - k;
+        picked[1] = rest - above;
+      }
+      above += c[k];
+    }
+    if (digit < 2) hist[tid] = 0;              // the next digits have 1024 counters
+    __syncthreads();
+    border = border << bits | (unsigned)picked[0];
+    rest = picked[1];
   }
   // rows above the border stay, and the first `rest` of those on it
   const unsigned long long below = (1ull << lane) - 1ull;
@@ -781,7 +813,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     on[i] = __ballot(r.in[i] && r.key[i] == border);
     n_on += __popcll(on[i]);
   }
-  int at_eq = __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_on : 0, wave_n));
+  // (a wave's numbers are uniform: its sum up to lane 63 is its own number)
+  int at_eq = __builtin_amdgcn_readfirstlane(before_waves(3, n_on, n_on));
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     stay[i] = __ballot(r.in[i] && (r.key[i] > border || (r.key[i] == border && at_eq + __popcll(on[i] & below) < rest)));
@@ -790,7 +823,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     n_move += __popcll(stay[i] & __ballot(r.t[i] >= K));
   }
   // both numbers in one scan (each below 2^14)
-  const int both = __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_hole << 16 | n_move : 0, wave_n));
+  const int mine = n_hole << 16 | n_move;
+  const int both = __builtin_amdgcn_readfirstlane(before_waves(4, mine, mine));
   int hole = both >> 16, move = both & 0xFFFF;
   if (tid == kEvictThreads - 1) p.count[b] = move + n_move;
 #pragma unroll
