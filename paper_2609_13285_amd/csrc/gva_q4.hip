@@ -464,31 +464,57 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     // Each of a head's two lanes takes the sum of the parts, and the exponential,
     // for one half of the rows: the high column's lane the first 16.
     float x[4];
+    auto take_scores = [&]() {                   // and the largest of the lane's
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = (is_lo ? sc[1][j] : sc[0][j]) + mirror<HPG>(is_lo ? sc[0][j] : sc[1][j]);
-    if (tail) {
-      __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < 4; ++j) x[j] = (is_lo ? sc[1][j] : sc[0][j]) + mirror<HPG>(is_lo ? sc[0][j] : sc[1][j]);
+      if (tail) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (row0 + (is_lo ? 16 : 0) + 4 * qd + j >= r1) x[j] = -INFINITY;
-      __builtin_amdgcn_sched_barrier(0);
-    }
+        for (int j = 0; j < 4; ++j)
+          if (row0 + (is_lo ? 16 : 0) + 4 * qd + j >= r1) x[j] = -INFINITY;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return max3(max3(x[0], x[1], x[2]), x[3], x[3]);
+    };
     // The scores come less the running maximum (the products start from it), which
     // moves only when a column's score passes it by 8 (log2), or its first one
     // comes: until then weights stay below 2^8, and most tiles need neither the
     // maximum over the lanes nor the rescaling.
-    const float mt = max3(max3(x[0], x[1], x[2]), x[3], x[3]);
+    const float mt = take_scores();
     if (__ballot(mt > m_limit) != 0) {
       const float top = max_over_rows(fmaxf(mt, mirror<HPG>(mt)));
-      const bool moves = top > m_limit;
-      const float by = moves ? top : 0.f;
-      const float alpha = moves && m_limit != -INFINITY ? __builtin_amdgcn_exp2f(-by) : 1.f;
+      const bool moves = top > m_limit, some = m_limit != -INFINITY;
+      float by = moves ? top : 0.f, next = m_run + by;
+      if (__ballot(moves && some && top > 64.f) == 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] -= by;
+      } else {
+        // Started from a maximum far below them, scores have lost what tells them
+        // apart (all of it, where the rows before were hidden by the lowest value
+        // of a type): they are taken again, from 0.
+        sc[0] = sc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int rc = 0; rc < NRC; ++rc)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+            sc[hf] = mfma16(as_bf16x8(__builtin_amdgcn_raw_buffer_load_b128(kres, k_lane[rc], (row0 + 16 * hf) * a.d_r * 2, 0)), bk[rc], sc[hf]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+            sc[hf] = mfma16(*reinterpret_cast<const bf16x8*>(tr_put + 16 * hf * PITCH + 16 * c), bq[c], sc[hf]);
+        const float most = take_scores();
+        const float again = max_over_rows(fmaxf(most, mirror<HPG>(most)));
+        next = moves ? again : m_run;
+        by = next - m_run;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] -= next;
+      }
+      const float alpha = moves && some ? __builtin_amdgcn_exp2f(-by) : 1.f;
       l_run *= alpha;
 #pragma unroll
       for (int ib = 0; ib < NB; ++ib) acc[ib] *= alpha;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] -= by;
-      m_run += by;
+      m_run = next;
       m_limit = moves ? 8.f : m_limit;
       const float s0 = is_lo ? 0.f : -m_run;
       start = f32x4{s0, s0, s0, s0};

@@ -345,14 +345,16 @@ def step(x, S=1, rows=0, stream=None):
     return o, lse
 
 
-def check_step(x, o, lse):
+def check_step(x, o, lse, size=None):
     """The query and the weights are kept as bf16 high + low parts, each off by
     at most 2^-18 of its size (two roundings of half a step, 2^-9, one after the
     other); sums are fp32 over d_v + d_r terms.  So a score is off by at most
     A (2^-18 + 256 * 2^-24), A its sum of magnitudes (log2(e) and the scale cost
     a few 2^-24 more), the weights by e^(2 |dx|) - 1 and 2^-17, and o by that
-    times the largest value of its sequence."""
-    sc, size = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], x["G"])
+    times the largest value of its sequence.  size: the sums of magnitudes, where
+    some rows' need not be counted."""
+    sc, every = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], x["G"])
+    size = every if size is None else size
     ro, rl = ref.attend(sc, x["v"], x["G"])
     ro, rl = ro[:, 0], rl[:, 0]
     o, lse = o.cpu().double(), lse.cpu().double()
@@ -449,6 +451,32 @@ def test_step_hidden_rows(hpg, d_v, S):
         got = w[b, :int(x["lens"][b])][live.cuda()].cpu().double()
         # a score near -21 (-30 in log2) and a log-sum-exp as large, each an fp32 number
         assert float((got * int(live.sum()) / (2 * hpg) - 1).abs().max()) <= 40 * 2.0 ** -22
+
+
+@gpu
+@pytest.mark.parametrize("hpg,d_v,S", [(4, 128, 1), (8, 64, 1), (1, 128, 2)])
+@pytest.mark.parametrize("low", [float(torch.finfo(torch.bfloat16).min), -1e30, -1e6])
+def test_step_scores_far_above_those_before(hpg, d_v, S, low):
+    """Every wave begins with tiles of finite scores far below the others', and
+    those rise (or fall) by hundreds twice more: a score that counts is off by
+    what its own terms allow, not by what the rows before it do."""
+    T = 1024
+    d = dims(batch=2, n_heads=2 * hpg, n_groups=2, d_v=d_v, d_c=64, d_r=16, t_max=T)
+    x = problem(2, T, 2 * hpg, 2, d_v, 64, 16, [T, 777], seed=hpg, q_std=6.0)
+    rows = torch.randn(2, 2, T, d_v, generator=torch.Generator().manual_seed(1))
+    rows[:, :, 512:, 0] = 300.0
+    rows[:, :, 768:, 0] = 900.0
+    code, byte = ref.quantize(rows.to(d.torch_dtype))
+    x["v"] = ref.values(code, byte)
+    x["vc"], x["sc"] = (u.cuda() for u in ref.pack(code, byte))
+    x["q"][..., -2:] = torch.tensor([0.5, 0.0])          # the slowest pair: hardly turned at these positions
+    counts = x["kr"].clone()
+    counts[:, :256, -2] = 0.0
+    x["kr"][:, :256, -2] = torch.tensor(low).to(torch.bfloat16).double()
+    x["kc"] = gva.tiled(x["kr"].to(torch.bfloat16)).cuda()
+    _, size = ref.scores(x["q"], x["m"], x["v"], counts, x["lens"], x["seen"], x["G"])
+    note(f"q4 step, rising scores hpg={hpg} d_v={d_v} S={S} low={low}")
+    check_step(x, *step(x, S), size=size)
 
 
 @gpu
