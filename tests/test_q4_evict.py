@@ -796,6 +796,148 @@ def test_generation_with_eviction(cache):
 
 
 @gpu
+@pytest.mark.parametrize("cache,T,N", [("q4", 320, 1), ("q4", 9280, 3), ("bf16", 320, 3), ("bf16", 9280, 1), ("f32", 320, 2)])
+def test_calls_streams_graph_and_guards(cache, T, N):
+    """Append, weights, eviction and (4 bits) unpack: on a side stream, and
+    captured together and replayed with eager work between; nothing written
+    outside the outputs."""
+    B, G, dv, dr = 3, 2, 64, 16
+    x = problem(B, T, 8, G, dv, 64, dr, [T - 1, 17, T // 2], N=N, cache=cache, seed=9)
+    d, dt = x["d"], x["d"].torch_dtype
+    pad, guards = 1024, []
+
+    def buffer(shape, dtype, value):
+        n = math.prod(shape)
+        raw = torch.full((pad + n + pad,), value, dtype=dtype, device="cuda")
+        guards.append((raw, n, value))
+        return raw[pad:pad + n].view(shape)
+
+    note(f"append, weights, eviction: streams, graph, guards, {cache} T={T} N={N}")
+    start = [u for u in (x["vc"], x["sc"], x["kc"]) if u is not None]
+    held = [buffer(u.shape, u.dtype, 5) for u in start]
+    vc, kc, sc = held[0], held[-1], held[1] if cache == "q4" else None
+    g = torch.Generator().manual_seed(3)
+    v, kn = torch.randn(B, G, dv, generator=g).to(dt).cuda(), torch.randn(B, dr, generator=g).to(dt).cuda()
+    seq = torch.arange(B, dtype=torch.int32, device="cuda")
+    row, lens = x["lens"].cuda(), x["lens"].cuda() + 1
+    pos, seen = row + 7, lens + 7
+    q, m = x["q"].cuda(), x["m"].cuda()
+    lse = torch.full((B, N, 8), 9.0, device="cuda")
+    w0 = torch.rand(B, T, generator=g).cuda()
+    rp0 = torch.arange(T, dtype=torch.int32, device="cuda").expand(B, T).contiguous()
+    rp, rp1 = buffer((B, T), torch.int32, 5), buffer((B, T), torch.int32, 5)
+    w, w1 = buffer((B, T), torch.float32, 5), buffer((B, T), torch.float32, 5)
+    new_l = buffer((B,), torch.int32, 5)
+    wsw = buffer((gva.gva_weights_workspace_size(d, N),), torch.uint8, 5)
+    wse = buffer((gva.gva_evict_workspace_size(d),), torch.uint8, 5)
+    flat = buffer((B, G, T, dv), torch.bfloat16, 5) if cache == "q4" else None
+    outs = held + [rp, rp1, w, w1, new_l] + ([flat] if flat is not None else [])
+
+    def reset():
+        for to, of in zip(held + [rp, w], start + [rp0, w0]):
+            to.copy_(of)
+        for u in (rp1, w1, new_l, flat):
+            if u is not None:
+                u.fill_(3)
+        for u in (wsw, wse):
+            u.fill_(0x77)
+
+    def calls(stream=None):
+        if cache == "q4":
+            gva.gva_q4_append_kv(d, vc, sc, kc, v, kn, seq, row, pos=pos, row_pos=rp, stream=stream)
+        else:
+            gva.gva_append_rows(d, vc, kc, v, kn, seq, row, pos=pos, row_pos=rp, stream=stream)
+        gva.gva_accumulate_weights(d, N, q, m, vc, sc, kc, lens, lse, w, w, workspace=wsw, seen=seen, decay=0.5, stream=stream)
+        gva.gva_evict_rows(d, T // 3, 2, 9, vc, sc, kc, lens, w, new_l, w1, workspace=wse, seen=seen, row_pos=rp,
+                           new_row_pos=rp1, stream=stream)
+        if flat is not None:
+            gva.gva_q4_unpack_kv(d, vc, sc, new_l, flat, stream=stream)
+
+    def same(want):
+        return all(torch.equal(u.view(torch.uint8), y) for u, y in zip(outs, want))
+
+    reset()
+    calls()
+    torch.cuda.synchronize()
+    want = [u.view(torch.uint8).clone() for u in outs]
+    assert new_l.tolist() == [T // 3, 18, T // 3]
+    side = torch.cuda.Stream()
+    reset()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    side.synchronize()
+    assert same(want)
+    reset()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(4):
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(want)
+        reset()
+        calls()
+        torch.cuda.synchronize()
+        assert same(want)
+    for raw, n, value in guards:
+        assert bool((raw[:pad] == value).all()) and bool((raw[pad + n:] == value).all())
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16"])
+def test_caches_past_two_gigabytes(cache):
+    """The last stream of a cache whose offsets pass 32 bits: append, weights,
+    eviction, unpack."""
+    G, dv = 9, 128
+    T = 1 << 20 if cache == "bf16" else 1 << 22
+    d = dims(batch=1, n_heads=G, n_groups=G, d_v=dv, d_c=32, d_r=0, t_max=T)
+    note(f"large cache {cache} T={T}")
+    if cache == "q4":
+        vc, sc = gva.q4_cache(d)
+        sc.fill_(127)
+    else:
+        vc, sc = torch.zeros(1, G, T, dv, dtype=torch.bfloat16, device="cuda"), None
+    assert vc.numel() * vc.element_size() > 1 << 31
+    rows = torch.tensor([T - 1, T - 3, 5], dtype=torch.int32, device="cuda")
+    v = torch.zeros(3, G, dv, dtype=torch.bfloat16, device="cuda")
+    v[:, -1] = 2.0                                       # in the last group only
+    rp = torch.arange(T, dtype=torch.int32, device="cuda").view(1, T)
+    if cache == "q4":
+        gva.gva_q4_append_kv(d, vc, sc, None, v, None, torch.zeros_like(rows), rows)
+    else:
+        gva.gva_append_rows(d, vc, None, v, None, torch.zeros_like(rows), rows)
+    q = torch.zeros(1, G, 32, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    m = torch.zeros(G, dv, 32, dtype=torch.bfloat16, device="cuda")
+    m[..., 0] = 0.125
+    lens = torch.tensor([T], dtype=torch.int32, device="cuda")
+    w = torch.zeros(1, T, device="cuda")
+    gva.accumulate_weights(d, q, m, vc, None, lens, torch.full((1, G), 8.0, device="cuda"), w, v4_scale=sc)
+    x = 0.125 * 2.0 * dv / math.sqrt(32)                 # the score of the three rows in the last group
+    low = G * math.exp(-8.0)
+    high = low - math.exp(-8.0) + math.exp(x - 8.0)
+    want = torch.full((1, T), low, dtype=torch.float64)
+    want[0, rows.cpu().long()] = high
+    # score and log-sum-exp up to 8 in fp32 and bf16 parts: 16 * 2^-18, sums 2^-20
+    assert float((w.cpu().double() / want - 1).abs().max()) <= 2.0 ** -13
+    new_l, new_w, new_p = gva.evict(d, 4, vc, None, lens, w, v4_scale=sc, row_pos=rp)
+    # kept: the three, and row 0, the first of those alike
+    assert int(new_l) == 4 and set(new_p[0, :4].tolist()) == {0, 5, T - 3, T - 1}
+    if cache == "q4":
+        flat = torch.empty(1, G, T, dv, dtype=torch.bfloat16, device="cuda")
+        gva.gva_q4_unpack_kv(d, vc, sc, new_l, flat)
+    else:
+        flat = vc
+    # rows 0 .. 15 of the last stream, tiled in pieces of 8 columns
+    last = flat[0, -1].reshape(-1)[:16 * dv].view(dv // 8, 16, 8).transpose(0, 1).reshape(16, dv)[:4]
+    for t in range(4):
+        assert bool((last[t] == (0.0 if int(new_p[0, t]) == 0 else 2.0)).all())
+
+
+@gpu
 def test_prompt_over_a_4_bit_cache():
     """Append a prompt, unpack, prefill; then the step at its last token agrees
     with the prompt's last row."""
