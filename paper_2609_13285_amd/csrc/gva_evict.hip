@@ -122,6 +122,8 @@ struct WeightStream {
 // that every exponential is taken once.  A wave's sums over the heads go to its
 // group's array of row sums, which are added in order at the end: the result
 // does not depend on timing.  The log-sum-exp is the products' initial value.
+// Bound by HBM: B32 T8K H32 G8 d 128/16 in 4 bits (154 MB) 28.2 us, 5.5 TB/s, and
+// 4.6 before it for the absorbed queries.
 template <int HPG, int DV, int NRC, bool Q4>
 __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) weights_step_kernel(WeightParams p) {
   using Stream = WeightStream<DV, NRC, Q4>;
@@ -226,7 +228,10 @@ __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) wei
 // head) pair, its query once as bf16 high parts and once as low parts into the
 // same sums, 32 columns a wave.  The waves are dealt first over the columns and
 // then over the tiles.  Sums over the columns go through LDS in a fixed order to
-// the group's row sums in the workspace, which weights_join_kernel adds up.
+// the group's row sums in the workspace, which weights_join_kernel adds up.  Bound
+// by latency at ordinary sizes (the queries, then a tile at a time): 32 queries on
+// B2 of 4K to 8K rows, H32 G8 d 128/16 bf16 (27 MB), 18.7 us, and 5 and 4 for the
+// absorption before and the join behind it.
 constexpr int kWindowRows = 512, kWindowCols = 32;   // most rows of a workgroup; columns of a wave
 
 template <int DV, int NRC, bool Q4>
@@ -344,7 +349,8 @@ __global__ void __launch_bounds__(kThreads) weights_join_kernel(WeightParams p) 
 }
 
 // fp32 storage: the same on the fp32 products, 16-row tiles, any d_v and d_r
-// that the tiled layout takes.
+// that the tiled layout takes.  Bound by the products and their loads' latency: a
+// checking path, not a serving one.
 __global__ void __launch_bounds__(64 * kWeightWaves) weights_f32_kernel(WeightParams p) {
   __shared__ float sums[kWeightWaves][kWeightChunk];
   const int nchunks = (p.t_max + p.chunk - 1) / p.chunk;
@@ -486,7 +492,8 @@ __device__ __forceinline__ unsigned evict_key(const EvictParams& p, int pos, flo
 // the first takes in the exponent and three bits more, so that keys of like weight
 // spread over many counters): every block counts its own keys, and the next launch
 // adds up the blocks' counters, each workgroup for itself.  The fourth numbers the
-// rows.  No counter is shared, so nothing has to be cleared.
+// rows.  No counter is shared, so nothing has to be cleared.  Bound by latency: four
+// sequences of 32K rows 4.7, 4.7, 4.8 and 7.2 us.
 template <int N>
 struct EvictRows {
   int t[N];
@@ -734,8 +741,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
 }
 
 // The whole selection of a sequence in one workgroup, N rows a thread: up to 8K
-// rows it takes less than the four launches above (4K rows, B = 32: 13 us against
-// 23; 32K rows, whose keys do not fit the registers beside the rest: 84 against 23).
+// rows it takes less than the four launches above (4K rows, B = 32: 10 us against
+// 21; 32K rows, whose keys do not fit the registers beside the rest: 84 against 21).
 template <int N>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
   __shared__ __attribute__((aligned(16))) int hist[1 << kDigit0];
@@ -861,7 +868,11 @@ struct MoveParams {
 // written and the moves need no order.  A wave takes 16 moves of one stream and
 // 16 of its 16-byte pieces, lane (n, qd) pieces qd, qd + 4, ... of move n, all
 // requested before the first is stored: moves next to each other come from, and
-// go to, nearby rows of a tile, whose pieces lie side by side.
+// go to, nearby rows of a tile, whose pieces lie side by side.  Half the rows of
+// four sequences of 32K go (G8 d 128/24 bf16): 85 us for 139 MB read and written,
+// but every line below the budget is rewritten in part, and so read too, and every
+// line behind it read: 410 MB, 78 us at a copy's pace (whole tiles written from
+// LDS took 77 us and a map of the moves more).
 template <bool Q4>
 __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
   const int b = blockIdx.z, nseg = Q4 ? 1 : (p.v_pieces + 15) / 16;

@@ -45,7 +45,9 @@ struct Q4AppendParams {
 // A wave takes one group's values of the rows of one 1 KB block, a lane one
 // scale block (32 columns) of a row: rows at consecutive places of a stream are
 // then stored as whole blocks.  The positional pairs, an fp64 rotation each,
-// have workgroups of their own.
+// have workgroups of their own.  A few rows are bound by the launch (8 rows of
+// G4 d 64: 2.5 us), a prompt by HBM: 8192 rows of G8 d 128/16 (43 MB) in 6.7 us,
+// 6.4 TB/s.
 template <int DV>
 __global__ void __launch_bounds__(kThreads) q4_append_kernel(Q4AppendParams p) {
   constexpr int R = block_rows(DV), NS = DV / kScaleCols;
@@ -214,6 +216,16 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // absorbed query (and its softmax weights) as bf16 high and low parts, and with
 // FUSED the workgroup absorbs its heads' queries itself while its first tiles
 // are on their way.
+//
+// A tile is converted once, in the score products' operand order, and goes
+// through the wave's LDS for the transposed operand of P.V, a tile later.  That
+// bounds the loop: 8 KB written and 8 KB read a tile at d_v = 128 are 176 cycles
+// of a CU's LDS, 3/4 of the loop's time, beside 135 of vector work, 77 of matrix
+// products and 177 of HBM's share (V^T by products with an identity, which need
+// no LDS, take as long in the matrix cores: 16 more of them a tile).
+// B32 T8K H32 G8 d 128/16 (153 MB): 35.8 us, 4.3 TB/s, of which about 7.5 are the
+// start, the absorption and the end; B4 of 64K to 128K rows (240 MB) 50 and 5 for
+// the combine, 4.8 TB/s in the loop.
 template <int HPG, int DV, int NRC, int NW, bool FUSED>
 __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_decode_kernel(GVA_Q4_HEAD_ARGS,
                                                                                             Q4DecodeParams p) {
@@ -636,10 +648,11 @@ inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) 
 
 // Waves per workgroup: eight while the workgroups are resident at once; with
 // bounded chunks (whose empty splits count among them) while a chunk is long and
-// the streams are no more than the CUs (us per step, eight and four waves: B32 T8K H32 G8 d 128, 256 workgroups, 35.4
-// and 43.1; B64 T2K, 512, 28.0 and 23.5; B4 of 64K to 128K rows, chunks of 13024,
-// 54.8 and 67.4; B64 to 32K rows, H16 G2, chunks of 4096 30.0 and 33.0, of 2048
-// 39.2 and 30.5; B64 to 8K rows, G8, chunks of 4096 41.4 and 30.8).
+// the streams are no more than the CUs.  us per step, eight and four waves: B32
+// T8K H32 G8 d 128, 256 workgroups, 35.4 and 43.1; B64 T2K, 512, 28.0 and 23.5; B4
+// of 64K to 128K rows, chunks of 13024, 54.8 and 67.4; B64 to 32K rows, H16 G2,
+// chunks of 4096 30.0 and 33.0, of 2048 39.2 and 30.5; B64 to 8K rows, G8, chunks
+// of 4096 41.4 and 30.8.
 int q4_waves(const gva_dims* d, int num_splits, int split_rows, int n_cu) {
   if (split_rows > 0) return split_rows >= 4096 && (long long)d->batch * d->n_groups <= n_cu ? 8 : kWaves;
   return decode_grid(d, num_splits, 0) <= (long long)n_cu * q4_resident(d->d_v, 8) ? 8 : kWaves;
