@@ -229,9 +229,10 @@ __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) wei
 // same sums, 32 columns a wave.  The waves are dealt first over the columns and
 // then over the tiles.  Sums over the columns go through LDS in a fixed order to
 // the group's row sums in the workspace, which weights_join_kernel adds up.  Bound
-// by latency at ordinary sizes (the queries, then a tile at a time): 32 queries on
-// B2 of 4K to 8K rows, H32 G8 d 128/16 bf16 (27 MB), 18.7 us, and 5 and 4 for the
-// absorption before and the join behind it.
+// by the matrix products (twice the algorithm's, for the low parts) where there
+// are many rows, 32 queries on B8 T16K H32 G8 d 128/16 bf16 in 100 us, 0.77
+// PFLOP/s of them, and by latency where there are few: B2 of 4K to 8K rows 18.7 us,
+// and 5 and 4 for the absorption before and the join behind it.
 constexpr int kWindowRows = 512, kWindowCols = 32;   // most rows of a workgroup; columns of a wave
 
 template <int DV, int NRC, bool Q4>

@@ -11,7 +11,7 @@
 // value is exactly a bf16: codes have two significant bits, and the bounds on e
 // keep 0.5 * 2^e normal and 6 * 2^e finite.
 // A row takes 4.25 bits an element, 576 B at G = 8, d_v = 128, d_r = 16 against
-// 2080 B in bf16 (the positional key, 1/16 of a bf16 row, stays bf16).
+// 2080 B in bf16 (the positional key, 1/65 of a bf16 row, stays bf16).
 //
 // Layout.  Codes in blocks of 1 KB, which a wave reads as 16 bytes a lane: lane
 // (n, p) = (lane % 16, lane / 16) receives piece p, d_v / 4 columns, of row n
@@ -46,8 +46,8 @@ struct Q4AppendParams {
 // scale block (32 columns) of a row: rows at consecutive places of a stream are
 // then stored as whole blocks.  The positional pairs, an fp64 rotation each,
 // have workgroups of their own.  A few rows are bound by the launch (8 rows of
-// G4 d 64: 2.5 us), a prompt by HBM: 8192 rows of G8 d 128/16 (43 MB) in 6.7 us,
-// 6.4 TB/s.
+// G4 d 64: 2.5 us), a prompt by that and HBM: 8192 rows of G8 d 128/16 (22 MB) in
+// 6.7 us, 3.3 TB/s.
 template <int DV>
 __global__ void __launch_bounds__(kThreads) q4_append_kernel(Q4AppendParams p) {
   constexpr int R = block_rows(DV), NS = DV / kScaleCols;
