@@ -590,7 +590,13 @@ int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, c
  * weights and positions.  new_weights (and new_row_pos) are written whole: 0
  * (-1) from new_lens[b] on.  Cache rows from new_lens[b] on keep what they
  * held, and lens, weights and row_pos are not written: the call can be repeated.
- * new_lens, new_weights and new_row_pos must not overlap their counterparts;
+ * After an eviction new rows go in by gva_append_rows or gva_q4_append_kv, and a
+ * query is rotated at its token's position, seen[b] - 1: gva_q4_decode_step takes
+ * seen; on a bf16 or fp32 cache gva_absorb_query with seen for its lens (and a
+ * t_max of at least that), then gva_decode_attention on q_abs and q_rot
+ * (gva_decode_step and an absorption inside the attention rotate at lens[b] - 1).
+ * new_lens, new_weights and new_row_pos must not overlap their counterparts, nor
+ * new_lens seen;
  * row_pos and new_row_pos come together (NULL: position = row, as long as
  * nothing has been evicted).  v_cache, v4_scale as for gva_accumulate_weights;
  * every shape that the tiled layout (or the 4-bit one) takes, batch <= 65535.

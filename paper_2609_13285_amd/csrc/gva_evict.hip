@@ -871,9 +871,9 @@ struct MoveParams {
 // requested before the first is stored: moves next to each other come from, and
 // go to, nearby rows of a tile, whose pieces lie side by side.  Half the rows of
 // four sequences of 32K go (G8 d 128/24 bf16): 85 us for 139 MB read and written,
-// but every line below the budget is rewritten in part, and so read too, and every
-// line behind it read: 410 MB, 78 us at a copy's pace (whole tiles written from
-// LDS took 77 us and a map of the moves more).
+// but every line below the budget is rewritten in part and every line behind it
+// read: with the former read too 410 MB, 78 us at a copy's pace (whole tiles read,
+// filled in LDS and written took 77 us, and a map of the moves more).
 template <bool Q4>
 __global__ void __launch_bounds__(kThreads) evict_move_kernel(MoveParams p) {
   const int b = blockIdx.z, nseg = Q4 ? 1 : (p.v_pieces + 15) / 16;
@@ -1051,7 +1051,7 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
       !aligned(row_pos, 4) || !aligned(new_lens, 4) || !aligned(new_weights, 4) || !aligned(new_row_pos, 4) ||
       (dims->d_r > 0 && !aligned(kr_cache, 16)))
     return GVA_ERR_INVALID_ARG;
-  if (new_lens == lens || new_weights == weights || (row_pos != nullptr && new_row_pos == row_pos))
+  if (new_lens == lens || new_lens == seen || new_weights == weights || (row_pos != nullptr && new_row_pos == row_pos))
     return GVA_ERR_INVALID_ARG;
   if (workspace == nullptr || workspace_bytes < L.bytes || !aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
   const bool q4 = v4_scale != nullptr;

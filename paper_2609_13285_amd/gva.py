@@ -1030,7 +1030,9 @@ def gva_evict_rows(dims: GvaDims, n_keep: int, n_first: int, n_recent: int, v_ca
 def evict(dims: GvaDims, n_keep: int, v_cache, kr_cache, lens, weights, n_first: int = 0, n_recent: int = 0,
           v4_scale=None, seen=None, row_pos=None, stream=None):
     """gva_evict_rows; returns (lens, weights, row_pos) as they are afterwards
-    (row_pos None where none is given)."""
+    (row_pos None where none is given).  From then on queries are rotated at
+    their token's position, ``seen - 1``: q4_decode takes seen, on other caches
+    gva_absorb_query takes it for its lens, before gva_decode_attention."""
     d = dims
     out = torch.empty_like(lens), torch.empty_like(weights), None if row_pos is None else torch.empty_like(row_pos)
     ws = evict_workspace_for(d, v_cache.device)

@@ -142,7 +142,7 @@ def test_evict_refusals():
     for d, s in ((dims(), None), (dims(), A), (dims(dtype="f32"), None)):
         for kw in (dict(keep=0), dict(keep=-1), dict(first=-1), dict(recent=-1), dict(first=9, recent=8), dict(v=None),
                    dict(k=None), dict(lens=None), dict(w=None), dict(nl=None), dict(nw=None), dict(rp=A), dict(nrp=A),
-                   dict(nl=A), dict(nw=A), dict(rp=A, nrp=A), dict(v=A + 8), dict(nl=A + 2), dict(ws=None), dict(ws=A + 64),
+                   dict(nl=A), dict(seen=A + 256), dict(nw=A), dict(rp=A, nrp=A), dict(v=A + 8), dict(nl=A + 2), dict(ws=None), dict(ws=A + 64),
                    dict(n=16)):
             assert evict_status(d, s=s, **kw) == gva.GVA_ERR_INVALID_ARG, kw
     assert evict_status(dims(dtype="f32"), s=A) == gva.GVA_ERR_UNSUPPORTED
