@@ -540,34 +540,41 @@ __device__ __forceinline__ int lane_scan(int v) {
   return v;
 }
 
-// Sums over the workgroup, each thread receiving those of the threads before it.
-__device__ __forceinline__ int block_before(int v, int* wave_n) {
-  const int incl = lane_scan(v);
-  __syncthreads();                             // wave_n may still be read
-  if ((threadIdx.x & 63) == 63) wave_n[threadIdx.x >> 6] = incl;
+// Sums over the workgroup: of the threads before this one, and of all.  Every
+// call has a row of counters of its own, so that one barrier is enough, and reads
+// them at once (a loop up to the own wave waits for each).
+struct WaveCounts {
+  int n[kEvictWaves];
+};
+__device__ __forceinline__ int block_before(int v, WaveCounts& c) {
+  const int incl = lane_scan(v), w = (int)(threadIdx.x >> 6);
+  if ((threadIdx.x & 63) == 63) c.n[w] = incl;
   __syncthreads();
+  const WaveCounts all = c;
   int before = incl - v;
-  for (int i = 0; i < (int)(threadIdx.x >> 6); ++i) before += wave_n[i];
+#pragma unroll
+  for (int i = 0; i < kEvictWaves; ++i) before += i < w ? all.n[i] : 0;
   return before;
 }
-__device__ __forceinline__ int block_sum(int v, int* wave_n) {
+__device__ __forceinline__ int block_sum(int v, WaveCounts& c) {
   const int s = lane_scan(v);
+  if ((threadIdx.x & 63) == 63) c.n[threadIdx.x >> 6] = s;
   __syncthreads();
-  if ((threadIdx.x & 63) == 63) wave_n[threadIdx.x >> 6] = s;
-  __syncthreads();
+  const WaveCounts all = c;
   int sum = 0;
-  for (int i = 0; i < kEvictWaves; ++i) sum += wave_n[i];
+#pragma unroll
+  for (int i = 0; i < kEvictWaves; ++i) sum += all.n[i];
   return sum;
 }
 
 // The counter that holds the rest-th key from the top, and the rank left in it:
 // thread t holds the t-th N counters from there (its first one `top`).
 template <int N>
-__device__ __forceinline__ void pick_digit(const int (&c)[N], int top, int& rest, int& bin, int* wave_n, int* picked) {
+__device__ __forceinline__ void pick_digit(const int (&c)[N], int top, int& rest, int& bin, WaveCounts& counts, int* picked) {
   int sum = 0;
 #pragma unroll
   for (int k = 0; k < N; ++k) sum += c[k];
-  int above = block_before(sum, wave_n);
+  int above = block_before(sum, counts);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     if (above < rest && rest <= above + c[k]) {
@@ -587,7 +594,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_count_kernel(EvictParams 
   constexpr int BITS = STAGE == 0 ? kDigit0 : kDigit12, SHIFT = STAGE == 0 ? 20 : (STAGE == 1 ? 10 : 0);
   constexpr int PER = (1 << BITS) / kEvictThreads;
   __shared__ __attribute__((aligned(16))) int hist[1 << BITS];
-  __shared__ int wave_n[kEvictWaves], picked[2];
+  __shared__ __attribute__((aligned(16))) WaveCounts counts[2];
+  __shared__ int picked[2];
   const int b = blockIdx.y, blk = blockIdx.x, tid = threadIdx.x;
   const int L = clamp_len(p.lens, b, p.t_max);
   if (L <= p.keep) return;
@@ -607,7 +615,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_count_kernel(EvictParams 
 #pragma unroll
       for (int k = 0; k < 4; ++k) c[k] += (int)(x >> (16 * (3 - k)) & 0xFFFFu);
     }
-    pick_digit(c, top, rest, bin, wave_n, picked);
+    pick_digit(c, top, rest, bin, counts[0], picked);
     if (blk == 0 && tid == 0) {
       p.state[4 * b] = bin;
       p.state[4 * b + 1] = rest;
@@ -620,7 +628,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_count_kernel(EvictParams 
     const uint16_t* h = p.hist1 + ((int64_t)b * p.blocks << kDigit12) + top;
 #pragma unroll 8
     for (int i = 0; i < p.blocks; ++i) c[0] += h[(int64_t)i << kDigit12];
-    pick_digit(c, top, rest, bin, wave_n, picked);
+    pick_digit(c, top, rest, bin, counts[0], picked);
     if (blk == 0 && tid == 0) {
       p.state[4 * b + 2] = bin;
       p.state[4 * b + 3] = rest;
@@ -639,7 +647,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_count_kernel(EvictParams 
     if (STAGE == 2) above += x >> BITS > prefix && x >> (BITS + kDigit12) == prefix >> kDigit12 ? 1 : 0;
   }
   if constexpr (STAGE > 0) {
-    above = block_sum(above, wave_n);
+    above = block_sum(above, counts[1]);
     if (tid == 0) p.above[(int64_t)(STAGE - 1) * p.B * p.blocks + at] = above;
   }
   __syncthreads();
@@ -654,7 +662,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_count_kernel(EvictParams 
 }
 
 __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams p) {
-  __shared__ int wave_n[kEvictWaves], picked[2], eq_n[2];
+  __shared__ __attribute__((aligned(16))) WaveCounts counts[5];
+  __shared__ int picked[2], eq_n[2];
   const int b = blockIdx.y, blk = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int L = clamp_len(p.lens, b, p.t_max), K = p.keep;
   const int64_t base = (int64_t)b * p.t_max;
@@ -684,7 +693,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
     before += i < blk ? x : 0;
     low += i < p.low ? x : 0;
   }
-  pick_digit(c, top, rest, bin, wave_n, picked);
+  pick_digit(c, top, rest, bin, counts[0], picked);
   const unsigned border = ((unsigned)p.state[4 * b] << kDigit12 | (unsigned)p.state[4 * b + 2]) << kDigit12 | (unsigned)bin;
   if (top == bin) {
     eq_n[0] = before;
@@ -697,8 +706,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
     more += i < blk ? x : 0;
     more_low += i < p.low ? x : 0;
   }
-  const int gt = block_sum(more + (top > bin ? before : 0), wave_n);
-  const int gt_low = block_sum(more_low + (top > bin ? low : 0), wave_n);
+  const int gt = block_sum(more + (top > bin ? before : 0), counts[1]);
+  const int gt_low = block_sum(more_low + (top > bin ? low : 0), counts[2]);
   // rows above the border stay, and the first `rest` of those on it
   const int eq = eq_n[0];
   const int kept_low = gt_low + min(rest, eq_n[1]), kept = gt + min(rest, eq);
@@ -712,8 +721,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
     on[i] = __ballot(r.in[i] && r.key[i] == border);
     n_on += __popcll(on[i]);
   }
-  int at_eq = eq + block_before(lane == 0 ? n_on : 0, wave_n);
-  at_eq = __builtin_amdgcn_readfirstlane(at_eq);
+  int at_eq = eq + __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_on : 0, counts[3]));
   int n_stay = 0, n_go = 0;
 #pragma unroll
   for (int i = 0; i < kEvictRows; ++i) {
@@ -724,7 +732,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
     n_go += __popcll(__ballot(r.in[i]) & ~stay[i]);
   }
   const bool is_low = blk < p.low;
-  int at = block_before(lane == 0 ? (is_low ? n_go : n_stay) : 0, wave_n);
+  int at = block_before(lane == 0 ? (is_low ? n_go : n_stay) : 0, counts[4]);
   at = __builtin_amdgcn_readfirstlane(at) + (is_low ? blk * kEvictBlock - kept : kept - kept_low);
   int32_t* const list = (is_low ? p.hole : p.move) + (int64_t)b * p.room;
 #pragma unroll
@@ -747,7 +755,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
 template <int N>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
   __shared__ __attribute__((aligned(16))) int hist[1 << kDigit0];
-  __shared__ int wave_n[5][kEvictWaves], picked[2];
+  __shared__ __attribute__((aligned(16))) WaveCounts counts[5];
+  __shared__ int picked[2];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int L = clamp_len(p.lens, b, p.t_max), K = p.keep;
   const int64_t base = (int64_t)b * p.t_max;
@@ -765,16 +774,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     for (int i = 0; i < N; ++i) store(i, r.in[i] ? r.weight[i] : 0.f, r.in[i] ? r.pos[i] : -1);
     return;
   }
-  // (every sum over the waves has a row of wave_n of its own, and the counters of
-  // a digit are cleared while the digit before is being settled: three barriers a
-  // digit)
-  auto before_waves = [&](int row, int incl, int own) {
-    if (lane == 63) wave_n[row][tid >> 6] = incl;
-    __syncthreads();
-    int before = incl - own;
-    for (int i = 0; i < (tid >> 6); ++i) before += wave_n[row][i];
-    return before;
-  };
+  // (the counters of a digit are cleared while the digit before is being settled:
+  // three barriers a digit)
   unsigned border = 0u;
   int rest = K;
 #pragma unroll
@@ -798,7 +799,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
       c[k] = hist[top - k];
       sum += c[k];
     }
-    int above = before_waves(digit, lane_scan(sum), sum);
+    int above = block_before(sum, counts[digit]);
 #pragma unroll
     for (int k = 0; k < per; ++k) {
       if (above < rest && rest <= above + c[k]) {
@@ -821,8 +822,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     on[i] = __ballot(r.in[i] && r.key[i] == border);
     n_on += __popcll(on[i]);
   }
-  // (a wave's numbers are uniform: its sum up to lane 63 is its own number)
-  int at_eq = __builtin_amdgcn_readfirstlane(before_waves(3, n_on, n_on));
+  int at_eq = __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_on : 0, counts[3]));
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     stay[i] = __ballot(r.in[i] && (r.key[i] > border || (r.key[i] == border && at_eq + __popcll(on[i] & below) < rest)));
@@ -831,8 +831,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams
     n_move += __popcll(stay[i] & __ballot(r.t[i] >= K));
   }
   // both numbers in one scan (each below 2^14)
-  const int mine = n_hole << 16 | n_move;
-  const int both = __builtin_amdgcn_readfirstlane(before_waves(4, mine, mine));
+  const int both = __builtin_amdgcn_readfirstlane(block_before(lane == 0 ? n_hole << 16 | n_move : 0, counts[4]));
   int hole = both >> 16, move = both & 0xFFFF;
   if (tid == kEvictThreads - 1) p.count[b] = move + n_move;
 #pragma unroll
