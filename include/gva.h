@@ -534,8 +534,8 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
  * 4-bit cache that holds the current token's row already (gva_q4_append_kv):
  * o and lse as there, with x_t over the values that the codes stand for and the
  * query rotated at position seen[b] - 1.  The query enters the products as a
- * bf16 high and a low part, so cached positional keys must be finite (their
- * lowest value hides a row as -inf would).  d_c a multiple of 32 (32 .. 512), H/G
+ * sum of bf16 parts, so cached positional keys must be finite (their lowest
+ * value hides a row as -inf would).  d_c a multiple of 32 (32 .. 512), H/G
  * in {1, 2, 4, 8}.  The caches are read only.  workspace: a caller-owned device
  * buffer of at least the bytes reported for the same dims, num_splits and
  * split_rows on the current device, 256-byte aligned, scratch.

@@ -203,6 +203,25 @@ __device__ __forceinline__ bf16x8 read_transposed(const uint8_t* p, int step) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Part k of eight floats as a sum of three bf16, each rounded to nearest.
+__device__ __forceinline__ bf16x8 split_part(const float* x, int k) {
+  bf16x8 out;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    f32x2 v = {x[j], x[j + 1]};
+    bf16x2 h = __builtin_convertvector(v, bf16x2);
+#pragma unroll
+    for (int i = 1; i < 3; ++i)
+      if (k >= i) {
+        v = v - __builtin_convertvector(h, f32x2);
+        h = __builtin_convertvector(v, bf16x2);
+      }
+    out[j] = h[0];
+    out[j + 1] = h[1];
+  }
+  return out;
+}
+
 // The largest of three (a NaN among them is passed over); fmaxf chains quiet every
 // operand with an instruction of its own first.
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -215,7 +234,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // of 32 rows.  As in the bf16 kernel a head has two columns of the products, its
 // absorbed query (and its softmax weights) as bf16 high and low parts, and with
 // FUSED the workgroup absorbs its heads' queries itself while its first tiles
-// are on their way.
+// are on their way.  Up to four heads a group leave columns 8 .. 15 free: column
+// 15 - n takes the query's third part for high column n, one more addition a
+// score (o is off by 5e-7 of its norm at B32 T8K H32 G8 d 128/16, by 2.5e-6 without;
+// 36.1 against 34.9 us).  Eight heads would need products of their own for it, and
+// the registers of a third workgroup (6 to 9% of the time): they have two parts.
 //
 // A tile is converted once, in the score products' operand order, and goes
 // through the wave's LDS for the transposed operand of P.V, a tile later.  That
@@ -254,9 +277,14 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, qd = lane >> 4;
   const int h0 = g * HPG;
-  const bool active = n < 2 * HPG;
-  const bool is_lo = n >= HPG;
-  const int col_head = !active ? 0 : (is_lo ? 2 * HPG - 1 - n : n);
+  const bool third = HPG <= 4 && n >= 8;       // the mirror column's third part
+  const int col = third ? 15 - n : n;
+  const bool active = col < 2 * HPG;
+  const bool is_lo = col >= HPG;
+  const int col_head = !active ? 0 : (is_lo ? 2 * HPG - 1 - col : col);
+  auto query_part = [&](const float* x) {
+    return !active || (third && is_lo) ? as_bf16x8(u32x4{0u, 0u, 0u, 0u}) : split_part(x, third ? 2 : (is_lo ? 1 : 0));
+  };
   const bf16x8 zero8 = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
   const int len_b = *(const __attribute__((address_space(4))) int32_t*)(head_lens + b);
   const int32_t* const seen_at = head_seen != nullptr ? head_seen : head_lens;
@@ -395,7 +423,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = src[j];
-      bq[c] = active ? split_hi_lo(x, is_lo) : zero8;
+      bq[c] = query_part(x);
     }
 #pragma unroll
     for (int rc = 0; rc < NRC; ++rc) {
@@ -403,7 +431,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = src[j];
-      bk[rc] = active ? split_hi_lo(x, is_lo) : zero8;
+      bk[rc] = query_part(x);
     }
   } else {
 #pragma unroll
@@ -411,14 +439,14 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = xa[c][j >> 2][j & 3] * a.scale_log2;
-      bq[c] = active ? split_hi_lo(x, is_lo) : zero8;
+      bq[c] = query_part(x);
     }
 #pragma unroll
     for (int rc = 0; rc < NRC; ++rc) {
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = xr[rc][j >> 2][j & 3] * a.scale_log2;
-      bk[rc] = active && 32 * rc + 8 * qd < a.d_r ? split_hi_lo(x, is_lo) : zero8;
+      bk[rc] = 32 * rc + 8 * qd < a.d_r ? query_part(x) : zero8;
     }
   }
   // the wave's tile: where the lane writes its pieces, and where it reads V^T
@@ -478,7 +506,10 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     float x[4];
     auto take_scores = [&]() {                   // and the largest of the lane's
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = (is_lo ? sc[1][j] : sc[0][j]) + mirror<HPG>(is_lo ? sc[0][j] : sc[1][j]);
+      for (int j = 0; j < 4; ++j) {
+        x[j] = (is_lo ? sc[1][j] : sc[0][j]) + mirror<HPG>(is_lo ? sc[0][j] : sc[1][j]);
+        if constexpr (HPG <= 4) x[j] = dpp_add<0x140>(x[j]);     // and the third part's, or to it
+      }
       if (tail) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -528,7 +559,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
       for (int ib = 0; ib < NB; ++ib) acc[ib] *= alpha;
       m_run = next;
       m_limit = moves ? 8.f : m_limit;
-      const float s0 = is_lo ? 0.f : -m_run;
+      const float s0 = is_lo || third ? 0.f : -m_run;
       start = f32x4{s0, s0, s0, s0};
     }
     // Weights as bf16 parts, each rounded to nearest: the high columns' own, and
@@ -536,21 +567,24 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     // most 2^-18; a single bf16 weight, 2^-9, would show in o at 1e-3).  The two
     // lanes exchange what the other needs.  The sum of the weights is a product
     // with ones.
-    uint32_t keep[2], got[2];
+    u32x4 parts;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const f32x2 e = {__builtin_amdgcn_exp2f(x[2 * j]), __builtin_amdgcn_exp2f(x[2 * j + 1])};
       const bf16x2 h = __builtin_convertvector(e, bf16x2);
       const bf16x2 l = __builtin_convertvector(e - __builtin_convertvector(h, f32x2), bf16x2);
       const uint32_t hb = __builtin_bit_cast(uint32_t, h), lb = __builtin_bit_cast(uint32_t, l);
-      keep[j] = is_lo ? lb : hb;
-      got[j] = __float_as_uint(mirror<HPG>(__uint_as_float(is_lo ? hb : lb)));
-    }
-    u32x4 parts;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      parts[j] = is_lo ? got[j] : keep[j];
-      parts[2 + j] = is_lo ? keep[j] : got[j];
+      if constexpr (HPG >= 4) {
+        // high and low columns are whole banks of four lanes: each takes the other's
+        // part where it is the one that lacks it
+        constexpr int LO = HPG == 4 ? 6 : 12;
+        parts[j] = (uint32_t)__builtin_amdgcn_update_dpp((int)hb, (int)lb, Mirror<HPG>::ctrl, 0xF, LO, false);
+        parts[2 + j] = (uint32_t)__builtin_amdgcn_update_dpp((int)lb, (int)hb, Mirror<HPG>::ctrl, 0xF, 15 - LO, false);
+      } else {
+        const uint32_t keep = is_lo ? lb : hb, got = __float_as_uint(mirror<HPG>(__uint_as_float(is_lo ? hb : lb)));
+        parts[j] = is_lo ? got : keep;
+        parts[2 + j] = is_lo ? keep : got;
+      }
     }
     bp = as_bf16x8(parts);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

@@ -480,6 +480,33 @@ def test_step_scores_far_above_those_before(hpg, d_v, S, low):
 
 
 @gpu
+@pytest.mark.parametrize("hpg,bits", [(1, 21), (2, 21), (4, 21), (8, 17)])
+@pytest.mark.parametrize("B,d_v", [(1, 64), (3, 128), (600, 64)])
+def test_step_query_parts(hpg, bits, B, d_v):
+    """One row, one column: lse is the score, a product of a query, a map and a
+    value that is exact in fp32.  The scaled query in three parts (up to four
+    heads a group) is off by 2^-27 of itself, the scale, the products, their
+    three sums and the factor at the end by 2^-24 each; in two parts by 2^-18."""
+    G, H = 2, 2 * hpg
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=32, d_r=0, t_max=32)
+    g = torch.Generator().manual_seed(hpg)
+    q, m = torch.zeros(B, H, 32), torch.zeros(H, d_v, 32)
+    q[..., 5] = torch.randn(B, H, generator=g)
+    m[:, 7, 5] = torch.randn(H, generator=g)
+    q, m = q.to(torch.bfloat16), m.to(torch.bfloat16)
+    v = torch.zeros(B, G, d_v, dtype=torch.bfloat16)
+    v[..., 7] = 48.0
+    note(f"q4 step, query parts hpg={hpg} B={B} d_v={d_v}")
+    c, s = gva.q4_cache(d)
+    seq = torch.arange(B, dtype=torch.int32).cuda()
+    gva.gva_q4_append_kv(d, c, s, None, v.cuda(), None, seq, torch.zeros_like(seq))
+    o, lse = gva.q4_decode(d, q.cuda(), m.cuda(), c, s, None, torch.ones_like(seq))
+    want = 48.0 * q[..., 5].double() * m[:, 7, 5].double() / math.sqrt(32)
+    assert bool(((lse.cpu().double() - want).abs() <= 2.0 ** -bits * want.abs()).all())
+    assert bool((o[..., 7] == 48.0).all())
+
+
+@gpu
 def test_step_reads_a_nan_block_as_nan_in_its_group_only():
     x = problem(1, 64, 4, 2, 64, 64, 0, [40], seed=6)
     code, byte = ref.unpack(x["vc"].cpu(), x["sc"].cpu())
