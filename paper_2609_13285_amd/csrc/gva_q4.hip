@@ -239,6 +239,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // score (o is off by 5e-7 of its norm at B32 T8K H32 G8 d 128/16, by 2.5e-6 without;
 // 36.1 against 34.9 us).  Eight heads would need products of their own for it, and
 // the registers of a third workgroup (6 to 9% of the time): they have two parts.
+// The weights have a third part in the same columns where a wave has at most four
+// tiles: the roundings of few rows show most (256 rows of H8 G2 d 64: 1.2e-6 with
+// two parts, 1.3e-7 with three; 5.7 and 5.9 us), and in every tile of a long split
+// it costs 2 to 5% for an error that is below 1e-6 already.
 //
 // A tile is converted once, in the score products' operand order, and goes
 // through the wave's LDS for the transposed operand of P.V, a tile later.  That
@@ -363,6 +367,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
   const int s_lane = (qd * NS / 4 * 16 + n) * 2;
   const int ntiles = (r1 - r0 + kTileRows - 1) / kTileRows;
   const int my_tiles = ntiles > w ? (ntiles - w + NW - 1) / NW : 0;
+  const bool fine = ntiles <= 4 * NW;          // the weights in three parts
   auto tile_row = [&](int j) { return r0 + (w + NW * j) * kTileRows; };
   auto load_tile = [&](TileT& t, int row0) {
 #pragma unroll
@@ -562,18 +567,26 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
       const float s0 = is_lo || third ? 0.f : -m_run;
       start = f32x4{s0, s0, s0, s0};
     }
-    // Weights as bf16 parts, each rounded to nearest: the high columns' own, and
-    // in the low columns that of what the high part leaves (together off by at
-    // most 2^-18; a single bf16 weight, 2^-9, would show in o at 1e-3).  The two
-    // lanes exchange what the other needs.  The sum of the weights is a product
-    // with ones.
+    // Weights as bf16 parts, each rounded to nearest: the high columns' own, in the
+    // low columns that of what the high part leaves, and in the mirror columns, where
+    // a split is short, that of the rest (two parts are together off by at most
+    // 2^-18; a single one, 2^-9, would show in o at 1e-3).  The two lanes of a pair
+    // exchange what the other needs.  The sum of the weights is a product with ones.
     u32x4 parts;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const f32x2 e = {__builtin_amdgcn_exp2f(x[2 * j]), __builtin_amdgcn_exp2f(x[2 * j + 1])};
       const bf16x2 h = __builtin_convertvector(e, bf16x2);
-      const bf16x2 l = __builtin_convertvector(e - __builtin_convertvector(h, f32x2), bf16x2);
-      const uint32_t hb = __builtin_bit_cast(uint32_t, h), lb = __builtin_bit_cast(uint32_t, l);
+      const f32x2 r = e - __builtin_convertvector(h, f32x2);
+      const bf16x2 l = __builtin_convertvector(r, bf16x2);
+      uint32_t hb = __builtin_bit_cast(uint32_t, h), lb = __builtin_bit_cast(uint32_t, l);
+      if constexpr (HPG <= 4) {
+        if (fine) {
+          const bf16x2 rest = __builtin_convertvector(r - __builtin_convertvector(l, f32x2), bf16x2);
+          hb = third ? __builtin_bit_cast(uint32_t, rest) : hb;
+          lb = third ? __builtin_bit_cast(uint32_t, rest) : lb;
+        }
+      }
       if constexpr (HPG >= 4) {
         // high and low columns are whole banks of four lanes: each takes the other's
         // part where it is the one that lacks it
@@ -606,12 +619,16 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
   l_run = mfma16(ones, bp, l_run);
 
   // ---- merge the waves and write this split's partial
-  const float l_sum = l_run[0] + mirror<HPG>(l_run[0]);
+  auto all_parts = [&](float y) {              // of a high column
+    const float two = y + mirror<HPG>(y);
+    return HPG <= 4 && fine ? two + mirror<8>(y) : two;
+  };
+  const float l_sum = all_parts(l_run[0]);
   if (l_sum == 0.f) m_run = -INFINITY;         // no row counted
 #pragma unroll
   for (int ib = 0; ib < NB; ++ib)
 #pragma unroll
-    for (int jj = 0; jj < 4; ++jj) acc[ib][jj] += mirror<HPG>(acc[ib][jj]);
+    for (int jj = 0; jj < 4; ++jj) acc[ib][jj] = all_parts(acc[ib][jj]);
   __syncthreads();                             // the tiles' LDS holds the records from here on
   float* const red = reinterpret_cast<float*>(lds);
   if (n < HPG) {
