@@ -494,7 +494,7 @@ __device__ __forceinline__ unsigned evict_key(const EvictParams& p, int pos, flo
 // spread over many counters): every block counts its own keys, and the next launch
 // adds up the blocks' counters, each workgroup for itself.  The fourth numbers the
 // rows.  No counter is shared, so nothing has to be cleared.  Bound by latency: four
-// sequences of 32K rows 4.7, 4.7, 4.8 and 7.2 us.
+// sequences of 32K rows 4.7, 4.7, 4.7 and 6.6 us.
 template <int N>
 struct EvictRows {
   int t[N];
@@ -750,8 +750,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_number_kernel(EvictParams
 }
 
 // The whole selection of a sequence in one workgroup, N rows a thread: up to 8K
-// rows it takes less than the four launches above (4K rows, B = 32: 10 us against
-// 21; 32K rows, whose keys do not fit the registers beside the rest: 84 against 21).
+// rows it takes less than the four launches above (4K rows, B = 32: 9.6 us against
+// 20; 32K rows, whose keys do not fit the registers beside the rest: 84 against 20).
 template <int N>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictParams p) {
   __shared__ __attribute__((aligned(16))) int hist[1 << kDigit0];

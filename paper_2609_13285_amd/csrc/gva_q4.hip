@@ -250,9 +250,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // of a CU's LDS, 3/4 of the loop's time, beside 135 of vector work, 77 of matrix
 // products and 177 of HBM's share (V^T by products with an identity, which need
 // no LDS, take as long in the matrix cores: 16 more of them a tile).
-// B32 T8K H32 G8 d 128/16 (153 MB): 35.8 us, 4.3 TB/s, of which about 7.5 are the
-// start, the absorption and the end; B4 of 64K to 128K rows (240 MB) 50 and 5 for
-// the combine, 4.8 TB/s in the loop.
+// B32 T8K H32 G8 d 128/16 (153 MB): 36.4 us, 4.2 TB/s, of which about 7.5 are the
+// start, the absorption and the end; B4 of 64K to 128K rows (240 MB) 51 and 5 for
+// the combine.
 template <int HPG, int DV, int NRC, int NW, bool FUSED>
 __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_decode_kernel(GVA_Q4_HEAD_ARGS,
                                                                                             Q4DecodeParams p) {
@@ -467,6 +467,16 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
   float m_run = 0.f, m_limit = -INFINITY;      // no maximum yet: any score sets it
   f32x4 start = {0.f, 0.f, 0.f, 0.f};          // of the score products: -m_run in the high columns
   f32x4 l_run = {0.f, 0.f, 0.f, 0.f};          // the sum of a column's weights, four times
+  // x - y, exact where y is x rounded: a dot product with (-1, 0) and (0, -1) each,
+  // one instruction where a conversion and a subtraction are two (36.4 against 36.7
+  // us at B32 T8K).  The pairs are held in registers: as constants they came out as
+  // the bits of an fp32 -1, the wrong half of a pair for one of them.
+  uint32_t minus_first = 0x0000BF80u, minus_second = 0xBF800000u;
+  asm volatile("" : "+s"(minus_first), "+s"(minus_second));
+  auto less = [&](f32x2 x, bf16x2 y) {
+    return f32x2{__builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, minus_first), x[0], false),
+                 __builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, minus_second), x[1], false)};
+  };
   const bf16x8 ones = as_bf16x8(u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
   f32x4 acc[NB];
 #pragma unroll
@@ -577,12 +587,12 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     for (int j = 0; j < 2; ++j) {
       const f32x2 e = {__builtin_amdgcn_exp2f(x[2 * j]), __builtin_amdgcn_exp2f(x[2 * j + 1])};
       const bf16x2 h = __builtin_convertvector(e, bf16x2);
-      const f32x2 r = e - __builtin_convertvector(h, f32x2);
+      const f32x2 r = less(e, h);
       const bf16x2 l = __builtin_convertvector(r, bf16x2);
       uint32_t hb = __builtin_bit_cast(uint32_t, h), lb = __builtin_bit_cast(uint32_t, l);
       if constexpr (HPG <= 4) {
         if (fine) {
-          const bf16x2 rest = __builtin_convertvector(r - __builtin_convertvector(l, f32x2), bf16x2);
+          const bf16x2 rest = __builtin_convertvector(less(r, l), bf16x2);
           hb = third ? __builtin_bit_cast(uint32_t, rest) : hb;
           lb = third ? __builtin_bit_cast(uint32_t, rest) : lb;
         }
