@@ -571,6 +571,8 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
  * bf16 and 4-bit caches: d_v in {64, 128}, d_c a multiple of 32, d_r one of 8
  * (<= 64), positional keys finite as for gva_q4_decode_step; fp32: what the
  * tiled layout takes.  Any H/G, batch <= 65535.  The sums have a fixed order.
+ * workspace here and below: as for gva_q4_decode_step, of the bytes that the
+ * size call reports; calls that run at the same time need one each.
  */
 int gva_weights_workspace_size(const gva_dims* dims, int32_t n_new, size_t* bytes);
 int gva_accumulate_weights(const gva_dims* dims, int32_t n_new, const void* q, const void* m, const void* v_cache,
