@@ -704,6 +704,16 @@ Q4DecodeFn pick_q4_decode(int hpg, int dv, int nrc, int nw, bool fused) {
   return nullptr;
 }
 
+// The shapes that the step takes: a 4-bit cache's, the absorption's widths, and
+// the heads per group that the kernel has columns for.
+int check_q4_step_dims(const gva_dims* d) {
+  const int st = check_q4_dims(d);
+  if (st != GVA_OK) return st;
+  const int hpg = d->n_heads / d->n_groups;
+  if (hpg != 1 && hpg != 2 && hpg != 4 && hpg != 8) return GVA_ERR_UNSUPPORTED;
+  return d->d_c % 32 != 0 || d->d_c < 32 || d->d_c > 512 ? GVA_ERR_UNSUPPORTED : GVA_OK;
+}
+
 // Workgroups that a CU holds at once, by their registers.
 inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) : 3; }
 
@@ -765,7 +775,7 @@ struct Q4StepLayout {
 };
 
 int q4_step_layout(const gva_dims* d, int32_t num_splits, int32_t split_rows, Q4StepLayout& L) {
-  int st = check_q4_dims(d);
+  const int st = check_q4_step_dims(d);
   if (st != GVA_OK) return st;
   if (num_splits < 1 || num_splits > GVA_MAX_SPLITS || split_rows < 0 || split_rows % kTileRows != 0)
     return GVA_ERR_INVALID_ARG;
@@ -853,7 +863,7 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
 
 int gva_q4_pick_splits(const gva_dims* dims, const int32_t* lens, int32_t n_cu, int32_t* split_rows) {
   if (split_rows != nullptr) *split_rows = 0;
-  if (check_q4_dims(dims) != GVA_OK) return 1;
+  if (check_q4_step_dims(dims) != GVA_OK) return 1;
   if (n_cu <= 0) n_cu = device_cu_count();
   const Q4Cost cost{n_cu, dims->n_groups, dims->d_v};
   int longest = 0;
@@ -907,7 +917,6 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
     return GVA_ERR_INVALID_ARG;
   if (L.bytes > 0 && (workspace == nullptr || workspace_bytes < L.bytes || !aligned(workspace, 256)))
     return GVA_ERR_INVALID_ARG;
-  if (dims->d_c % 32 != 0 || dims->d_c < 32 || dims->d_c > 512) return GVA_ERR_UNSUPPORTED;
   const int hpg = dims->n_heads / dims->n_groups;
   const int nw = q4_waves(dims, num_splits, split_rows, device_cu_count());
   const Q4DecodeFn fn = pick_q4_decode(hpg, dims->d_v, (dims->d_r + 31) / 32, nw, L.fused);
