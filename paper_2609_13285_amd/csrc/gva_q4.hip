@@ -687,9 +687,15 @@ Q4DecodeFn pick_q4_nrc(int nrc) {
   return nullptr;
 }
 
+// Eight waves absorb inside but for chunks of 4096 <= split_rows < 4 (H/G) d_c (see
+// q4_waves, q4_fused), which takes four heads a group at least (d_c <= 512).
 template <int HPG, int DV>
 Q4DecodeFn pick_q4_waves(int nrc, int nw, bool fused) {
-  if (nw == 8) return fused ? pick_q4_nrc<HPG, DV, 8, true>(nrc) : pick_q4_nrc<HPG, DV, 8, false>(nrc);
+  if (nw == 8 && fused) return pick_q4_nrc<HPG, DV, 8, true>(nrc);
+  if (nw == 8) {
+    if constexpr (HPG >= 4) return pick_q4_nrc<HPG, DV, 8, false>(nrc);
+    return nullptr;
+  }
   return fused ? pick_q4_nrc<HPG, DV, 4, true>(nrc) : pick_q4_nrc<HPG, DV, 4, false>(nrc);
 }
 
