@@ -536,7 +536,8 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
  * query rotated at position seen[b] - 1.  The query enters the products as a
  * sum of bf16 parts, so cached positional keys must be finite (their lowest
  * value hides a row as -inf would).  d_c a multiple of 32 (32 .. 512), H/G
- * in {1, 2, 4, 8}.  The caches are read only.  workspace: a caller-owned device
+ * in {1, 2, 4, 8}: others GVA_ERR_UNSUPPORTED, from the size call too; the step
+ * may refuse more than 2^20 sequences likewise.  The caches are read only.  workspace: a caller-owned device
  * buffer of at least the bytes reported for the same dims, num_splits and
  * split_rows on the current device, 256-byte aligned, scratch.
  * gva_q4_pick_splits -- host heuristic: the split plan (num_splits, and in
@@ -570,7 +571,8 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
  * v_cache is a bf16 or fp32 cache where v4_scale is NULL, else a 4-bit one.
  * bf16 and 4-bit caches: d_v in {64, 128}, d_c a multiple of 32, d_r one of 8
  * (<= 64), positional keys finite as for gva_q4_decode_step; fp32: what the
- * tiled layout takes.  Any H/G, batch <= 65535.  The sums have a fixed order.
+ * tiled layout takes.  Any H/G, B <= 65535, B * n_new <= 2^20.  The sums have a
+ * fixed order.
  * workspace here and below: as for gva_q4_decode_step, of the bytes that the
  * size call reports; calls that run at the same time need one each.
  */
