@@ -3,11 +3,15 @@ serving runs them at (many tiles a wave, absorption outside the launch, several
 tiles a workgroup, selection over blocks), and what their plans and sizes refuse."""
 
 import ctypes
+import math
 
 import pytest
+import torch
 
+import q4_ref as ref
+from gpu_helpers import note
 from paper_2609_13285_amd import gva
-from test_q4_evict import A, dims, step_status, weights_status
+from test_q4_evict import A, check_step, dims, problem, step, step_status, weights_status
 
 gpu = pytest.mark.gpu
 
@@ -44,3 +48,118 @@ def test_more_query_rows_than_the_absorption_takes_are_refused():
     d = dims(batch=1 << 10, t_max=1 << 12)
     assert weights_status(d, N=(1 << 10) + 1) == gva.GVA_ERR_UNSUPPORTED
     assert step_status(dims(batch=(1 << 20) + 1, t_max=32), S=1) == gva.GVA_ERR_UNSUPPORTED
+
+
+# --------------------------------------------------------------- decode
+def tiles_of_longest_split(T, S, rows):
+    """32-row tiles of a full sequence's splits (include/gva.h's split rule)."""
+    n = S if rows == 0 else min(S, max(1, -(-T // rows)))
+    return -(-(-(-T // n)) // 32)
+
+
+def absorbs_outside(d, S, rows):
+    """Whether the workspace holds absorbed queries beside the splits' partials."""
+    up = lambda n: -(-n // 256) * 256                    # noqa: E731
+    BH = d.batch * d.n_heads
+    parts = up(BH * S * d.d_v * 4) + up(BH * S * 4) if S > 1 else 0
+    return gva.gva_q4_decode_workspace_size(d, S, rows) > parts
+
+
+@gpu
+@pytest.mark.parametrize("hpg", [1, 2, 4, 8])
+@pytest.mark.parametrize("d_v,d_r", [(64, 16), (128, 40), (64, 40), (128, 16)])
+@pytest.mark.parametrize("S,rows", [(1, 0), (2, 1504)])
+def test_step_many_tiles_a_wave(hpg, d_v, d_r, S, rows):
+    """Splits of over four tiles for each of eight waves: the weights in two
+    parts, the tiles in registers taken round several times."""
+    T = 2976
+    x = problem(4, T, 2 * hpg, 2, d_v, 64, d_r, [T, 2081, 37, 1291], extra=77, seed=hpg + d_v + d_r)
+    note(f"q4 step, long splits hpg={hpg} d={d_v}/{d_r} S={S} rows={rows}")
+    assert tiles_of_longest_split(T, S, rows) > 4 * 8
+    assert not absorbs_outside(x["d"], S, rows)
+    check_step(x, *step(x, S, rows))
+
+
+@gpu
+@pytest.mark.parametrize("hpg,d_v,d_r", [(1, 64, 8), (2, 128, 24), (4, 64, 64), (4, 128, 40), (8, 64, 40), (8, 128, 16)])
+@pytest.mark.parametrize("B,S,rows", [(300, 1, 0), (100, 3, 0), (100, 3, 32)])
+def test_step_absorption_outside(hpg, d_v, d_r, B, S, rows):
+    """More workgroups than two per CU: queries absorbed, and rotated at seen -
+    1, by a launch before, with splits and bounded chunks."""
+    T = 96
+    lens = torch.randint(-2, T + 9, (B,), generator=torch.Generator().manual_seed(B + S + hpg)).tolist()
+    lens[:5] = [T, 0, 1, 33, T - 1]
+    x = problem(B, T, 2 * hpg, 2, d_v, 64, d_r, lens, extra=1000, seed=hpg * 10 + d_r)
+    note(f"q4 step, absorption outside hpg={hpg} d={d_v}/{d_r} B={B} S={S} rows={rows}")
+    assert absorbs_outside(x["d"], S, rows)
+    check_step(x, *step(x, S, rows))
+
+
+@gpu
+@pytest.mark.parametrize("hpg", [4, 8])
+def test_step_eight_waves_absorption_outside(hpg):
+    """Long chunks of few streams, but more (sequence, split) slots than are
+    resident, and wide maps."""
+    B, T, S, rows = 65, 8256, 4, 4128
+    lens = [T, 8192 - 31] + [1 + 97 * i % 400 for i in range(B - 2)]
+    x = problem(B, T, 2 * hpg, 2, 64, 288, 16, lens, extra=5, seed=hpg)
+    d = x["d"]
+    note(f"q4 step, eight waves, absorption outside hpg={hpg}")
+    assert absorbs_outside(d, S, rows) and B * 2 <= 256 <= gva.device_cu_count()
+    check_step(x, *step(x, S, rows))
+
+
+@gpu
+@pytest.mark.parametrize("hpg", [1, 2, 4])
+@pytest.mark.parametrize("B,d_v", [(3, 64), (64, 128), (600, 64)])
+def test_step_weight_parts(hpg, B, d_v):
+    """Two rows with scores 0 and x in (-2, 0) (log2), x = q~ v with one column:
+    o = v e / (1 + e) there, e = 2^x.  In units of 2^-24: x is off by 4.2 |x| (the
+    scale, its product, two sums of the parts, the parts), so e by 5.8 of itself, by
+    2 more for the exponential and by 1/4 for its three parts (2^-26); the products'
+    and waves' sums, the division and the stored result are 7.  Two parts alone
+    would be off by up to 128."""
+    G, H = 2, 2 * hpg
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=32, d_r=0, t_max=32)
+    q, m = torch.zeros(B, H, 32), torch.zeros(H, d_v, 32)
+    q[..., 5] = -0.05 - 1.2 * torch.rand(B, H, generator=torch.Generator().manual_seed(B + hpg))
+    m[:, 7, 5] = 1.0
+    q, m = q.to(torch.bfloat16), m.to(torch.bfloat16)
+    v = torch.zeros(B, 2, G, d_v, dtype=torch.bfloat16)
+    v[:, 1, :, 7] = 6.0
+    note(f"q4 step, weight parts hpg={hpg} B={B} d_v={d_v}")
+    c, s = gva.q4_cache(d)
+    seq, row = torch.arange(B, dtype=torch.int32).repeat_interleave(2).cuda(), torch.arange(2, dtype=torch.int32).repeat(B).cuda()
+    gva.gva_q4_append_kv(d, c, s, None, v.view(2 * B, G, d_v).cuda(), None, seq, row)
+    o, lse = gva.q4_decode(d, q.cuda(), m.cuda(), c, s, None, torch.full((B,), 2, dtype=torch.int32, device="cuda"))
+    e = torch.exp(6.0 * q[..., 5].double() / math.sqrt(32))
+    want = 6.0 * e / (1 + e)
+    assert float((o[..., 7].cpu().double() / want - 1).abs().max()) <= 16 * 2.0 ** -24
+    # the logarithm of a sum in (1, 2), in base 2, and the factor to the natural one
+    assert float((lse.cpu().double() - torch.log1p(e)).abs().max()) <= 16 * 2.0 ** -24
+
+
+@gpu
+@pytest.mark.parametrize("hpg,bits", [(1, 21), (2, 21), (4, 21), (8, 16)])
+@pytest.mark.parametrize("d_r,at", [(8, 6), (40, 38), (64, 32)])
+@pytest.mark.parametrize("B", [3, 600])
+def test_step_positional_query_parts(hpg, bits, d_r, at, B):
+    """One row at position 0, one column of the positional key: lse is the score.
+    In three parts (up to four heads a group) the query is off by 2^-26 of itself,
+    and the scale, its product, the parts' sums and the factor at the end by 2^-24
+    each, under 2^-21; in two parts by 2^-17 more."""
+    G, H, d_v = 2, 2 * hpg, 64
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=32, d_r=d_r, t_max=32)
+    q, m = torch.zeros(B, H, 32 + d_r), torch.zeros(H, d_v, 32)
+    q[..., 32 + at] = torch.randn(B, H, generator=torch.Generator().manual_seed(hpg + d_r))
+    q = q.to(torch.bfloat16)
+    v, k = torch.zeros(B, G, d_v, dtype=torch.bfloat16), torch.zeros(B, d_r, dtype=torch.bfloat16)
+    k[:, at] = 24.0
+    note(f"q4 step, positional query parts hpg={hpg} d_r={d_r} B={B}")
+    c, s = gva.q4_cache(d)
+    kr = torch.zeros(B, 32, d_r, dtype=torch.bfloat16, device="cuda")
+    seq = torch.arange(B, dtype=torch.int32).cuda()
+    gva.gva_q4_append_kv(d, c, s, kr, v.cuda(), k.cuda(), seq, torch.zeros_like(seq))
+    o, lse = gva.q4_decode(d, q.cuda(), m.to(torch.bfloat16).cuda(), c, s, kr, torch.ones_like(seq))
+    want = 24.0 * q[..., 32 + at].double() / math.sqrt(32 + d_r)
+    assert bool(((lse.cpu().double() - want).abs() <= 2.0 ** -bits * want.abs()).all())
