@@ -163,3 +163,107 @@ def test_step_positional_query_parts(hpg, bits, d_r, at, B):
     o, lse = gva.q4_decode(d, q.cuda(), m.to(torch.bfloat16).cuda(), c, s, kr, torch.ones_like(seq))
     want = 24.0 * q[..., 32 + at].double() / math.sqrt(32 + d_r)
     assert bool(((lse.cpu().double() - want).abs() <= 2.0 ** -bits * want.abs()).all())
+
+
+# -------------------------------------------------------------- weights
+def rows_per_workgroup(d, N):
+    """gva_accumulate_weights' rule: whole tiles, few enough for two workgroups per CU."""
+    joined = d.dtype == gva.GVA_DTYPE_BF16 and not (N == 1 and d.n_heads // d.n_groups in (1, 2, 4, 8))
+    streams, chunk = d.batch * (d.n_groups if joined else 1), 512
+    while chunk > 32 and streams * -(-d.t_max // chunk) < 2 * gva.device_cu_count():
+        chunk //= 2
+    return chunk
+
+
+def large_weights(cache, B, T, H, G, d_v, d_r, N, lens, least, seed):
+    """gva_accumulate_weights against 64 bits on the GPU.  Values are 4-bit
+    numbers (every block holds its largest, 6 * 2^-2), so that every cache holds
+    them exactly.  Tolerances: a score of two bf16 parts is off by 2^-17 of its sum
+    of magnitudes (fp32: 2^-24), its fp32 sums over at most 192 terms by 200 *
+    2^-24, the absorbed query by 66 * 2^-24 of its 64 terms' magnitudes, the
+    log-sum-exp's difference by a few 2^-24 of both; the sum over queries and heads by
+    2^-23 a term."""
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=64, d_r=d_r, t_max=T, dtype="f32" if cache == "f32" else "bf16")
+    assert rows_per_workgroup(d, N) >= least
+    dt, hpg, W = d.torch_dtype, H // G, 64 + d_r
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda")     # noqa: E731
+    level = torch.cat((ref.LEVELS, -ref.LEVELS)).float().cuda() / 4
+    rows = level[torch.randint(0, 16, (B, G, T, d_v), generator=g, device="cuda")]
+    rows[..., ::32] = 1.5
+    kr, q, m = rand(B, T, d_r).to(dt), rand(B, N, H, W).to(dt), (rand(H, d_v, 64) / 8).to(dt)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    L = ln.clamp(0, T)
+    dead = torch.arange(T, device="cuda") >= L.unsqueeze(1)
+    kc = gva.tiled(kr.masked_fill(dead[..., None], math.nan)) if d_r else None
+    if cache == "q4":
+        vc, sc = gva.q4_cache(d)
+        sc.fill_(255)                                    # rows never written read as NaN
+        seq, row = (~dead).nonzero(as_tuple=True)
+        spare = torch.zeros(B, T, d_r, dtype=dt, device="cuda") if d_r else None
+        gva.gva_q4_append_kv(d, vc, sc, spare, rows.transpose(1, 2)[seq, row].to(dt).contiguous(), kr[seq, row].contiguous() if d_r else None,
+                             seq.int(), row.int())
+    else:
+        vc, sc = gva.tiled(rows.to(dt).masked_fill(dead[:, None, :, None], math.nan)), None
+    seen = L + 11
+    # the definition, and what its terms allow
+    x = torch.full((B, N, H, T), -math.inf, dtype=torch.float64, device="cuda")
+    size, made = torch.zeros_like(x), torch.zeros_like(x)
+    for b in range(B):
+        n = int(L[b])
+        if n == 0:
+            continue
+        qd = q[b].double()
+        qa = torch.matmul(qd[..., :64].transpose(0, 1).contiguous(), m.double().transpose(1, 2).contiguous())      # [H, N, d_v]
+        terms = torch.matmul(qd[..., :64].abs().transpose(0, 1).contiguous(), m.double().abs().transpose(1, 2).contiguous())
+        qr = ref.rotate(qd[..., 64:].cpu(), (int(seen[b]) - N + torch.arange(N)).clamp(min=0).unsqueeze(1)).cuda().transpose(0, 1).contiguous()
+        vb = rows[b, :, :n].double().repeat_interleave(hpg, 0).transpose(1, 2).contiguous()
+        kb = kr[b, :n].double().t().contiguous()
+        hidden = torch.arange(n, device="cuda") > (n - N + torch.arange(N, device="cuda")).unsqueeze(1)
+        s = (torch.matmul(qa, vb) + torch.matmul(qr, kb)) / math.sqrt(W)
+        x[b, :, :, :n] = s.masked_fill(hidden, -math.inf).transpose(0, 1)
+        size[b, :, :, :n] = ((torch.matmul(qa.abs(), vb.abs()) + torch.matmul(qr.abs(), kb.abs())) / math.sqrt(W)).transpose(0, 1)
+        made[b, :, :, :n] = (torch.matmul(terms, vb.abs()) / math.sqrt(W)).transpose(0, 1)
+    lse = torch.logsumexp(x, -1).float()
+    w = torch.rand(B, T, generator=g, device="cuda").masked_fill(dead, math.nan)
+    out = torch.full((B, T), 55.0, device="cuda")
+    note(f"weights {cache} B={B} T={T} H={H} G={G} d={d_v}/{d_r} N={N}")
+    ws = gva.weights_workspace_for(d, N)
+    ws.fill_(0xFF)
+    gva.gva_accumulate_weights(d, N, q, m, vc, sc, kc, ln, lse, w, out, workspace=ws, seen=seen, decay=0.75)
+    some = torch.isfinite(lse).unsqueeze(-1)
+    l64 = torch.where(some, lse.double().unsqueeze(-1), torch.zeros_like(x[..., :1]))
+    p = torch.exp(x - l64) * some
+    dx = size * ((2.0 ** -24 if cache == "f32" else 2.0 ** -17) + 200 * 2.0 ** -24) + made * 66 * 2.0 ** -24 + 4 * 2.0 ** -24 * (1 + l64.abs() + size)
+    want = p.sum((1, 2)) + 0.75 * w.double()
+    tol = (p * torch.expm1(dx)).sum((1, 2)) + 2.0 ** -23 * (N * H + 4) * want
+    err = (out.double() - want).abs()
+    assert bool((err <= tol)[~dead].all()), float((err / tol)[~dead].max())
+    assert bool((out[dead] == 55.0).all())
+
+
+def ragged(B, T):
+    """Lengths that end inside a tile, on one, in the first and the last chunk; full, none."""
+    some = [T, T - 1, 0, 1, T // 2 + 3, 33, 512, 513, T - 31, T - 32, 3 * T // 4 + 17, 479]
+    return [some[i % 12] for i in range(B)]
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16", "f32"])
+@pytest.mark.parametrize("G,hpg,d_v,d_r,T,least", [(4, 4, 64, 16, 8160, 256), (8, 1, 64, 40, 4096, 128), (2, 8, 128, 0, 8192, 256),
+                                                   (11, 2, 64, 8, 4064, 128)])
+def test_weights_of_a_token_many_tiles(cache, G, hpg, d_v, d_r, T, least):
+    """Several tiles a wave: the start tile of a stream's own, the ring of
+    tiles in registers, groups in rounds."""
+    large_weights(cache, 16, T, G * hpg, G, d_v, d_r, 1, ragged(16, T), least, seed=G)
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16", "f32"])
+@pytest.mark.parametrize("G,hpg,d_v,d_r,N", [(4, 4, 64, 16, 3), (4, 4, 64, 40, 12), (4, 4, 128, 0, 40), (8, 3, 64, 24, 1),
+                                             (4, 3, 64, 8, 17)])
+def test_weights_of_a_window_many_tiles(cache, G, hpg, d_v, d_r, N):
+    """One, two and over four column sets (tiles dealt over four, two waves and
+    one), each over several tiles."""
+    T = 4096 - 16 * (cache != "q4")
+    large_weights(cache, 16, T, G * hpg, G, d_v, d_r, N, ragged(16, T), 128, seed=N)
