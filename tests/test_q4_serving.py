@@ -11,7 +11,7 @@ import torch
 import q4_ref as ref
 from gpu_helpers import note
 from paper_2609_13285_amd import gva
-from test_q4_evict import A, check_step, dims, problem, step, step_status, weights_status
+from test_q4_evict import A, check_step, dims, evict_case, problem, step, step_status, weights_status
 
 gpu = pytest.mark.gpu
 
@@ -267,3 +267,43 @@ def test_weights_of_a_window_many_tiles(cache, G, hpg, d_v, d_r, N):
     one), each over several tiles."""
     T = 4096 - 16 * (cache != "q4")
     large_weights(cache, 16, T, G * hpg, G, d_v, d_r, N, ragged(16, T), 128, seed=N)
+
+
+# ------------------------------------------------------------- eviction
+def order_weights(kind, B, T):
+    g = torch.Generator().manual_seed(T)
+    if kind == "equal":
+        return torch.full((B, T), 0.5)
+    if kind == "special":
+        few = torch.tensor([0.0, -0.0, math.nan, math.inf, -math.inf, -1.0, 1e-40, -1e-40, 3.0, 3.4e38])
+        return few[torch.randint(0, 10, (B, T), generator=g)]
+    if kind == "close":                                  # neighbouring floats: the border's last digit decides
+        return 1.0 + torch.randint(0, 300, (B, T), generator=g) * 2.0 ** -23
+    up = torch.arange(T).float().div(3).floor().expand(B, T).contiguous()      # threes alike
+    return -up if kind == "decreasing" else up
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["equal", "special", "close", "increasing", "decreasing"])
+@pytest.mark.parametrize("T,keep", [(6016, 2500), (8192, 5000), (13024, 6500), (20000, 9001), (8224, 8200)])
+def test_evict_orders_over_blocks(kind, T, keep):
+    """Ties on the border over several blocks on both sides of the budget (past
+    8192 rows) or eight rows a thread, sequences that keep every row beside others."""
+    lens = [T, 0, keep - 1, keep, keep + 1, T - 7]
+    w = order_weights(kind, len(lens), T)
+    note(f"evict order {kind} T={T} keep={keep}")
+    evict_case(len(lens), T, 1, 64, 0, "q4", lens, keep, 2, 30, weights=w, seed=1)
+    evict_case(len(lens), T, 1, 64, 0, "q4", lens, keep, 0, 0, with_pos=False, weights=w, seed=2, runs=1)
+
+
+@gpu
+@pytest.mark.parametrize("cache,G,d_v,d_r", [("bf16", 2, 64, 24), ("f32", 1, 20, 8), ("q4", 2, 128, 16)])
+@pytest.mark.parametrize("T,keep,first,recent", [(12320, 5000, 4, 700), (9280, 1, 0, 0), (16400, 12288, 5000, 4200), (9296, 20000, 0, 0)])
+def test_evict_over_blocks(cache, G, d_v, d_r, T, keep, first, recent):
+    """The rows themselves, at sizes of the selection over blocks: few weights
+    that many rows share, protected ranges longer than a block."""
+    T = (T + 31) // 32 * 32
+    lens = [T - 5, min(keep, T), T, 17]
+    note(f"evict over blocks {cache} T={T} keep={keep}")
+    evict_case(len(lens), T, G, d_v, d_r, cache, lens, keep, first, recent, seed=keep, runs=1)
+    evict_case(len(lens), T, G, d_v, d_r, cache, lens, keep, first, recent, with_pos=False, seed=keep + 1, runs=1)
