@@ -720,8 +720,16 @@ int check_q4_step_dims(const gva_dims* d) {
   return d->d_c % 32 != 0 || d->d_c < 32 || d->d_c > 512 ? GVA_ERR_UNSUPPORTED : GVA_OK;
 }
 
-// Workgroups that a CU holds at once, by their registers.
-inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) : 3; }
+// Workgroups that a CU holds at once, at least, by the registers of a lane: at d_v
+// = 128 up to 164, 191 with a second chunk of the positional key (d_r > 32); at d_v
+// = 64 up to 120 with eight waves and 144 with four, 143 and 170 with that chunk (168,
+// which a third workgroup of four waves would fit, with the absorption outside or one
+// head a group).
+inline int q4_resident(const gva_dims* d, int nw) {
+  const bool two_chunks = d->d_r > 32;
+  if (nw == 8) return d->d_v == 128 || two_chunks ? 1 : 2;
+  return two_chunks ? 2 : 3;
+}
 
 // Waves per workgroup: eight while the workgroups are resident at once; with
 // bounded chunks (whose empty splits count among them) while a chunk is long and
@@ -729,10 +737,12 @@ inline int q4_resident(int d_v, int nw) { return nw == 8 ? (d_v == 128 ? 1 : 2) 
 // T8K H32 G8 d 128, 256 workgroups, 35.4 and 43.1; B64 T2K, 512, 28.0 and 23.5; B4
 // of 64K to 128K rows, chunks of 13024, 54.8 and 67.4; B64 to 32K rows, H16 G2,
 // chunks of 4096 30.0 and 33.0, of 2048 39.2 and 30.5; B64 to 8K rows, G8, chunks
-// of 4096 41.4 and 30.8.
+// of 4096 41.4 and 30.8.  Even splits at d_v = 64, H32 G8: d_r = 16, 320 workgroups
+// of T4K 21.3 and 23.7, 512 of T2K 16.1 and 16.0; d_r = 64, 320 of T4K 30.7 and 27.8,
+// 512 of T2K 22.3 and 18.7, of T256 11.5 and 8.5.
 int q4_waves(const gva_dims* d, int num_splits, int split_rows, int n_cu) {
   if (split_rows > 0) return split_rows >= 4096 && (long long)d->batch * d->n_groups <= n_cu ? 8 : kWaves;
-  return decode_grid(d, num_splits, 0) <= (long long)n_cu * q4_resident(d->d_v, 8) ? 8 : kWaves;
+  return decode_grid(d, num_splits, 0) <= (long long)n_cu * q4_resident(d, 8) ? 8 : kWaves;
 }
 
 // Whether the workgroups absorb their queries themselves: while they are resident
@@ -746,12 +756,16 @@ bool q4_fused(const gva_dims* d, int num_splits, int split_rows, int n_cu) {
 }
 
 // What a plan costs in microseconds, from the times above: a workgroup's start and
-// end, its rows at the pace of its CU (which the workgroups there share), and the
-// combine.  Only the order of two plans matters.
+// end, its rows at the pace of its CU (which the workgroups there share), the
+// absorption where it is a launch before, and the combine.  Only the order of two
+// plans matters.  (With the absorption, and the workgroups that fit at d_r > 32,
+// against without: B53 of 1K to 2K rows, H4 G1 d 128/16, 4 splits with it inside
+// 12.0 us, 10 with it before 18.1; B17 to 10K rows, H32 G8 d 64/16, 14.2 and 17.2;
+// B40 of 2K to 4K rows, H32 G8 d 128/40, chunks of 2912 30.8, of 1632 39.0.)
 struct Q4Cost {
   int n_cu, groups, d_v;
   double us(const gva_dims* d, const int32_t* lens, int S, int c) const {
-    const int nw = q4_waves(d, S, c, n_cu), most = q4_resident(d_v, nw);
+    const int nw = q4_waves(d, S, c, n_cu), most = q4_resident(d, nw);
     long long items = 0, rows = 0, longest = 0;
     for (int b = 0; b < d->batch; ++b) {
       const long long L = lens != nullptr ? (lens[b] < 0 ? 0 : (lens[b] > d->t_max ? d->t_max : lens[b])) : d->t_max;
@@ -771,6 +785,7 @@ struct Q4Cost {
     const double rounds = (double)items / ((double)n_cu * most);
     double t = rounds <= 1.0 ? 7.0 + (last > mean ? last : mean) : 7.0 + 4.0 * (rounds - 1.0) + mean + last / 2;
     const double idle = (double)(decode_grid(d, S, c) - items) / ((double)n_cu * most);      // empty splits
+    if (!q4_fused(d, S, c, n_cu)) t += 4.0;
     return t + (idle > 0 ? idle * 1.2 : 0.0) + (S > 1 ? 4.5 + 0.05 * S + (S > 16 ? 3.0 : 0.0) : 0.0);
   }
 };

@@ -50,6 +50,27 @@ def test_more_query_rows_than_the_absorption_takes_are_refused():
     assert step_status(dims(batch=(1 << 20) + 1, t_max=32), S=1) == gva.GVA_ERR_UNSUPPORTED
 
 
+# --------------------------------------------------------------- plans
+@pytest.mark.parametrize("kw,lens", [
+    (dict(batch=53, n_heads=4, n_groups=1, d_r=16, t_max=2144), [1072 + 1072 * i // 52 for i in range(53)]),
+    (dict(batch=28, n_heads=8, n_groups=4, d_v=64, d_r=32, t_max=4352), [round(128 * 34 ** (i / 27)) for i in range(28)]),
+    (dict(batch=74, n_heads=8, n_groups=1, d_r=16, t_max=3136), [1568 + 1568 * i // 73 for i in range(74)])])
+def test_plans_count_the_absorption_that_they_cause(kw, lens):
+    """Streams of a few thousand rows: splits past two workgroups per CU save less
+    than the absorption's launch, which they make necessary, takes."""
+    d = dims(**kw)
+    S, rows = gva.gva_q4_pick_splits(d, torch.tensor(lens))
+    assert not absorbs_outside(d, S, rows)
+
+
+def test_plans_fit_the_registers_of_wide_positional_keys():
+    """Two workgroups of four waves on a CU at d_r > 32, not three."""
+    d = dims(batch=40, n_heads=32, n_groups=8, d_r=40, t_max=4096)
+    lens = [2048 + 2048 * i // 39 for i in range(40)]
+    S, rows = gva.gva_q4_pick_splits(d, torch.tensor(lens), 256)
+    assert S == 1 or sum(-(-n // rows) if rows else S for n in lens) * 8 <= 2 * 256
+
+
 # --------------------------------------------------------------- decode
 def tiles_of_longest_split(T, S, rows):
     """32-row tiles of a full sequence's splits (include/gva.h's split rule)."""
