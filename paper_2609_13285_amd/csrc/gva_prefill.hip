@@ -27,7 +27,7 @@ namespace {
 // shared by the column blocks).
 // Precision.  The absorbed and rotated queries enter the score product as
 // bf16 high + low pairs (x = hi + lo to ~2^-16 of x, as in the decode
-// kernel): a single bf16 query moves every logit by up to 2^-9 of its size,
+// kernel): a single bf16 query moves every logit by up to 2^-8 of its size,
 // an error that grows with the sharpness of the scores.  The high parts
 // stay in registers; the low parts, the same for every tile and every wave
 // of the workgroup, are read from LDS each tile (registers are the limit).

@@ -580,8 +580,9 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
     // Weights as bf16 parts, each rounded to nearest: the high columns' own, in the
     // low columns that of what the high part leaves, and in the mirror columns, where
     // a split is short, that of the rest (two parts are together off by at most
-    // 2^-18; a single one, 2^-9, would show in o at 1e-3).  The two lanes of a pair
-    // exchange what the other needs.  The sum of the weights is a product with ones.
+    // 2^-17, three hold an fp32 number; a single one, 2^-8, would show in o at 1e-3).
+    // The two lanes of a pair exchange what the other needs.  The sum of the weights
+    // is a product with ones.
     u32x4 parts;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
