@@ -476,7 +476,8 @@ int gva_prefer_fused(const gva_dims* dims, int32_t num_splits, int32_t split_row
  *   code    = the nearest (ties to the even code; past 6 it saturates), with
  *             the element's sign; a block that holds a NaN or an infinity is
  *             stored as NaN throughout
- * so an element is off by at most 2^e, and every value is exactly a bf16.
+ * so an element is off by at most 2^e, and every value is exactly a bf16.  (At the
+ * bound e = 125, which a block past 7 * 2^125 gets too, by less than 2 * 2^e.)
  * v4_cache  B*G streams of T rows, d_v / 2 bytes a row, in blocks of 1 KB, R =
  *           2048 / d_v rows each: column i of row t is in byte
  *             (t/R)*1024 + ((i/P)*16 + t%16)*16 + (t%R/16)*8 + (i%P)/2,
@@ -535,7 +536,10 @@ int gva_q4_unpack_kv(const gva_dims* dims, const void* v4_cache, const void* v4_
  * o and lse as there, with x_t over the values that the codes stand for and the
  * query rotated at position seen[b] - 1.  The query enters the products as a
  * sum of bf16 parts, so cached positional keys must be finite (their lowest
- * value hides a row as -inf would).  d_c a multiple of 32 (32 .. 512), H/G
+ * value hides a row as -inf would): three parts, as exact as fp32, for up to four
+ * heads a group, two (off by at most 2^-17 of an entry) for eight.  The softmax
+ * weights enter in two, for up to four heads a group in three where splits are
+ * short.  d_c a multiple of 32 (32 .. 512), H/G
  * in {1, 2, 4, 8}: others GVA_ERR_UNSUPPORTED, from the size call too; the step
  * may refuse more than 2^20 sequences likewise.  The caches are read only.  workspace: a caller-owned device
  * buffer of at least the bytes reported for the same dims, num_splits and
@@ -570,8 +574,8 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
  * step's query, more are a window of a prompt's last ones (1 <= n_new <= T).
  * v_cache is a bf16 or fp32 cache where v4_scale is NULL, else a 4-bit one.
  * bf16 and 4-bit caches: d_v in {64, 128}, d_c a multiple of 32, d_r one of 8
- * (<= 64), positional keys finite as for gva_q4_decode_step; fp32: what the
- * tiled layout takes.  Any H/G, B <= 65535, B * n_new <= 2^20.  The sums have a
+ * (<= 64), positional keys finite as for gva_q4_decode_step, the query in two bf16
+ * parts (off by at most 2^-17 of an entry); fp32: what the tiled layout takes.  Any H/G, B <= 65535, B * n_new <= 2^20.  The sums have a
  * fixed order.
  * workspace here and below: as for gva_q4_decode_step, of the bytes that the
  * size call reports; calls that run at the same time need one each.

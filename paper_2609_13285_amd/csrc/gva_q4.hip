@@ -7,7 +7,9 @@
 // The scale is the smallest 2^e with amax <= 7 * 2^e, -119 <= e <= 125: up to
 // 7 an element that saturates at 6 is off by at most 2^e, no more than one
 // between 4 and 6 is, and the finer scale pays for it (rms error of N(0, 1)
-// rows 0.112; 0.115 with amax <= 6 * 2^e and with floor(log2 amax) - 2).  Every
+// rows 0.112; 0.115 with amax <= 6 * 2^e and with floor(log2 amax) - 2).  (Past 7 *
+// 2^125 there is no larger scale, and the last bf16 numbers are off by up to twice
+// that.)  Every
 // value is exactly a bf16: codes have two significant bits, and the bounds on e
 // keep 0.5 * 2^e normal and 6 * 2^e finite.
 // A row takes 4.25 bits an element, 576 B at G = 8, d_v = 128, d_r = 16 against

@@ -190,7 +190,10 @@ def _stream(stream) -> Optional[int]:
 def _in_use_on(stream, *tensors):
     """Tell torch's caching allocator that ``tensors``, allocated on the
     current stream, are also read by kernels enqueued on ``stream``, so their
-    memory is not handed out again before that work is done."""
+    memory is not handed out again before that work is done.  It does not
+    order the streams: the memory may have been freed by work that the current
+    stream has yet to finish, so callers make ``stream`` wait for it first
+    (``stream.wait_stream(torch.cuda.current_stream())``)."""
     if stream is None:
         return
     s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
@@ -943,8 +946,16 @@ def gva_q4_decode_step(dims: GvaDims, q, m, v4_cache, v4_scale, kr_cache, lens, 
 
 def q4_decode(dims: GvaDims, q, m, v4_cache, v4_scale, kr_cache, lens, seen=None,
               stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """One decode step on a 4-bit cache, planned for its lengths (which it
-    reads); returns (o, lse) fp32."""
+    """One decode step on a 4-bit cache, planned for its lengths; returns (o,
+    lse) fp32.
+
+    Every call copies ``lens`` to the host, which waits for the current stream
+    and cannot be captured into a graph, and prices plans there (some 4 to 40 us
+    for 1 to 64 sequences).  A serving loop plans once instead (q4_plan_for), keeps
+    the buffer of q4_workspace_for and calls gva_q4_decode_step: any plan is right
+    for any lengths.  ``stream`` has to wait for the current one, on which the
+    outputs and the workspace are allocated.
+    """
     d = dims
     S, rows = q4_plan_for(d, lens)
     dev = v4_cache.device
@@ -990,7 +1001,8 @@ def gva_accumulate_weights(dims: GvaDims, n_new: int, q, m, v_cache, v4_scale, k
 def accumulate_weights(dims: GvaDims, q, m, v_cache, kr_cache, lens, lse, weights, v4_scale=None, seen=None,
                        decay: float = 1.0, stream=None) -> torch.Tensor:
     """gva_accumulate_weights in place; q [B, N, H, d_c+d_r], or [B, H, ...]
-    for a decode step (lse alike).  Returns weights."""
+    for a decode step (lse alike).  Returns weights.  ``stream`` has to wait for
+    the current one, on which the workspace is allocated."""
     d = dims
     if q.dim() == 3:
         q, lse = q.unsqueeze(1), lse.unsqueeze(1)
@@ -1032,7 +1044,9 @@ def evict(dims: GvaDims, n_keep: int, v_cache, kr_cache, lens, weights, n_first:
     """gva_evict_rows; returns (lens, weights, row_pos) as they are afterwards
     (row_pos None where none is given).  From then on queries are rotated at
     their token's position, ``seen - 1``: q4_decode takes seen, on other caches
-    gva_absorb_query takes it for its lens, before gva_decode_attention."""
+    gva_absorb_query takes it for its lens, before gva_decode_attention.
+    ``stream`` has to wait for the current one, on which the outputs and the
+    workspace are allocated."""
     d = dims
     out = torch.empty_like(lens), torch.empty_like(weights), None if row_pos is None else torch.empty_like(row_pos)
     ws = evict_workspace_for(d, v_cache.device)
