@@ -121,7 +121,9 @@ struct WeightStream {
 // the pair for the tile's first 16 rows and the low column's for the others, so
 // that every exponential is taken once.  A wave's sums over the heads go to its
 // group's array of row sums, which are added in order at the end: the result
-// does not depend on timing.  The log-sum-exp is the products' initial value.
+// does not depend on timing.  The log-sum-exp is the products' initial value.  With
+// the query in two parts a sum over 32 heads is off by 3e-8 of its size (an
+// evaluation in fp32: 4e-8), over two by up to 2.2e-6; three parts cost 3%.
 // Bound by HBM: B32 T8K H32 G8 d 128/16 in 4 bits (154 MB) 28.2 us, 5.5 TB/s, and
 // 4.6 before it for the absorbed queries.
 template <int HPG, int DV, int NRC, bool Q4>
@@ -232,7 +234,8 @@ __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) wei
 // by the matrix products (twice the algorithm's, for the low parts) where there
 // are many rows, 32 queries on B8 T16K H32 G8 d 128/16 bf16 in 100 us, 0.77
 // PFLOP/s of them, and by latency where there are few: B2 of 4K to 8K rows 18.7 us,
-// and 5 and 4 for the absorption before and the join behind it.
+// and 5 and 4 for the absorption before and the join behind it (sums over 1024
+// queries and heads off by 3.2e-8, as in fp32; 4-bit rows 24.4 us in all).
 constexpr int kWindowRows = 512, kWindowCols = 32;   // most rows of a workgroup; columns of a wave
 
 template <int DV, int NRC, bool Q4>
@@ -350,8 +353,9 @@ __global__ void __launch_bounds__(kThreads) weights_join_kernel(WeightParams p) 
 }
 
 // fp32 storage: the same on the fp32 products, 16-row tiles, any d_v and d_r
-// that the tiled layout takes.  Bound by the products and their loads' latency: a
-// checking path, not a serving one.
+// that the tiled layout takes.  Bound by the products and their loads' latency, the
+// rows read again for every 16 columns: a checking path, not a serving one (H32 G8 d
+// 128/16: a token of B8 T8K, 275 MB, 87 us, 32 queries on B2 of 4K to 8K rows 117).
 __global__ void __launch_bounds__(64 * kWeightWaves) weights_f32_kernel(WeightParams p) {
   __shared__ float sums[kWeightWaves][kWeightChunk];
   const int nchunks = (p.t_max + p.chunk - 1) / p.chunk;

@@ -247,14 +247,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // it costs 2 to 5% for an error that is below 1e-6 already.
 //
 // A tile is converted once, in the score products' operand order, and goes
-// through the wave's LDS for the transposed operand of P.V, a tile later.  That
-// bounds the loop: 8 KB written and 8 KB read a tile at d_v = 128 are 176 cycles
-// of a CU's LDS, 3/4 of the loop's time, beside 135 of vector work, 77 of matrix
-// products and 177 of HBM's share (V^T by products with an identity, which need
-// no LDS, take as long in the matrix cores: 16 more of them a tile).
-// B32 T8K H32 G8 d 128/16 (153 MB): 36.4 us, 4.2 TB/s, of which about 7.5 are the
-// start, the absorption and the end; B4 of 64K to 128K rows (240 MB) 51 and 5 for
-// the combine.
+// through the wave's LDS for the transposed operand of P.V, a tile later.  At d_v
+// = 128 a tile takes the loop about 235 cycles of a CU, which nothing fills alone: HBM's
+// share is 177, LDS 176 (8 KB written, 8 KB read), vector work 134, matrix products
+// 77.  What is lost is overlap, with one workgroup of eight waves on a CU (V^T by
+// products with an identity, which need no LDS, was slower: 16 more of them a tile).
+// B32 T8K H32 G8 d 128/16 (153 MB): 36.4 to 38.9 us on different GPUs, 3.9 to 4.2 TB/s,
+// of which about 7.5 are the start, the absorption and the end, which nothing hides;
+// B4 of 64K to 128K rows (240 MB) 51 to 52 and 5 for the combine.
 template <int HPG, int DV, int NRC, int NW, bool FUSED>
 __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_decode_kernel(GVA_Q4_HEAD_ARGS,
                                                                                             Q4DecodeParams p) {
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(64 * NW, (Q4Cfg<HPG, DV, NRC, NW>::OCC)) q4_de
   f32x4 l_run = {0.f, 0.f, 0.f, 0.f};          // the sum of a column's weights, four times
   // x - y, exact where y is x rounded: a dot product with (-1, 0) and (0, -1) each,
   // one instruction where a conversion and a subtraction are two (36.4 against 36.7
-  // us at B32 T8K).  The pairs are held in registers: as constants they came out as
+  // us at B32 T8K on one GPU).  The pairs are held in registers: as constants they came out as
   // the bits of an fp32 -1, the wrong half of a pair for one of them.
   uint32_t minus_first = 0x0000BF80u, minus_second = 0xBF800000u;
   asm volatile("" : "+s"(minus_first), "+s"(minus_second));
