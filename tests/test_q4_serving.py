@@ -196,23 +196,23 @@ def rows_per_workgroup(d, N):
     return chunk
 
 
-def large_weights(cache, B, T, H, G, d_v, d_r, N, lens, least, seed):
+def large_weights(cache, B, T, H, G, d_v, d_r, N, lens, least, seed, d_c=64):
     """gva_accumulate_weights against 64 bits on the GPU.  Values are 4-bit
     numbers (every block holds its largest, 6 * 2^-2), so that every cache holds
     them exactly.  Tolerances: a score of two bf16 parts is off by 2^-17 of its sum
     of magnitudes (fp32: 2^-24), its fp32 sums over at most 192 terms by 200 *
-    2^-24, the absorbed query by 66 * 2^-24 of its 64 terms' magnitudes, the
+    2^-24, the absorbed query by (d_c + 2) 2^-24 of its terms' magnitudes, the
     log-sum-exp's difference by a few 2^-24 of both; the sum over queries and heads by
     2^-23 a term."""
-    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=64, d_r=d_r, t_max=T, dtype="f32" if cache == "f32" else "bf16")
+    d = dims(batch=B, n_heads=H, n_groups=G, d_v=d_v, d_c=d_c, d_r=d_r, t_max=T, dtype="f32" if cache == "f32" else "bf16")
     assert rows_per_workgroup(d, N) >= least
-    dt, hpg, W = d.torch_dtype, H // G, 64 + d_r
+    dt, hpg, W = d.torch_dtype, H // G, d_c + d_r
     g = torch.Generator(device="cuda").manual_seed(seed)
     rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda")     # noqa: E731
     level = torch.cat((ref.LEVELS, -ref.LEVELS)).float().cuda() / 4
     rows = level[torch.randint(0, 16, (B, G, T, d_v), generator=g, device="cuda")]
     rows[..., ::32] = 1.5
-    kr, q, m = rand(B, T, d_r).to(dt), rand(B, N, H, W).to(dt), (rand(H, d_v, 64) / 8).to(dt)
+    kr, q, m = rand(B, T, d_r).to(dt), rand(B, N, H, W).to(dt), (rand(H, d_v, d_c) / math.sqrt(d_c)).to(dt)
     ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
     L = ln.clamp(0, T)
     dead = torch.arange(T, device="cuda") >= L.unsqueeze(1)
@@ -235,9 +235,9 @@ def large_weights(cache, B, T, H, G, d_v, d_r, N, lens, least, seed):
         if n == 0:
             continue
         qd = q[b].double()
-        qa = torch.matmul(qd[..., :64].transpose(0, 1).contiguous(), m.double().transpose(1, 2).contiguous())      # [H, N, d_v]
-        terms = torch.matmul(qd[..., :64].abs().transpose(0, 1).contiguous(), m.double().abs().transpose(1, 2).contiguous())
-        qr = ref.rotate(qd[..., 64:].cpu(), (int(seen[b]) - N + torch.arange(N)).clamp(min=0).unsqueeze(1)).cuda().transpose(0, 1).contiguous()
+        qa = torch.matmul(qd[..., :d_c].transpose(0, 1).contiguous(), m.double().transpose(1, 2).contiguous())      # [H, N, d_v]
+        terms = torch.matmul(qd[..., :d_c].abs().transpose(0, 1).contiguous(), m.double().abs().transpose(1, 2).contiguous())
+        qr = ref.rotate(qd[..., d_c:].cpu(), (int(seen[b]) - N + torch.arange(N)).clamp(min=0).unsqueeze(1)).cuda().transpose(0, 1).contiguous()
         vb = rows[b, :, :n].double().repeat_interleave(hpg, 0).transpose(1, 2).contiguous()
         kb = kr[b, :n].double().t().contiguous()
         hidden = torch.arange(n, device="cuda") > (n - N + torch.arange(N, device="cuda")).unsqueeze(1)
@@ -255,7 +255,7 @@ def large_weights(cache, B, T, H, G, d_v, d_r, N, lens, least, seed):
     some = torch.isfinite(lse).unsqueeze(-1)
     l64 = torch.where(some, lse.double().unsqueeze(-1), torch.zeros_like(x[..., :1]))
     p = torch.exp(x - l64) * some
-    dx = size * ((2.0 ** -24 if cache == "f32" else 2.0 ** -17) + 200 * 2.0 ** -24) + made * 66 * 2.0 ** -24 + 4 * 2.0 ** -24 * (1 + l64.abs() + size)
+    dx = size * ((2.0 ** -24 if cache == "f32" else 2.0 ** -17) + 200 * 2.0 ** -24) + made * (d_c + 2) * 2.0 ** -24 + 4 * 2.0 ** -24 * (1 + l64.abs() + size)
     want = p.sum((1, 2)) + 0.75 * w.double()
     tol = (p * torch.expm1(dx)).sum((1, 2)) + 2.0 ** -23 * (N * H + 4) * want
     err = (out.double() - want).abs()
@@ -288,6 +288,47 @@ def test_weights_of_a_window_many_tiles(cache, G, hpg, d_v, d_r, N):
     one), each over several tiles."""
     T = 4096 - 16 * (cache != "q4")
     large_weights(cache, 16, T, G * hpg, G, d_v, d_r, N, ragged(16, T), 128, seed=N)
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["q4", "bf16", "f32"])
+@pytest.mark.parametrize("G,hpg,d_v,d_c,d_r,N", [(2, 16, 64, 1024, 56, 1), (1, 40, 128, 96, 64, 2), (3, 5, 128, 32, 0, 1),
+                                                 (1, 1, 64, 256, 8, 33)])
+def test_weights_any_heads_per_group_wide_maps(cache, G, hpg, d_v, d_c, d_r, N):
+    T = 224
+    large_weights(cache, 5, T, G * hpg, G, d_v, d_r, N, [T, 0, 97, 33, T + 3], 32, seed=hpg, d_c=d_c)
+
+
+@gpu
+def test_two_streams_at_once():
+    """A step, its weights and an eviction on each of two streams, with buffers
+    of their own, give what they give one after the other."""
+    def work(x, stream):
+        d = x["d"]
+        with torch.cuda.stream(stream):
+            o, lse = gva.q4_decode(d, x["q1"], x["m1"], x["vc"], x["sc"], x["kc"], x["l1"], seen=x["s1"])
+            w = gva.accumulate_weights(d, x["q1"], x["m1"], x["vc"], x["kc"], x["l1"], lse, x["w0"].clone(), v4_scale=x["sc"], seen=x["s1"])
+            out = gva.evict(d, 5000, x["vc"].clone(), x["kc"].clone(), x["l1"], w, n_first=2, n_recent=40, v4_scale=x["sc"].clone(),
+                            seen=x["s1"], row_pos=x["rp"])
+        return o, lse, w, *out
+
+    xs = []
+    for k in range(2):
+        x = problem(3, 8640, 8, 2, 64, 64, 16, [8640, 5001, 7000 + k], extra=3, seed=50 + k)
+        x.update(q1=x["q"][:, 0].contiguous().cuda(), m1=x["m"].cuda(), l1=x["lens"].cuda(), s1=x["seen"].cuda(),
+                 w0=torch.rand(3, 8640, generator=torch.Generator().manual_seed(k)).cuda(),
+                 rp=torch.arange(8640, dtype=torch.int32, device="cuda").expand(3, 8640).contiguous())
+        xs.append(x)
+    note("two streams at once")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    want = [work(x, streams[0]) for x in xs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [work(x, s) for x, s in zip(xs, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(u.view(torch.uint8), v.view(torch.uint8)) for u, v in zip(a, b))
 
 
 # ------------------------------------------------------------- eviction
