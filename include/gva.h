@@ -567,8 +567,9 @@ int gva_q4_decode_step(const gva_dims* dims, const void* q, const void* m, const
  * with x the scaled score of gva_decode_attention, query i of sequence b at
  * position seen[b] - n_new + i, seeing rows t <= L_b - n_new + i as in a
  * prompt.  Rows from L_b on of new_weights are left as they were.  A query with
- * lse -inf (nothing to see) adds nothing.  decay (>= 0) of 0 reads no weights (NULL
- * is allowed); new_weights may be weights itself, else it must not overlap it.
+ * nothing to see adds nothing: lse -inf, or below -2^20, where rows hidden by a large
+ * finite value are all that it sees.  decay (>= 0) of 0 reads no weights (NULL is
+ * allowed); new_weights may be weights itself, else it must not overlap it.
  * q [B][n_new][H][d_c + d_r] and M in the storage dtype, lse [B][n_new][H] as
  * the attention calls return it, weights [B][T] fp32.  n_new == 1 is a decode
  * step's query, more are a window of a prompt's last ones (1 <= n_new <= T).

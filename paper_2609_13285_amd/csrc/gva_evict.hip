@@ -114,6 +114,14 @@ struct WeightStream {
   }
 };
 
+// What the score products start from, -log2(e) lse.  -inf, whose weights are 0, for a
+// query with nothing to see: lse is -inf, or so low that rows hidden by a large finite
+// value are all there is.  Scores are as large then, and x - lse would be their
+// rounding (past 2^20 over 2^-4, at a type's lowest value anything: weights of 1e27
+// and infinity, which no later one outweighs).  A NaN stays.
+constexpr float kNothingSeen = -1048576.f;
+__device__ __forceinline__ float weight_start(float lse) { return lse < kNothingSeen ? -INFINITY : -lse * (float)kLog2e; }
+
 // One query per sequence (a decode step).  The workgroup takes `chunk` rows of
 // one sequence; wave w scores group w % GP of a round of GP = min(G, 8) groups (a
 // power of two), every (8 / GP)-th tile of the chunk.  A head has two columns of
@@ -176,8 +184,7 @@ __global__ void __launch_bounds__(64 * kWeightWaves, Q4 || DV == 64 ? 4 : 2) wei
       in.template load<kAuxNT>(buf[d], tile_row(d));
       __builtin_amdgcn_sched_barrier(0);
     }
-    // -inf: a query with nothing to see, whose weights are 0
-    const float init = is_lo ? 0.f : (ls != -INFINITY ? -ls * (float)kLog2e : -INFINITY);
+    const float init = is_lo ? 0.f : weight_start(ls);
     bf16x8 bq[NC], bk[NRC > 0 ? NRC : 1];
 #pragma unroll
     for (int c = 0; c < NC; ++c) bq[c] = active ? in.part(q, c, p.scale_log2, is_lo) : zero8;
@@ -280,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2) weights_window_kernel(WeightParam
     float init[2];
 #pragma unroll
     for (int cb = 0; cb < 2; ++cb) {
-      init[cb] = ls[cb] != -INFINITY ? -ls[cb] * (float)kLog2e : -INFINITY;
+      init[cb] = weight_start(ls[cb]);
 #pragma unroll
       for (int c = 0; c < NK; ++c) {
         hi[cb][c] = in.part(q[cb], c, p.scale_log2, false);
@@ -384,9 +391,10 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_f32_kernel(WeightPa
       const int qi = active ? col / hpg : 0;
       const int64_t qrow = ((int64_t)b * p.N + qi) * p.H + g * hpg + (active ? col % hpg : 0);
       const float ls = active ? p.lse[qrow] : -INFINITY;
-      const bool live = ls != -INFINITY;
+      const float start = weight_start(ls);
+      const bool live = start != -INFINITY;
       const int last = L - p.N + qi;
-      const float init = live ? -ls * (float)kLog2e : 0.f;
+      const float init = live ? start : 0.f;
       for (int j = w / GP; j < ntiles; j += TS) {
         const int64_t row0 = r0 + j * 16;
         f32x4 sc = {init, init, init, init};

@@ -300,6 +300,58 @@ def test_weights_any_heads_per_group_wide_maps(cache, G, hpg, d_v, d_c, d_r, N):
 
 
 @gpu
+@pytest.mark.parametrize("cache,N", [("q4", 1), ("q4", 3), ("bf16", 1), ("bf16", 3), ("f32", 1), ("f32", 3)])
+@pytest.mark.parametrize("low,q_at", [(-1e9, 1.0), (float(torch.finfo(torch.bfloat16).min), 0.01),
+                                      (float(torch.finfo(torch.bfloat16).min), 6.0)])
+def test_weights_where_finite_values_hide_every_row(cache, N, low, q_at):
+    """A sequence with nothing but rows hidden by a large finite value: scores and
+    log-sum-exp are as large, and their difference is rounding.  Hidden rows draw no
+    weight; the other sequence's weights are its own."""
+    H, T = 8, 96
+    x = problem(2, T, H, 2, 64, 64, 16, [T, 70], N=N, cache=cache, seed=3)
+    d = x["d"]
+    x["q"][..., -2:] = torch.tensor([q_at, 0.0])         # the slowest pair: hardly turned at these positions
+    x["kr"][0, :, 14] = low
+    x["kr"] = x["kr"].to(d.torch_dtype).double()
+    x["kc"] = gva.tiled(x["kr"].to(d.torch_dtype)).cuda()
+    s, _ = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], 2)
+    lse = torch.logsumexp(s, -1).float().cuda()
+    note(f"weights, every row hidden by {low}, {cache} N={N}")
+    w = torch.zeros(2, T, device="cuda")
+    gva.accumulate_weights(d, x["q"].cuda(), x["m"].cuda(), x["vc"], x["kc"], x["lens"].cuda(), lse, w, v4_scale=x["sc"],
+                           seen=x["seen"].cuda(), decay=0.0)
+    assert bool((w[0] == 0).all())
+    p = torch.exp(s[1] - lse[1].cpu().double().unsqueeze(-1)).sum((0, 1))
+    assert float((w[1, :70].cpu().double() - p[:70]).abs().max()) <= 1e-3 * N * H
+
+
+@gpu
+@pytest.mark.parametrize("cache,N", [("q4", 1), ("q4", 3), ("bf16", 1), ("bf16", 3), ("f32", 1), ("f32", 3)])
+def test_weights_of_a_nan_row_are_nan(cache, N):
+    """A NaN in a value row reaches that row's weight, and no other's."""
+    H, T = 8, 96
+    x = problem(2, T, H, 2, 64, 64, 16, [T, 70], N=N, cache=cache, seed=4)
+    d = x["d"]
+    s, _ = ref.scores(x["q"], x["m"], x["v"], x["kr"], x["lens"], x["seen"], 2)
+    lse = torch.logsumexp(s, -1).float().cuda()
+    if cache == "q4":
+        code, byte = ref.unpack(x["vc"].cpu(), x["sc"].cpu())
+        byte[0, 1, 37, 1] = 255
+        x["sc"] = ref.pack(code, byte)[1].cuda()
+    else:
+        v = gva.untiled(x["vc"].cpu())
+        v[0, 1, 37, 40] = math.nan
+        x["vc"] = gva.tiled(v).cuda()
+    note(f"weights, a NaN row, {cache} N={N}")
+    w = torch.zeros(2, T, device="cuda")
+    gva.accumulate_weights(d, x["q"].cuda(), x["m"].cuda(), x["vc"], x["kc"], x["lens"].cuda(), lse, w, v4_scale=x["sc"],
+                           seen=x["seen"].cuda(), decay=0.0)
+    nan = torch.zeros(2, T, dtype=torch.bool)
+    nan[0, 37] = True
+    assert torch.equal(torch.isnan(w).cpu(), nan)
+
+
+@gpu
 def test_two_streams_at_once():
     """A step, its weights and an eviction on each of two streams, with buffers
     of their own, give what they give one after the other."""
