@@ -30,6 +30,10 @@
  * A value cache may be held in 4 bits (gva_q4_append_kv, gva_q4_decode_step,
  * gva_q4_unpack_kv), and rows may be evicted from a cache by the attention
  * weight that they drew (gva_accumulate_weights, gva_evict_rows).
+ * Many requests are served from one pool of pages by gva_page_tables (block
+ * tables and slot maps), gva_append_slots, gva_packed_prefill (prompts of
+ * different lengths in one call), gva_tree_attention (trees of drafted tokens)
+ * and gva_tree_commit.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -615,6 +619,143 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
                    void* v4_scale, void* kr_cache, const int32_t* lens, const int32_t* seen, const float* weights,
                    const int32_t* row_pos, int32_t* new_lens, float* new_weights, int32_t* new_row_pos,
                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ------------------------------------------ many requests on one pool of pages
+ * Packed rows.  The new rows, or queries, of all sequences lie one behind the
+ * other: those of sequence b are rows cu_rows[b] .. cu_rows[b+1] - 1 of n_rows
+ * (cu_rows [B+1] int32, not decreasing; read as if clamped to [0, n_rows]).  A
+ * sequence may have none.  Rows outside cu_rows[0] .. cu_rows[B] - 1 belong to
+ * none (a batch padded to a fixed n_rows, as a captured graph replays it).
+ * A slot is a row of the pools: slot s is row s % page_rows of page
+ * s / page_rows; -1 stands for none.  n_pages * page_rows < 2^31.
+ *
+ * A step is gva_page_tables for the rows to come, gva_append_slots for their
+ * values and keys, gva_packed_prefill or gva_tree_attention for their queries
+ * (or gva_paged_decode_attention where every sequence has one), and after a tree
+ * gva_tree_commit and gva_page_tables with what the tree has lost.
+ */
+
+/*
+ * gva_page_tables -- block tables and slot maps from the requests' lengths.
+ * n_new[b] rows are to join sequence b, or, where it is negative, -n_new[b] of
+ * its last rows to go (all of them: it has ended), with lens[b] before the call
+ * (n_new is read as clamped to [-lens[b], T]).  With pages(x) = ceil(x /
+ * page_rows) a sequence holds block_table[b][0 .. pages(lens[b]) - 1], and the
+ * stack free_pages [n_pages], of n_free[0] entries, the pages that none holds.
+ *   back   the pages of rows that go are put on the stack, in order of sequence
+ *          and page; of a page some rows of which stay, nothing changes
+ *   grant  then the sequences that grow take theirs from its top, in order of
+ *          sequence and page.  Nobody overtakes: a sequence gets its pages if it
+ *          needs none, or if the stack holds what it and all growing ones before
+ *          it need.  One that would pass T rows gets none and counts for none.
+ * Written: the entries of new pages in block_table (others are left as they
+ * were), free_pages, new_n_free[0], and
+ *   new_lens[b]  lens[b] + n_new[b], or lens[b] where nothing was granted
+ *   cu_rows      the packed offsets of the rows to come, max(n_new, 0) of each
+ *                sequence whether granted or not (at most n_rows)
+ *   seq, row, slot [n_rows]  of each packed row its sequence (-1 past the last),
+ *                its row in it, from lens[b] on, and its slot; row and slot are -1
+ *                where nothing was granted, and so is the slot where the table names
+ *                no page of the pool.  seq and row are what gva_paged_append_kv
+ *                takes, slot and row (the position) what gva_append_slots takes: both
+ *                skip rows of -1.  Each of the three may be NULL.
+ * lens, n_new and n_free are only read, so the call can be repeated with the
+ * same result; new_lens, cu_rows and new_n_free must not overlap them.  dims gives
+ * batch (<= 65535) and t_max = max_pages * page_rows; its other entries are
+ * checked as everywhere, and not used.
+ */
+int gva_page_tables(const gva_dims* dims, const gva_paging* paging, const int32_t* lens, const int32_t* n_new,
+                    int32_t* block_table, int32_t* free_pages, const int32_t* n_free, int32_t n_rows, int32_t* new_lens,
+                    int32_t* new_n_free, int32_t* cu_rows, int32_t* seq, int32_t* row, int32_t* slot, void* stream);
+
+/*
+ * gva_append_slots -- gva_paged_append_kv (bf16 or fp32 pools) with the place in
+ * the pools given, apart from the position: new row r goes to slot[r], its
+ * positional key rotated at pos[r].  Drafted tokens need both: a tree's nodes
+ * stand in rows of their own at positions that they share.  Rows whose slot is
+ * outside the pools are skipped; two rows naming the same slot race.
+ */
+int gva_append_slots(const gva_dims* dims, const gva_paging* paging, void* v_pool, void* kr_pool, const void* v_new,
+                     const void* kr_new, const int32_t* slot, const int32_t* pos, int32_t n_rows, void* stream);
+
+/*
+ * gva_packed_prefill -- causal attention of packed queries: the n_b of sequence
+ * b are its last n_b cached rows, as in gva_prefill, but every sequence has its
+ * own n_b (0, one token of a decode step, a prompt), on contiguous caches
+ * (paging and block_table NULL) or paged ones.  Query i stands at position
+ * p = L_b - n_b + i and sees rows 0..p:
+ *   x_t       = scale * ( q~ . V[b][g(h)][t] + q^rope . kr[b][t] ),  t <= p
+ *   o[r][h]   = sum_t softmax(x)_t V[b][g(h)][t]        in the storage dtype
+ *   lse[r][h] = log sum_t exp(x_t)                      fp32; lse may be NULL
+ * Queries with p < 0 get o = 0, lse = -inf; rows of o and lse that no sequence
+ * has are left as they were.  An infinity or a NaN in a row that a query does not
+ * see does not reach it.
+ * o is in the storage dtype, half of the bytes, because what follows a prompt's
+ * rows is a matrix product in that type.  bf16: the queries enter the products
+ * as bf16 high + low pairs, the softmax weights as bf16 (off by at most 2^-8 each,
+ * as o's own rounding is); lse has no part of the latter.  fp32: fp32 products throughout.
+ * q [n_rows][H][d_c+d_r], M [H][d_v][d_c]; o [n_rows][H][d_v], lse [n_rows][H].
+ * num_splits, split_rows: a sequence's rows are divided as in
+ * gva_decode_attention (any plan is right for any lengths).
+ * Supported: d_v in {64, 128}, d_c a multiple of 32 (<= 512), d_r one of 8
+ * (<= 64), H/G in {1, 2, 4, 8}, n_rows <= 2^20, and what the caches' layout
+ * takes.  Others: GVA_ERR_UNSUPPORTED.  Pointers 16-byte aligned (int32 arrays
+ * and lse 4).  The caches are read only.
+ * gva_packed_workspace_size -- the bytes of `workspace` that the two attention
+ * calls need for the same dims, n_rows and num_splits on the current device:
+ * scratch, 256-byte aligned (0 bytes: may be NULL).  Calls that run at the same
+ * time need one each.
+ * gva_packed_pick_splits -- host heuristic: the split plan for the lengths and
+ * counts of new rows in the HOST arrays lens and n_new [B] (NULL: every sequence
+ * t_max; n_rows shared evenly), on a device with n_cu compute units (0 = ask the
+ * current device).  Returns num_splits, and in split_rows what to pass with it
+ * (NULL: even splits only); 1 for dims that the calls do not take.  Pure host code.
+ */
+int gva_packed_workspace_size(const gva_dims* dims, int32_t n_rows, int32_t num_splits, size_t* bytes);
+int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int32_t* n_new, int32_t n_rows, int32_t n_cu,
+                           int32_t* split_rows);
+int gva_packed_prefill(const gva_dims* dims, const gva_paging* paging, const void* q, const void* m, const void* v_cache,
+                       const void* kr_cache, const int32_t* block_table, const int32_t* lens, const int32_t* cu_rows,
+                       int32_t n_rows, int32_t num_splits, int32_t split_rows, void* workspace, size_t workspace_bytes,
+                       void* o, float* lse, void* stream);
+
+/* Largest tree that gva_tree_attention and gva_tree_commit take. */
+#define GVA_MAX_TREE 256
+
+/*
+ * gva_tree_attention -- gva_packed_prefill for trees of drafted tokens.  The n_b
+ * nodes of sequence b's tree are its last n_b cached rows, in an order in which
+ * a node follows its parent; parent [n_rows] int32 is a node's parent, counted
+ * from the sequence's first node, -1 where it hangs on the last row before the
+ * tree (read as -1 unless 0 <= parent < own index).  Node i sees the L_b - n_b rows
+ * before the tree, its ancestors and itself, and its query is rotated at
+ * position L_b - n_b + its depth (0 for parent -1), the position at which its row
+ * must have been appended.  A sequence of more than GVA_MAX_TREE nodes gets
+ * o = 0, lse = -inf for all of them.
+ */
+int gva_tree_attention(const gva_dims* dims, const gva_paging* paging, const void* q, const void* m, const void* v_cache,
+                       const void* kr_cache, const int32_t* block_table, const int32_t* lens, const int32_t* cu_rows,
+                       const int32_t* parent, int32_t n_rows, int32_t num_splits, int32_t split_rows, void* workspace,
+                       size_t workspace_bytes, void* o, float* lse, void* stream);
+
+/*
+ * gva_tree_commit -- keep the path to one node of every tree: with leaf[b] the
+ * accepted node (-1, or no node of the tree: none) and a_0 < a_1 < .. the path
+ * from the root to it, row L_b - n_b + a_k moves to row L_b - n_b + k, values and
+ * positional key (stored rotated at that position already), and
+ *   new_lens[b]            = L_b - n_b + (nodes of the path)
+ *   accepted[cu_rows[b]+k] = a_k, -1 past the path   (may be NULL)
+ * Rows from new_lens[b] on hold what is left of the tree; the pages that only
+ * they used come back by gva_page_tables.  Nothing moves, new_lens is
+ * max(L_b - n_b, 0) and accepted -1, for trees of more than GVA_MAX_TREE nodes or more than
+ * L_b.  bf16 or fp32 caches of any shape that the tiled layout takes, contiguous
+ * (paging and block_table NULL) or paged; rows whose page is not in the pool are
+ * skipped.  new_lens must not overlap lens.  Not repeatable: the rows have moved.
+ */
+int gva_tree_commit(const gva_dims* dims, const gva_paging* paging, void* v_cache, void* kr_cache, const int32_t* block_table,
+                    const int32_t* lens, const int32_t* cu_rows, const int32_t* parent, const int32_t* leaf, int32_t n_rows,
+                    int32_t* new_lens, int32_t* accepted, void* stream);
 
 /* Human-readable name of a gva_status value (static storage). */
 const char* gva_status_string(int status);

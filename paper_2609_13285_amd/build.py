@@ -2,7 +2,7 @@
 
 ``python -m paper_2609_13285_amd.build`` compiles the kernel sources under
 ``csrc/`` (decode path, ordinary-RoPE contrast path, causal prefill, the 4-bit
-cache, eviction, and the read-bandwidth probe) to objects in parallel and links them into
+cache, eviction, packed and tree attention, page tables, and the read-bandwidth probe) to objects in parallel and links them into
 ``paper_2609_13285_amd/libgva.so``.  Packed-FP32 instructions are disabled for
 the device code (``-packed-fp32-ops``); hipcc's host pass warns that it does
 not know that feature, which is harmless.
@@ -20,7 +20,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SRCS = [os.path.join(CSRC, f) for f in ("gva_decode.hip", "gva_rope.hip", "gva_prefill.hip", "gva_q4.hip",
-                                           "gva_evict.hip", "probe.hip")]
+                                           "gva_evict.hip", "gva_window.hip", "gva_pages.hip", "probe.hip")]
 LIB = os.path.join(HERE, "libgva.so")
 ARCH = "gfx950"
 FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

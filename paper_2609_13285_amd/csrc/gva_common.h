@@ -41,6 +41,7 @@ struct AppendParams {
   const int32_t* seq;
   const int32_t* pos;           // the rotation's position
   const int32_t* row;           // the place in the cache (NULL: pos)
+  const int32_t* slot;          // or the row of a pool: row slot % t_max of stream slot / t_max (seq, row NULL)
   int32_t* row_pos;             // optional: the positions of cached rows
   int32_t B, G, t_max, d_v, d_r, n_rows;
   const int32_t* block_table;   // paged caches (NULL: contiguous streams)
@@ -557,6 +558,16 @@ inline int check_q4_dims(const gva_dims* d) {
   if (d->dtype != GVA_DTYPE_BF16 || (d->d_v != 64 && d->d_v != 128)) return GVA_ERR_UNSUPPORTED;
   if (d->t_max % kTileRows != 0 || d->d_r % 8 != 0 || d->d_r > 64) return GVA_ERR_UNSUPPORTED;
   return check_cache_layout(d);
+}
+
+// A pool of pages that holds a sequence's t_max rows.
+inline int check_pool(const gva_dims* d, const gva_paging* pg) {
+  if (pg == nullptr) return GVA_ERR_INVALID_ARG;
+  if (pg->page_rows < kTileRows || pg->page_rows % kTileRows != 0) return GVA_ERR_INVALID_ARG;
+  if (pg->max_pages < 1 || pg->n_pages < 1) return GVA_ERR_INVALID_ARG;
+  if ((long long)pg->max_pages * pg->page_rows != d->t_max) return GVA_ERR_INVALID_ARG;
+  if (pg->max_pages > kMaxPages) return GVA_ERR_UNSUPPORTED;
+  return GVA_OK;
 }
 
 inline void fill_inv_freq(const gva_dims* d, double* out) {

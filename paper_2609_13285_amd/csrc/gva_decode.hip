@@ -46,7 +46,7 @@
 #include <mutex>
 #include <type_traits>
 
-#include "gva_common.h"
+#include "gva_window.h"
 
 namespace {
 
@@ -107,6 +107,13 @@ __device__ __forceinline__ bool append_place(const AppendParams& p, int b, int p
   return true;
 }
 
+// The place of new row r, whose row in its sequence is rows[r].
+__device__ __forceinline__ bool append_place_of(const AppendParams& p, int r, const int32_t* rows, AppendPlace& at) {
+  if (p.slot == nullptr) return append_place(p, p.seq[r], rows[r], at);
+  const int s = p.slot[r];
+  return s >= 0 && append_place(p, s / p.t_max, s % p.t_max, at);
+}
+
 template <typename T, int KP>
 __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
   constexpr int P = 16 / sizeof(T);
@@ -129,7 +136,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
 #pragma unroll
       for (int k = 0; k < KP; ++k)
         if (c0 + 4 * k < npc) piece[k] = src[c0 + 4 * k];
-      if (!append_place(p, p.seq[r], rows[r], at)) return;
+      if (!append_place_of(p, r, rows, at)) return;
       if (p.row_pos != nullptr && g == 0 && c0 == 0) p.row_pos[(int64_t)p.seq[r] * p.t_max + rows[r]] = p.pos[r];
       T* stream = static_cast<T*>(p.v_cache) + at.vstream0 + g * at.vstride + tiled_off<T>(at.row, c0 * P, p.d_v);
       constexpr int kStep = 4 * kLayoutRows * P; // elements between pieces c and c + 4 of a row
@@ -148,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
   const T* kin = static_cast<const T*>(p.kr_new) + (int64_t)r * p.d_r + 2 * i;
   const double k0 = load_elem<T>(kin, 0), k1 = load_elem<T>(kin, 1);
   const int ps = p.pos[r];
-  if (!append_place(p, p.seq[r], rows[r], at)) return;
+  if (!append_place_of(p, r, rows, at)) return;
   double y0, y1;
   rotate_pair(k0, k1, (double)ps * p.inv_freq[i], y0, y1);
   T* kstream = static_cast<T*>(p.kr_cache) + at.kstream0;
@@ -258,7 +265,7 @@ __global__ void __launch_bounds__(kThreads) absorb_bf16_kernel(AbsorbParams p) {
     }
   }
   // the positional pairs of the workgroup's rows: 16 RB d_r / 2 tasks
-  const int npair = p.d_r / 2;
+  const int npair = p.q_rot != nullptr ? p.d_r / 2 : 0;
   for (int task = tid; task < 16 * RB * npair; task += kThreads) {
     const int pb = b0 + task / npair, pi = task % npair;
     if (pb >= p.B) break;
@@ -328,6 +335,7 @@ __global__ void __launch_bounds__(128) absorb_f32_kernel(AbsorbParams p) {
   for (int i = threadIdx.x; i < p.d_v; i += blockDim.x) {
     p.q_abs[(int64_t)bh * p.d_v + i] = dot_f32(q, m + (int64_t)i * p.d_c, p.d_c);
   }
+  if (p.q_rot == nullptr) return;
   const int pos = query_pos(p, b);
   for (int i = threadIdx.x; i < p.d_r / 2; i += blockDim.x) {
     double y0, y1;
@@ -1669,15 +1677,16 @@ int absorb_impl(const gva_dims* dims, int n_per_seq, const void* q, const void* 
 
 int append_impl(const gva_dims* dims, const gva_paging* paging, const int32_t* block_table, void* v_cache,
                 void* kr_cache, const void* v_new, const void* kr_new, const int32_t* seq, const int32_t* pos,
-                int32_t n_rows, void* stream, const int32_t* row = nullptr, int32_t* row_pos = nullptr) {
+                int32_t n_rows, void* stream, const int32_t* row = nullptr, int32_t* row_pos = nullptr,
+                const int32_t* slot = nullptr) {
   int st = check_dims(dims);
   if (st != GVA_OK) return st;
   if (n_rows < 0) return GVA_ERR_INVALID_ARG;
   if (n_rows == 0) return GVA_OK;
-  if (!v_cache || !v_new || !seq || !pos) return GVA_ERR_INVALID_ARG;
+  if (!v_cache || !v_new || (!seq && !slot) || !pos) return GVA_ERR_INVALID_ARG;
   if (dims->d_r > 0 && (!kr_cache || !kr_new)) return GVA_ERR_INVALID_ARG;
   if (!aligned(v_cache, 16) || !aligned(v_new, 16) || !aligned(seq, 4) || !aligned(pos, 4) || !aligned(row, 4) ||
-      !aligned(row_pos, 4))
+      !aligned(row_pos, 4) || !aligned(slot, 4))
     return GVA_ERR_INVALID_ARG;
   if (dims->d_r > 0 && (!aligned(kr_cache, 16) || !aligned(kr_new, 4))) return GVA_ERR_INVALID_ARG;
   st = check_cache_layout(dims);
@@ -1691,6 +1700,7 @@ int append_impl(const gva_dims* dims, const gva_paging* paging, const int32_t* b
   p.pos = pos;
   p.row = row;
   p.row_pos = row_pos;
+  p.slot = slot;
   p.B = dims->batch;
   p.G = dims->n_groups;
   p.t_max = dims->t_max;
@@ -1718,11 +1728,9 @@ int append_impl(const gva_dims* dims, const gva_paging* paging, const int32_t* b
 // a block-table row covering the capacity exactly, ids for at most
 // kMaxPages pages per sequence.
 int check_paging(const gva_dims* dims, const gva_paging* pg, const int32_t* block_table) {
-  if (pg == nullptr || block_table == nullptr || !aligned(block_table, 4)) return GVA_ERR_INVALID_ARG;
-  if (pg->page_rows < kTileRows || pg->page_rows % kTileRows != 0) return GVA_ERR_INVALID_ARG;
-  if (pg->max_pages < 1 || pg->n_pages < 1) return GVA_ERR_INVALID_ARG;
-  if ((long long)pg->max_pages * pg->page_rows != dims->t_max) return GVA_ERR_INVALID_ARG;
-  if (pg->max_pages > kMaxPages) return GVA_ERR_UNSUPPORTED;
+  if (block_table == nullptr || !aligned(block_table, 4)) return GVA_ERR_INVALID_ARG;
+  const int st = check_pool(dims, pg);
+  if (st != GVA_OK) return st;
   if (dims->dtype != GVA_DTYPE_BF16) return GVA_ERR_UNSUPPORTED;
   return GVA_OK;
 }
@@ -1935,6 +1943,28 @@ int static_scratch(char** out) {
 
 }  // namespace
 
+int absorb_rows(const gva_dims* dims, int n_rows, const void* q, const void* m, float* q_abs, hipStream_t stream) {
+  AbsorbParams p{};
+  p.q = q;
+  p.m = m;
+  p.q_abs = q_abs;
+  p.B = n_rows;
+  p.H = dims->n_heads;
+  p.d_v = dims->d_v;
+  p.d_c = dims->d_c;
+  p.d_r = dims->d_r;
+  p.t_max = dims->t_max;
+  p.n_per_seq = 1;
+  p.row_blocks = n_rows >= 2048 ? 4 : (n_rows >= 1024 ? 2 : 1);    // as in absorb_impl
+  if (dims->dtype == GVA_DTYPE_BF16) {
+    const int per = 16 * p.row_blocks;
+    hipLaunchKernelGGL(absorb_bf16_kernel, dim3(dims->n_heads, (n_rows + per - 1) / per), dim3(kThreads), 0, stream, p);
+  } else {
+    hipLaunchKernelGGL(absorb_f32_kernel, dim3((unsigned)((long long)n_rows * dims->n_heads)), dim3(128), 0, stream, p);
+  }
+  return launch_status();
+}
+
 extern "C" {
 
 
@@ -2001,6 +2031,21 @@ int gva_paged_append_kv(const gva_dims* dims, const gva_paging* paging, void* v_
   st = check_paging(dims, paging, block_table);
   if (st != GVA_OK) return st;
   return append_impl(dims, paging, block_table, v_pool, kr_pool, v_new, kr_new, seq, pos, n_rows, stream);
+}
+
+int gva_append_slots(const gva_dims* dims, const gva_paging* paging, void* v_pool, void* kr_pool, const void* v_new,
+                     const void* kr_new, const int32_t* slot, const int32_t* pos, int32_t n_rows, void* stream) {
+  int st = check_dims(dims);
+  if (st != GVA_OK) return st;
+  st = check_pool(dims, paging);
+  if (st != GVA_OK) return st;
+  if (n_rows > 0 && !slot) return GVA_ERR_INVALID_ARG;
+  if ((long long)paging->n_pages * paging->page_rows > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
+  gva_dims pool = *dims;                       // a page is a stream of page_rows rows
+  pool.batch = paging->n_pages;
+  pool.t_max = paging->page_rows;
+  return append_impl(&pool, nullptr, nullptr, v_pool, kr_pool, v_new, kr_new, nullptr, pos, n_rows, stream, nullptr, nullptr,
+                     slot);
 }
 
 int gva_gqa_decode_attention(const gva_dims* dims, const void* q, int32_t q_stride,

@@ -1,0 +1,348 @@
+// libgva.so -- many requests on one pool of pages: block tables and slot maps
+// from the requests' lengths (gva_page_tables), and what of a drafted tree is
+// kept (gva_tree_commit).
+
+#include "gva_window.h"
+
+namespace {
+
+// ========================================================== tables and slots
+// One launch, no workspace, no atomics.  Every workgroup adds up what all
+// sequences give back, need and bring (three sums over B, each thread a run of
+// sequences, then a scan over the threads), and then does its share: a wave per
+// sequence for the table and the stack, a thread per packed row for the maps.
+// A row's page, or a page that is handed out, is found from those sums alone,
+// never read back from what another workgroup writes: entry i of the stack is
+// free_pages[i] below the old n_free, where nothing is written, and above it a
+// page of a sequence that shrinks, whose table row nothing is written to either.
+// Bound by latency: loads, scan, search, a dependent load, the stores.
+struct TablesParams {
+  const int32_t* lens;
+  const int32_t* n_new;
+  int32_t* table;
+  int32_t* free_pages;
+  const int32_t* n_free;
+  int32_t* new_lens;
+  int32_t* new_n_free;
+  int32_t* cu;
+  int32_t* seq;
+  int32_t* row;
+  int32_t* slot;
+  int32_t B, t_max, page_rows, max_pages, n_pages, n_rows;
+};
+
+struct Request {
+  int len, n;                   // cached rows, rows to come (or to go)
+  int have, hold;               // pages before and after
+  bool fits;
+};
+
+__device__ __forceinline__ Request request_of(const TablesParams& p, int b) {
+  Request r;
+  r.len = clamp_len(p.lens, b, p.t_max);
+  const int n = p.n_new[b];
+  r.n = n < -r.len ? -r.len : (n > p.t_max ? p.t_max : n);
+  const long long want = (long long)r.len + r.n;
+  r.fits = want <= p.t_max;
+  r.have = (int)(((long long)r.len + p.page_rows - 1) / p.page_rows);
+  r.hold = r.fits ? (int)((want + p.page_rows - 1) / p.page_rows) : r.have;
+  return r;
+}
+
+// What sequences give back, need and bring.
+struct Sums {
+  int back, need;
+  long long rows;
+};
+__device__ __forceinline__ void add_request(Sums& s, const Request& r) {
+  s.back += r.n < 0 ? r.have - r.hold : 0;
+  s.need += r.n > 0 ? r.hold - r.have : 0;
+  s.rows += r.n > 0 ? r.n : 0;
+}
+
+__device__ __forceinline__ long long wave_incl_scan64(long long v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+__global__ void __launch_bounds__(kThreads) page_tables_kernel(TablesParams p) {
+  // of the sequences before each thread's run; at kThreads those of all
+  __shared__ int s_back[kThreads + 1], s_need[kThreads + 1];
+  __shared__ long long s_rows[kThreads + 1];
+  __shared__ Sums s_wave[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int run = (p.B + kThreads - 1) / kThreads;
+  const int old_free = min(max(p.n_free[0], 0), p.n_pages);
+  Sums mine{0, 0, 0};
+  for (int j = 0; j < run; ++j) {
+    const int b = tid * run + j;
+    if (b < p.B) add_request(mine, request_of(p, b));
+  }
+  Sums in{wave_incl_scan(mine.back), wave_incl_scan(mine.need), wave_incl_scan64(mine.rows)};
+  if (lane == 63) s_wave[w] = in;
+  __syncthreads();
+  Sums before{0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k)
+    if (k < w) {
+      before.back += s_wave[k].back;
+      before.need += s_wave[k].need;
+      before.rows += s_wave[k].rows;
+    }
+  s_back[tid + 1] = before.back + in.back;
+  s_need[tid + 1] = before.need + in.need;
+  s_rows[tid + 1] = before.rows + in.rows;
+  if (tid == 0) {
+    s_back[0] = s_need[0] = 0;
+    s_rows[0] = 0;
+  }
+  __syncthreads();
+  const int top = min(old_free + s_back[kThreads], p.n_pages);   // entries of the stack before it is taken from
+
+  // sums of the sequences before b
+  auto before_of = [&](int b) {
+    const int t = b / run;
+    Sums s{s_back[t], s_need[t], s_rows[t]};
+    for (int j = t * run; j < b; ++j) add_request(s, request_of(p, j));
+    return s;
+  };
+  // entry i of the stack
+  auto entry = [&](int i) {
+    if (i < old_free) return p.free_pages[i];
+    int k = i - old_free, lo = 0, hi = kThreads;         // s_back[lo] <= k < s_back[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (s_back[mid] <= k) lo = mid;
+      else hi = mid;
+    }
+    k -= s_back[lo];
+    for (int b = lo * run; b < p.B; ++b) {
+      const Request r = request_of(p, b);
+      const int back = r.n < 0 ? r.have - r.hold : 0;
+      if (k < back) return p.table[(long long)b * p.max_pages + r.hold + k];
+      k -= back;
+    }
+    return -1;
+  };
+  auto granted = [&](const Request& r, const Sums& s) {
+    const int need = r.n > 0 ? r.hold - r.have : 0;
+    return r.fits && (need == 0 || s.need + need <= top);
+  };
+
+  for (int b = blockIdx.x * kWaves + w; b < p.B; b += gridDim.x * kWaves) {
+    const Request r = request_of(p, b);
+    const Sums s = before_of(b);
+    const bool ok = granted(r, s);
+    if (lane == 0) {
+      p.new_lens[b] = r.n > 0 && !ok ? r.len : r.len + r.n;
+      p.cu[b] = (int)(s.rows < p.n_rows ? s.rows : p.n_rows);
+    }
+    int32_t* const entries = p.table + (long long)b * p.max_pages;
+    if (r.n < 0)
+      for (int j = lane; j < r.have - r.hold; j += 64) {
+        const int to = old_free + s.back + j;
+        if (to < p.n_pages) p.free_pages[to] = entries[r.hold + j];
+      }
+    if (r.n > 0 && ok)
+      for (int j = lane; j < r.hold - r.have; j += 64) entries[r.have + j] = entry(top - 1 - s.need - j);
+  }
+  if (blockIdx.x == 0 && tid == 0) p.cu[p.B] = (int)(s_rows[kThreads] < p.n_rows ? s_rows[kThreads] : p.n_rows);
+  // All that is granted: those refused are the last that need any, so it is
+  // the largest sum that fits.
+  if (blockIdx.x == 0 && w == 0) {
+    int given = 0;
+    for (int t = lane; t < kThreads; t += 64) {
+      if (s_need[t] > top) continue;
+      if (s_need[t + 1] <= top) {
+        given = max(given, s_need[t + 1]);
+        continue;
+      }
+      int need = s_need[t];
+      given = max(given, need);
+      for (int b = t * run; b < min((t + 1) * run, p.B); ++b) {
+        const Request r = request_of(p, b);
+        need += r.n > 0 ? r.hold - r.have : 0;
+        if (need <= top) given = max(given, need);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) given = max(given, __shfl_xor(given, o, 64));
+    if (lane == 0) p.new_n_free[0] = top - given;
+  }
+  if (p.seq == nullptr && p.row == nullptr && p.slot == nullptr) return;
+  for (int i = blockIdx.x * kThreads + tid; i < p.n_rows; i += gridDim.x * kThreads) {
+    int seq = -1, row = -1, slot = -1;
+    if (i < s_rows[kThreads]) {
+      int lo = 0, hi = kThreads;                           // s_rows[lo] <= i < s_rows[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (s_rows[mid] <= i) lo = mid;
+        else hi = mid;
+      }
+      Sums s{0, s_need[lo], s_rows[lo]};
+      Request r = request_of(p, seq = min(lo * run, p.B - 1));
+      while (i >= s.rows + max(r.n, 0) && seq < p.B - 1) {
+        add_request(s, r);
+        r = request_of(p, ++seq);
+      }
+      if (granted(r, s)) {
+        row = r.len + (int)(i - s.rows);
+        const int pg = row / p.page_rows;
+        const int id = pg < r.have ? p.table[(long long)seq * p.max_pages + pg] : entry(top - 1 - s.need - (pg - r.have));
+        if (id >= 0 && id < p.n_pages) slot = id * p.page_rows + row % p.page_rows;
+      }
+    }
+    if (p.seq != nullptr) p.seq[i] = seq;
+    if (p.row != nullptr) p.row[i] = row;
+    if (p.slot != nullptr) p.slot[i] = slot;
+  }
+}
+
+// ================================================================== commit
+// A workgroup per sequence and group, and one more for the positional keys.
+// The path is walked from the leaf up by one thread over the parents in LDS and
+// written down from its end.  Rows move toward the front: a_k >= k and the path
+// rises, so row k of the path overwrites only rows that earlier rows of it were
+// read from, or itself; kThreads pieces are read, then written, at a time, in
+// order.  Bound by latency: the parents, the walk, a row's read and write.
+struct CommitParams {
+  void* v;
+  void* kr;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* cu;
+  const int32_t* parent;
+  const int32_t* leaf;
+  int32_t* new_lens;
+  int32_t* accepted;
+  int32_t B, G, t_max, n_rows, v_pieces, kr_pieces;   // 16-byte pieces of a row
+  int32_t page_rows, max_pages, n_pages;
+};
+
+__global__ void __launch_bounds__(kThreads) tree_commit_kernel(CommitParams p) {
+  __shared__ int16_t up[kMaxTree], path[kMaxTree];
+  __shared__ int s_len;
+  const int b = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
+  const int first = min(max(p.cu[b], 0), p.n_rows);
+  const int n = max(min(max(p.cu[b + 1], 0), p.n_rows) - first, 0);
+  const int L = clamp_len(p.lens, b, p.t_max);
+  const int leaf = p.leaf[b];
+  const int P = L - n;
+  const bool takes = n <= kMaxTree && P >= 0 && leaf >= 0 && leaf < n;
+  if (takes) {
+    for (int i = tid; i < n; i += kThreads) {
+      const int a = p.parent[first + i];
+      up[i] = (int16_t)(a >= 0 && a < i ? a : -1);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int len = 0;
+      for (int i = leaf; i >= 0; i = up[i]) path[kMaxTree - ++len] = (int16_t)i;
+      s_len = len;
+    }
+    __syncthreads();
+  }
+  const int len = takes ? s_len : 0;
+  const int16_t* const node = path + kMaxTree - len;        // the k-th from the root
+  if (g == 0) {
+    if (tid == 0) p.new_lens[b] = max(P, 0) + len;
+    if (p.accepted != nullptr)
+      for (int i = tid; i < n; i += kThreads) p.accepted[first + i] = i < len ? node[i] : -1;
+  }
+  // the pieces of a row of this stream, and where row t's piece c lies
+  const bool keys = g == p.G;
+  const int npc = keys ? p.kr_pieces : p.v_pieces;
+  u32x4* const base = static_cast<u32x4*>(keys ? p.kr : p.v);
+  const int rows = p.table != nullptr ? p.page_rows : p.t_max;
+  auto place = [&](int t, int c, long long& at) {
+    long long page = b;
+    if (p.table != nullptr) {
+      page = p.table[(long long)b * p.max_pages + t / rows];
+      if (page < 0 || page >= p.n_pages) return false;
+      t %= rows;
+    }
+    at = ((keys ? page : page * p.G + g) * rows + t / kLayoutRows * kLayoutRows) * npc + c * kLayoutRows + t % kLayoutRows;
+    return true;
+  };
+  const long long total = (long long)len * npc;
+  for (long long i0 = 0; i0 < total; i0 += kThreads) {
+    const long long i = i0 + tid;
+    const int k = (int)(i / npc), c = (int)(i % npc);
+    long long from = 0, to = 0;
+    const bool moves = i < total && node[k] != k && place(P + node[k], c, from) && place(P + k, c, to);
+    u32x4 piece = {0u, 0u, 0u, 0u};
+    if (moves) piece = base[from];
+    __syncthreads();                           // all of these rows have been read
+    if (moves) base[to] = piece;
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int gva_page_tables(const gva_dims* dims, const gva_paging* paging, const int32_t* lens, const int32_t* n_new,
+                    int32_t* block_table, int32_t* free_pages, const int32_t* n_free, int32_t n_rows, int32_t* new_lens,
+                    int32_t* new_n_free, int32_t* cu_rows, int32_t* seq, int32_t* row, int32_t* slot, void* stream) {
+  int st = check_dims(dims);
+  if (st != GVA_OK) return st;
+  st = check_pool(dims, paging);
+  if (st != GVA_OK) return st;
+  if (n_rows < 0) return GVA_ERR_INVALID_ARG;
+  if (!lens || !n_new || !block_table || !free_pages || !n_free || !new_lens || !new_n_free || !cu_rows) return GVA_ERR_INVALID_ARG;
+  for (const void* x : {(const void*)lens, (const void*)n_new, (const void*)block_table, (const void*)free_pages,
+                        (const void*)n_free, (const void*)new_lens, (const void*)new_n_free, (const void*)cu_rows,
+                        (const void*)seq, (const void*)row, (const void*)slot})
+    if (!aligned(x, 4)) return GVA_ERR_INVALID_ARG;
+  const int B = dims->batch;
+  auto apart = [](const int32_t* a, long long na, const int32_t* c, long long nc) { return a + na <= c || c + nc <= a; };
+  for (const int32_t* in : {lens, n_new})
+    if (!apart(new_lens, B, in, B) || !apart(cu_rows, B + 1, in, B) || !apart(new_n_free, 1, in, B)) return GVA_ERR_INVALID_ARG;
+  if (!apart(new_lens, B, n_free, 1) || !apart(cu_rows, B + 1, n_free, 1) || new_n_free == n_free) return GVA_ERR_INVALID_ARG;
+  if (B > 65535 || (long long)paging->n_pages * paging->page_rows > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
+  TablesParams p{lens, n_new, block_table, free_pages, n_free, new_lens, new_n_free, cu_rows, seq, row, slot,
+                 B, dims->t_max, paging->page_rows, paging->max_pages, paging->n_pages, n_rows};
+  const long long by_rows = seq || row || slot ? ((long long)n_rows + kThreads - 1) / kThreads : 0;
+  const long long by_seqs = (B + kWaves - 1) / kWaves;
+  long long grid = by_rows > by_seqs ? by_rows : by_seqs;
+  const long long most = device_cu_count();
+  if (grid > most) grid = most;
+  hipLaunchKernelGGL(page_tables_kernel, dim3((unsigned)grid), dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
+  return launch_status();
+}
+
+int gva_tree_commit(const gva_dims* dims, const gva_paging* paging, void* v_cache, void* kr_cache, const int32_t* block_table,
+                    const int32_t* lens, const int32_t* cu_rows, const int32_t* parent, const int32_t* leaf, int32_t n_rows,
+                    int32_t* new_lens, int32_t* accepted, void* stream) {
+  int st = check_dims(dims);
+  if (st != GVA_OK) return st;
+  if (n_rows < 0 || (paging != nullptr) != (block_table != nullptr)) return GVA_ERR_INVALID_ARG;
+  if (paging != nullptr) {
+    st = check_pool(dims, paging);
+    if (st != GVA_OK) return st;
+  }
+  if (!v_cache || !lens || !cu_rows || !leaf || !new_lens || (dims->d_r > 0 && !kr_cache) || (n_rows > 0 && !parent))
+    return GVA_ERR_INVALID_ARG;
+  if (!aligned(v_cache, 16) || (dims->d_r > 0 && !aligned(kr_cache, 16)) || !aligned(block_table, 4) || !aligned(lens, 4) ||
+      !aligned(cu_rows, 4) || !aligned(parent, 4) || !aligned(leaf, 4) || !aligned(new_lens, 4) || !aligned(accepted, 4))
+    return GVA_ERR_INVALID_ARG;
+  if (new_lens < lens + dims->batch && lens < new_lens + dims->batch) return GVA_ERR_INVALID_ARG;
+  st = check_cache_layout(dims);
+  if (st != GVA_OK) return st;
+  const int streams = dims->n_groups + (dims->d_r > 0 ? 1 : 0);
+  if (streams > 65535) return GVA_ERR_UNSUPPORTED;
+  const int piece = (int)(16 / elem_size(dims));
+  CommitParams p{v_cache, kr_cache, block_table, lens, cu_rows, parent, leaf, new_lens, accepted, dims->batch, dims->n_groups,
+                 dims->t_max, n_rows, dims->d_v / piece, dims->d_r / piece,
+                 paging ? paging->page_rows : 0, paging ? paging->max_pages : 0, paging ? paging->n_pages : 0};
+  hipLaunchKernelGGL(tree_commit_kernel, dim3(dims->batch, streams), dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
+  return launch_status();
+}
+
+}  // extern "C"

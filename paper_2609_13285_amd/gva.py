@@ -29,8 +29,11 @@ EXPORTS = ("gva_append_kv", "gva_absorb_query", "gva_decode_attention", "gva_com
            "gva_prefer_fused", "gva_status_string", "gva_version", "gva_decode_workspace_size", "gva_decode_step", "gva_decode_step_static",
            "gva_q4_append_kv", "gva_append_rows", "gva_q4_unpack_kv", "gva_q4_pick_splits",
            "gva_q4_decode_workspace_size", "gva_q4_decode_step", "gva_weights_workspace_size",
-           "gva_accumulate_weights", "gva_evict_workspace_size", "gva_evict_rows")
+           "gva_accumulate_weights", "gva_evict_workspace_size", "gva_evict_rows", "gva_page_tables",
+           "gva_append_slots", "gva_packed_workspace_size", "gva_packed_pick_splits", "gva_packed_prefill",
+           "gva_tree_attention", "gva_tree_commit")
 GVA_MAX_PAGES = 4096
+GVA_MAX_TREE = 256
 PROBE_EXPORTS = ("gva_probe_read",)      # include/gva_probe.h
 
 
@@ -102,6 +105,13 @@ def lib() -> ctypes.CDLL:
         L.gva_accumulate_weights.argtypes = [D, I32, P, P, P, P, P, P, P, P, ctypes.c_double, P, P, P, SZ, P]
         L.gva_evict_workspace_size.argtypes = [D, SZP]
         L.gva_evict_rows.argtypes = [D, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P]
+        L.gva_page_tables.argtypes = [D, PG, P, P, P, P, P, I32, P, P, P, P, P, P, P]
+        L.gva_append_slots.argtypes = [D, PG, P, P, P, P, P, P, I32, P]
+        L.gva_packed_workspace_size.argtypes = [D, I32, I32, SZP]
+        L.gva_packed_pick_splits.argtypes = [D, P, P, I32, I32, ctypes.POINTER(I32)]
+        L.gva_packed_prefill.argtypes = [D, PG, P, P, P, P, P, P, P, I32, I32, I32, P, SZ, P, P, P]
+        L.gva_tree_attention.argtypes = [D, PG, P, P, P, P, P, P, P, P, I32, I32, I32, P, SZ, P, P, P]
+        L.gva_tree_commit.argtypes = [D, PG, P, P, P, P, P, P, P, I32, P, P, P]
         L.gva_status_string.argtypes = [ctypes.c_int]
         L.gva_status_string.restype = ctypes.c_char_p
         L.gva_version.argtypes = []
@@ -114,7 +124,9 @@ def lib() -> ctypes.CDLL:
                      "gva_decode_workspace_size", "gva_decode_step", "gva_decode_step_static",
                      "gva_q4_append_kv", "gva_append_rows", "gva_q4_unpack_kv", "gva_q4_pick_splits",
                      "gva_q4_decode_workspace_size", "gva_q4_decode_step", "gva_weights_workspace_size",
-                     "gva_accumulate_weights", "gva_evict_workspace_size", "gva_evict_rows"):
+                     "gva_accumulate_weights", "gva_evict_workspace_size", "gva_evict_rows", "gva_page_tables",
+                     "gva_append_slots", "gva_packed_workspace_size", "gva_packed_pick_splits", "gva_packed_prefill",
+                     "gva_tree_attention", "gva_tree_commit"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -1054,3 +1066,151 @@ def evict(dims: GvaDims, n_keep: int, v_cache, kr_cache, lens, weights, n_first:
     gva_evict_rows(d, n_keep, n_first, n_recent, v_cache, v4_scale, kr_cache if d.d_r > 0 else None, lens, weights, out[0],
                    out[1], workspace=ws, seen=seen, row_pos=row_pos, new_row_pos=out[2], stream=stream)
     return out
+
+
+# ------------------------------------------ many requests on one pool of pages
+def _pool_ptrs(d: GvaDims, paging: Optional[GvaPaging], v, kr, block_table):
+    """A contiguous cache (paging None) or page pools with their table."""
+    dt = d.torch_dtype
+    if paging is None:
+        if block_table is not None:
+            raise ValueError("block_table given without paging")
+        return (_ptr(v, "v_cache", dt, (d.batch, d.n_groups, d.t_max, d.d_v)),
+                _ptr(kr, "kr_cache", dt, (d.batch, d.t_max, d.d_r)), None)
+    if block_table is None:
+        raise ValueError("paged caches need a block_table")
+    return (_ptr(v, "v_pool", dt, (paging.n_pages, d.n_groups, paging.page_rows, d.d_v)),
+            _ptr(kr, "kr_pool", dt, (paging.n_pages, paging.page_rows, d.d_r)),
+            _ptr(block_table, "block_table", torch.int32, (d.batch, paging.max_pages)))
+
+
+def _paging_ref(paging: Optional[GvaPaging]):
+    return None if paging is None else ctypes.byref(paging)
+
+
+def gva_page_tables(dims: GvaDims, paging: GvaPaging, lens, n_new, block_table, free_pages, n_free, new_lens, new_n_free,
+                    cu_rows, seq=None, row=None, slot=None, n_rows: Optional[int] = None, stream=None):
+    """Pages returned and handed out for n_new rows of each sequence (negative:
+    rows that go), block_table and the stack free_pages updated; new lengths,
+    packed offsets and per packed row its sequence, row and slot.  ``n_rows`` is
+    the size of seq, row and slot (needed only where none is given)."""
+    d, B = dims, dims.batch
+    _here(lens, n_new, block_table, free_pages, n_free, new_lens, new_n_free, cu_rows, seq, row, slot)
+    maps = [t for t in (seq, row, slot) if t is not None]
+    if maps:
+        n = maps[0].numel() if n_rows is None else int(n_rows)
+    elif n_rows is None:
+        raise ValueError("n_rows is needed where none of seq, row and slot is given")
+    else:
+        n = int(n_rows)
+    i32 = torch.int32
+    st = lib().gva_page_tables(
+        ctypes.byref(d), ctypes.byref(paging), _ptr(lens, "lens", i32, (B,)), _ptr(n_new, "n_new", i32, (B,)),
+        _ptr(block_table, "block_table", i32, (B, paging.max_pages)),
+        _ptr(free_pages, "free_pages", i32, (paging.n_pages,)), _ptr(n_free, "n_free", i32, (1,)), n,
+        _ptr(new_lens, "new_lens", i32, (B,)), _ptr(new_n_free, "new_n_free", i32, (1,)),
+        _ptr(cu_rows, "cu_rows", i32, (B + 1,)), _ptr(seq, "seq", i32, (n,)), _ptr(row, "row", i32, (n,)),
+        _ptr(slot, "slot", i32, (n,)), _stream(stream))
+    _check("gva_page_tables", st)
+
+
+def gva_append_slots(dims: GvaDims, paging: GvaPaging, v_pool, kr_pool, v_new, kr_new, slot, pos, stream=None):
+    """New row r into slot[r] of the pools, its positional key rotated at pos[r]."""
+    d, n = dims, slot.numel()
+    dt = d.torch_dtype
+    _here(v_pool, kr_pool, v_new, kr_new, slot, pos)
+    st = lib().gva_append_slots(
+        ctypes.byref(d), ctypes.byref(paging),
+        _ptr(v_pool, "v_pool", dt, (paging.n_pages, d.n_groups, paging.page_rows, d.d_v)),
+        _ptr(kr_pool, "kr_pool", dt, (paging.n_pages, paging.page_rows, d.d_r)),
+        _ptr(v_new, "v_new", dt, (n, d.n_groups, d.d_v)), _ptr(kr_new, "kr_new", dt, (n, d.d_r)),
+        _ptr(slot, "slot", torch.int32, (n,)), _ptr(pos, "pos", torch.int32, (n,)), n, _stream(stream))
+    _check("gva_append_slots", st)
+
+
+def gva_packed_workspace_size(dims: GvaDims, n_rows: int, num_splits: int = 1) -> int:
+    return _bytes("gva_packed_workspace_size", ctypes.byref(dims), int(n_rows), int(num_splits))
+
+
+def packed_workspace_for(dims: GvaDims, n_rows: int, num_splits: int = 1, device="cuda") -> Optional[torch.Tensor]:
+    """A device buffer for gva_packed_prefill and gva_tree_attention (None when they need none)."""
+    return _scratch(gva_packed_workspace_size(dims, n_rows, num_splits), device)
+
+
+def gva_packed_pick_splits(dims: GvaDims, lens=None, n_new=None, n_rows: Optional[int] = None, n_cu: int = 0,
+                           chunked: bool = True) -> Tuple[int, int]:
+    """(num_splits, split_rows) of the packed attention calls for the lengths
+    ``lens`` and the queries ``n_new`` of each sequence (copied to the host; None:
+    full sequences, ``n_rows`` shared evenly)."""
+    def host(t, name):
+        if t is None:
+            return None
+        t = t.detach().to("cpu", torch.int32).contiguous()
+        if tuple(t.shape) != (dims.batch,):
+            raise ValueError(f"{name} must have shape {(dims.batch,)}, got {tuple(t.shape)}")
+        return t
+    hl, hn = host(lens, "lens"), host(n_new, "n_new")
+    if n_rows is None:
+        if hn is None:
+            raise ValueError("n_rows is needed where n_new is not given")
+        n_rows = int(hn.clamp(min=0).sum())
+    rows = ctypes.c_int32(0)
+    S = lib().gva_packed_pick_splits(ctypes.byref(dims), None if hl is None else ctypes.c_void_p(hl.data_ptr()),
+                                     None if hn is None else ctypes.c_void_p(hn.data_ptr()), int(n_rows), int(n_cu),
+                                     ctypes.byref(rows) if chunked else None)
+    return int(S), int(rows.value)
+
+
+def packed_plan_for(dims: GvaDims, lens, n_new, n_rows: Optional[int] = None, n_cu: int = 0) -> Tuple[int, int]:
+    """gva_packed_pick_splits for the lengths in ``lens`` and ``n_new`` (host copies)."""
+    return gva_packed_pick_splits(dims, lens, n_new, n_rows, n_cu)
+
+
+def _packed_args(d: GvaDims, paging, q, m, v, kr, block_table, lens, cu_rows, o, lse, workspace):
+    dt = d.torch_dtype
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a [n_rows, H, d_c + d_r] tensor")
+    n = q.shape[0]
+    _here(q, m, v, kr, block_table, lens, cu_rows, o, lse, workspace)
+    pv, pk, pt = _pool_ptrs(d, paging, v, kr, block_table)
+    head = [ctypes.byref(d), _paging_ref(paging), _ptr(q, "q", dt, (n, d.n_heads, d.d_c + d.d_r)),
+            _ptr(m, "m", dt, (d.n_heads, d.d_v, d.d_c)), pv, pk, pt, _ptr(lens, "lens", torch.int32, (d.batch,)),
+            _ptr(cu_rows, "cu_rows", torch.int32, (d.batch + 1,))]
+    tail = [*_workspace(workspace), _ptr(o, "o", dt, (n, d.n_heads, d.d_v)), _ptr(lse, "lse", torch.float32, (n, d.n_heads))]
+    return n, head, tail
+
+
+def gva_packed_prefill(dims: GvaDims, q, m, v, kr, lens, cu_rows, o, lse=None, paging=None, block_table=None,
+                       num_splits: int = 1, split_rows: int = 0, workspace=None, stream=None):
+    """Causal attention of packed queries [n_rows, H, d_c+d_r], each sequence's
+    its last cached rows, on contiguous caches or (paging given) paged ones.  o is
+    in the storage dtype."""
+    n, head, tail = _packed_args(dims, paging, q, m, v, kr, block_table, lens, cu_rows, o, lse, workspace)
+    st = lib().gva_packed_prefill(*head, n, int(num_splits), int(split_rows), *tail, _stream(stream))
+    _check("gva_packed_prefill", st)
+
+
+def gva_tree_attention(dims: GvaDims, q, m, v, kr, lens, cu_rows, parent, o, lse=None, paging=None, block_table=None,
+                       num_splits: int = 1, split_rows: int = 0, workspace=None, stream=None):
+    """gva_packed_prefill for trees of drafted tokens: node i of a sequence sees
+    the rows before the tree, its ancestors by ``parent`` and itself."""
+    n, head, tail = _packed_args(dims, paging, q, m, v, kr, block_table, lens, cu_rows, o, lse, workspace)
+    _here(parent)
+    st = lib().gva_tree_attention(*head, _ptr(parent, "parent", torch.int32, (n,)), n, int(num_splits), int(split_rows),
+                                  *tail, _stream(stream))
+    _check("gva_tree_attention", st)
+
+
+def gva_tree_commit(dims: GvaDims, v, kr, lens, cu_rows, parent, leaf, new_lens, accepted=None, paging=None,
+                    block_table=None, stream=None):
+    """Keep the path to node leaf[b] of every tree: its rows move to the front."""
+    d = dims
+    n = parent.numel()
+    _here(v, kr, block_table, lens, cu_rows, parent, leaf, new_lens, accepted)
+    pv, pk, pt = _pool_ptrs(d, paging, v, kr, block_table)
+    i32 = torch.int32
+    st = lib().gva_tree_commit(
+        ctypes.byref(d), _paging_ref(paging), pv, pk, pt, _ptr(lens, "lens", i32, (d.batch,)),
+        _ptr(cu_rows, "cu_rows", i32, (d.batch + 1,)), _ptr(parent, "parent", i32, (n,)), _ptr(leaf, "leaf", i32, (d.batch,)),
+        n, _ptr(new_lens, "new_lens", i32, (d.batch,)), _ptr(accepted, "accepted", i32, (n,)), _stream(stream))
+    _check("gva_tree_commit", st)
