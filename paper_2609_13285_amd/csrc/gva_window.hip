@@ -55,10 +55,10 @@ struct WindowParams {
   float* o_part;                // [n_rows][H][S][d_v] (more splits)
   float* lse_part;              // [n_rows][H][S]
   int32_t B, H, G, d_c, d_r, t_max, n_rows, S, split_rows;
-  int32_t rows;                 // query rows of a workgroup
+  int32_t rows_log2;            // query rows of a workgroup
   int32_t page_rows, max_pages, n_pages;
   float scale_log2;
-  double inv_freq[kMaxPairs];
+  double quarters[kMaxPairs];   // a pair's frequency, in quarter turns a position
 };
 
 // A sequence's window: its first packed row, rows and cached rows.
@@ -68,6 +68,11 @@ struct Window {
 __device__ __forceinline__ Window window_of(const WindowParams& p, int b) {
   const int a = min(max(p.cu[b], 0), p.n_rows), e = min(max(p.cu[b + 1], 0), p.n_rows);
   return Window{a, max(e - a, 0), clamp_len(p.lens, b, p.t_max)};
+}
+
+// blocks of query rows
+__device__ __forceinline__ int window_blocks_of(const WindowParams& p, int n) {
+  return (int)(((unsigned)n + (1u << p.rows_log2) - 1) >> p.rows_log2);
 }
 
 __device__ __forceinline__ int window_splits(const WindowParams& p, int L) {
@@ -105,19 +110,17 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
     }
     // blocks of a sequence below the first with at least t tiles (all, if none)
     auto below = [&](int k, int t) {
-      const int nb = (n[k] + p.rows - 1) / p.rows;
-      const long long key = 32LL * (t - 1) + 1;           // keys that make t tiles
+      const int key = kTileRows * (t - 1) + 1;            // keys that make t tiles
       if (t <= 0) return 0;
-      if (key > (long long)P[k] + n[k]) return nb;
-      const long long need = key - P[k];                  // rows of the window up to the last
-      const int j = need <= 0 ? 0 : (int)((need + p.rows - 1) / p.rows) - 1;
-      return min(max(j, 0), nb);
+      if (key > P[k] + n[k]) return window_blocks_of(p, n[k]);
+      const int need = key - P[k];                        // rows of the window up to the last
+      return need <= 0 ? 0 : (need - 1) >> p.rows_log2;
     };
     auto at_least = [&](int t) {
       int c = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (64 * k < p.B) c += (n[k] + p.rows - 1) / p.rows - below(k, t);
+        if (64 * k < p.B) c += window_blocks_of(p, n[k]) - below(k, t);
       return wave_sum_dpp(c);
     };
     if (i >= at_least(0)) return false;
@@ -150,7 +153,7 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
   auto items = [&](int bb) {
     if (bb >= p.B) return 0;
     const Window w = window_of(p, bb);
-    return (w.n + p.rows - 1) / p.rows * window_splits(p, w.L);
+    return window_blocks_of(p, w.n) * window_splits(p, w.L);
   };
   int sum = 0;
   for (int j = 0; j < k; ++j) sum += items(lane * k + j);
@@ -170,7 +173,7 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
     }
     local -= __builtin_amdgcn_readlane(in2, 63);
   }
-  const int nb = (window_of(p, b).n + p.rows - 1) / p.rows;
+  const int nb = window_blocks_of(p, window_of(p, b).n);
   s = __builtin_amdgcn_readfirstlane(local / nb);
   blk = __builtin_amdgcn_readfirstlane(local % nb);
   return true;
@@ -253,6 +256,32 @@ __device__ __forceinline__ bf16x8 take_part(float* x) {
 
 // row of a 32-row tile in score register r of a lane in half h
 __device__ __forceinline__ constexpr int score_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// A pair rotated by an angle in quarter turns.  The whole quarters come off in 64
+// bits, exactly; sine and cosine of the rest, at most pi/4, are their power series up
+// to x^9 and x^10 (what follows is below 2e-9 of either), in fp32 as the scores are.
+__device__ __forceinline__ void rotate_quarters(float x0, float x1, double quarters, float& y0, float& y1) {
+  const double whole = rint(quarters);
+  const float x = (float)(quarters - whole) * 1.57079632679489661923f, z = x * x;
+  const float si = x + x * z * fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f);
+  const float co = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  const int k = (int)whole;
+  float s = (k & 1) ? co : si, c = (k & 1) ? si : co;
+  if (k & 2) s = -s;
+  if ((k + 1) & 2) c = -c;
+  y0 = x0 * c - x1 * s;
+  y1 = x0 * s + x1 * c;
+}
+
+// -inf for the scores whose row has no bit in `sees`, the tile's rows from the
+// lane's first on.
+__device__ __forceinline__ void hide(f32x16& sn, uint32_t sees) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)sees, score_row(r, 0), 1);      // all ones or none
+    sn[r] = __uint_as_float((__float_as_uint(sn[r]) & keep) | (0xFF800000u & ~keep));
+  }
+}
 
 // A running maximum moves when a column's tile maximum exceeds it by more
 // than this (log2 units): weights stay below 2^8, which costs a sum in fp32 and
@@ -337,18 +366,18 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
 
   const Window win = window_of(p, b);
   const int P = win.L - win.n;                 // rows before the window (negative: some of it has no row)
-  const int ppb = p.rows;
-  const int i0 = blk * ppb, i1 = min(win.n, i0 + ppb);
+  const int lg = p.rows_log2, ppb = 1 << lg;   // query rows of the block
+  const int i0 = blk << lg, i1 = min(win.n, i0 + ppb);
   const bool tree = p.parent != nullptr;
   const bool too_large = tree && win.n > kMaxTree;
 
   // ---- this wave's columns: row i of the window, head.  Head by head, the
   // block's rows of each.
   const int col = 32 * w + n;
-  const int i_col = i0 + col % ppb;
-  const int head = g * hpg + col / ppb;
+  const int i_col = i0 + (col & (ppb - 1));
+  const int head = g * hpg + (col >> lg);
   const bool live_col = i_col < win.n;
-  const bool live = i0 + (32 * w) % ppb < win.n;   // some column of the wave is
+  const bool live = i0 + ((32 * w) & (ppb - 1)) < win.n;   // some column of the wave is
   const int own_row = P + i_col;
   const bool has_row = live_col && own_row >= 0 && !too_large;
   const int packed = win.first + min(i_col, win.n - 1);
@@ -364,7 +393,7 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
   }
   if (too_large) kend = kbeg;
   const int masked_from = tree ? P : P + i0 + 1;
-  const int wave_masked_from = tree ? P : P + i0 + (32 * w) % ppb + 1;
+  const int wave_masked_from = tree ? P : P + i0 + ((32 * w) & (ppb - 1)) + 1;
   const int ntiles = kend > kbeg ? (kend - kbeg + kTileRows - 1) / kTileRows : 0;
   const int nit = (ntiles + KW - 1) / KW;      // the same for all sets (they share the barriers)
   auto tile_row = [&](int j) { return kbeg + (KW * j + grp) * kTileRows; };
@@ -430,7 +459,7 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
   bf16x8 qh[NCH], ql[NCH], q3[NCH], rh[NRC], rl[NRC], r3[NRC];
   auto put_query = [&](bf16x8& hi, bf16x8& lo, bf16x8& third, float* xv) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) xv[j] = has_row ? xv[j] * p.scale_log2 : 0.f;
+    for (int j = 0; j < 8; ++j) xv[j] *= p.scale_log2;
     hi = take_part(xv);
     lo = take_part(xv);
     third = take_part(xv);
@@ -441,42 +470,64 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
     // The absorption on the same products: q~^T[i][col] = sum_k M_h[i][k]
     // q[col][k].  Row m of an A operand is row i(m) of M_h, bits 2 and 3 of m
     // swapped, so that a lane's 16 results of a block are two B operands of the
-    // score product as they lie.  One pass per head of the wave's columns.
+    // score product as they lie.  One pass per head of the wave's columns, each
+    // with the loads of CS chunks of 16 columns ahead of the products.
     f32x16 d[NIB];
     const int mrow = (n & 19) | ((n & 4) << 1) | ((n & 8) >> 1);
-    const int npass = ppb >= 32 ? 1 : 32 / ppb;
-    constexpr int CS = 4;                      // 16-column chunks per load round
-    const int nround = (p.d_c + 16 * CS - 1) / (16 * CS);
-    for (int ps = 0; ps < npass; ++ps) {
-      const bool mine = npass == 1 || n / ppb == ps;
-      const int hd = g * hpg + 32 * w / ppb + ps;
-      const uint16_t* mh = static_cast<const uint16_t*>(p.m) + ((int64_t)hd * DV + mrow) * p.d_c;
-      f32x16 e[NIB];
+    auto absorb = [&](auto cs_tag, int hd, f32x16 (&e)[NIB]) __attribute__((always_inline)) {
+      constexpr int CS = decltype(cs_tag)::value;
+      const uint16_t* const mh = static_cast<const uint16_t*>(p.m) + ((int64_t)hd * DV + mrow) * p.d_c;
+      const int nround = (p.d_c + 16 * CS - 1) / (16 * CS);
+      u32x4 xq[2][CS], xm[2][CS][NIB];
+      auto load = [&](int ro, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < CS; ++c) {         // columns past d_c: any valid ones against zeros
+          const int kc = min(16 * (CS * ro + c) + 8 * h, p.d_c - 8);
+          xq[at][c] = *reinterpret_cast<const u32x4*>(qraw + kc);
+#pragma unroll
+          for (int ib = 0; ib < NIB; ++ib)
+            xm[at][c][ib] = *reinterpret_cast<const u32x4*>(mh + (int64_t)(32 * ib) * p.d_c + kc);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto multiply = [&](int ro, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < CS; ++c) {
+          const bf16x8 bq = 16 * (CS * ro + c) < p.d_c ? as_bf16x8(xq[at][c]) : zero8;
+#pragma unroll
+          for (int ib = 0; ib < NIB; ++ib) e[ib] = mfma32(as_bf16x8(xm[at][c][ib]), bq, e[ib]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
 #pragma unroll
       for (int ib = 0; ib < NIB; ++ib)
 #pragma unroll
         for (int r = 0; r < 16; ++r) e[ib][r] = 0.f;
-      for (int ro = 0; ro < nround; ++ro) {
-        u32x4 xq[CS], xm[CS][NIB];
-#pragma unroll
-        for (int c = 0; c < CS; ++c) {         // columns past d_c: any valid ones against zeros
-          const int kc = min(16 * (CS * ro + c) + 8 * h, p.d_c - 8);
-          xq[c] = *reinterpret_cast<const u32x4*>(qraw + kc);
-#pragma unroll
-          for (int ib = 0; ib < NIB; ++ib)
-            xm[c][ib] = *reinterpret_cast<const u32x4*>(mh + (int64_t)(32 * ib) * p.d_c + kc);
-        }
-#pragma unroll
-        for (int c = 0; c < CS; ++c) {
-          const bf16x8 bq = 16 * (CS * ro + c) < p.d_c ? as_bf16x8(xq[c]) : zero8;
-#pragma unroll
-          for (int ib = 0; ib < NIB; ++ib) e[ib] = mfma32(as_bf16x8(xm[c][ib]), bq, e[ib]);
+      load(0, 0);
+#pragma unroll 1
+      for (int ro = 0; ro < nround; ro += 2) {
+        if (ro + 1 < nround) load(ro + 1, 1);
+        multiply(ro, 0);
+        if (ro + 1 < nround) {
+          if (ro + 2 < nround) load(ro + 2, 0);
+          multiply(ro + 1, 1);
         }
       }
+    };
+    const int h_first = g * hpg + (32 * w >> lg);
+    if (ppb >= 32) {
+      absorb(std::integral_constant<int, 4>{}, h_first, d);
+    } else {
+#pragma unroll 1
+      for (int ps = 0; ps < 32 >> lg; ++ps) {
+        f32x16 e[NIB];
+        absorb(std::integral_constant<int, 2>{}, h_first + ps, e);
+        const bool mine = (n >> lg) == ps;
 #pragma unroll
-      for (int ib = 0; ib < NIB; ++ib)
+        for (int ib = 0; ib < NIB; ++ib)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) d[ib][r] = ps == 0 || mine ? e[ib][r] : d[ib][r];
+          for (int r = 0; r < 16; ++r) d[ib][r] = ps == 0 || mine ? e[ib][r] : d[ib][r];
+      }
     }
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -503,8 +554,8 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
       const u32x4 raw = *reinterpret_cast<const u32x4*>(qraw + p.d_c + 8 * piece);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        rotate_query_pair(bf16_bits_to_f32(raw[k] & 0xFFFFu), bf16_bits_to_f32(raw[k] >> 16),
-                          (double)pos * p.inv_freq[4 * piece + k], 1.f, xv[2 * k], xv[2 * k + 1]);
+        rotate_quarters(bf16_bits_to_f32(raw[k] & 0xFFFFu), __uint_as_float(raw[k] & 0xFFFF0000u),
+                        (double)pos * p.quarters[4 * piece + k], xv[2 * k], xv[2 * k + 1]);
     }
     put_query(rh[rc], rl[rc], r3[rc], xv);
   }
@@ -562,19 +613,13 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
       *at = u;
     }
   };
-  auto mask = [&](f32x16& sn, int row0) {
+  // scores of rows that the column does not see, and of those past the keys
+  auto mask = [&](f32x16& sn, int row0) __attribute__((always_inline)) {
     if (row0 + kTileRows <= wave_masked_from && row0 + kTileRows <= kend) return;
-    if (tree) {
-      const uint32_t sees = tree_sees(masks + (col % ppb) * kTreeWords, row0 - P);
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!(sees >> score_row(r, h) & 1u) || row0 + score_row(r, h) >= kend) sn[r] = -INFINITY;
-    } else {
-      const int last = min(own_row, kend - 1);
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (row0 + score_row(r, h) > last) sn[r] = -INFINITY;
-    }
+    const int last = (tree ? kend : min(own_row + 1, kend)) - row0;       // rows of the tile up to it
+    uint32_t sees = last >= 32 ? ~0u : last <= 0 ? 0u : (1u << last) - 1u;
+    if (tree) sees &= tree_sees(masks + (col & (ppb - 1)) * kTreeWords, row0 - P);
+    hide(sn, sees >> (4 * h));
   };
   // One tile: scores sn of tile j, beside them the softmax weights of the
   // tile before (scores sp), then that tile's P.V, beside it tile j's maxima.
@@ -700,10 +745,11 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
     }
     if (j < nit) {
       step(std::false_type{}, j, buf, s0, s1);
-      last(j, buf, s1);
-    } else {
-      last(j - 1, buf == 0 ? NBUF - 1 : buf - 1, s0);
+      s0 = s1;
+      ++j;
+      buf = buf == NBUF - 1 ? 0 : buf + 1;
     }
+    last(j - 1, buf == 0 ? NBUF - 1 : buf - 1, s0);
   }
 
   // ---- merge the sets, normalise, write
@@ -772,10 +818,10 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
     for (int it = 0; it < 32 * LPR / 64; ++it) {
       const int c = it * (64 / LPR) + lane / LPR, e = lane % LPR;
       const u32x4 u = *reinterpret_cast<const u32x4*>(ob + c * Cfg::OUT_PITCH + e * 16);
-      const int cc = 32 * w + c, i = i0 + cc % ppb;
+      const int cc = 32 * w + c, i = i0 + (cc & (ppb - 1));
       if (i < win.n)
         *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.o) +
-                                  ((int64_t)(win.first + i) * p.H + g * hpg + cc / ppb) * DV + 8 * e) = u;
+                                  ((int64_t)(win.first + i) * p.H + g * hpg + (cc >> lg)) * DV + 8 * e) = u;
     }
     if (p.lse != nullptr && h == 0 && live_col) p.lse[qrow] = lse;
     return;
@@ -796,10 +842,10 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
     for (int it = 0; it < 4; ++it) {
       const int c = 8 * it + (lane >> 3);
       const f32x4 o = *reinterpret_cast<const f32x4*>(ob + c * Cfg::PART_PITCH + 4 * (lane & 7));
-      const int cc = 32 * w + c, i = i0 + cc % ppb;
+      const int cc = 32 * w + c, i = i0 + (cc & (ppb - 1));
       if (i < win.n)
         *reinterpret_cast<f32x4*>(
-            p.o_part + (((int64_t)(win.first + i) * p.H + g * hpg + cc / ppb) * p.S + split) * DV + 32 * ib + 4 * (lane & 7)) = o;
+            p.o_part + (((int64_t)(win.first + i) * p.H + g * hpg + (cc >> lg)) * p.S + split) * DV + 32 * ib + 4 * (lane & 7)) = o;
     }
   }
   if (h == 0 && live_col) {
@@ -839,15 +885,15 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
 
   const Window win = window_of(p, b);
   const int P = win.L - win.n;
-  const int ppb = p.rows;
-  const int i0 = blk * ppb, i1 = min(win.n, i0 + ppb);
+  const int lg = p.rows_log2, ppb = 1 << lg;   // query rows of the block
+  const int i0 = blk << lg, i1 = min(win.n, i0 + ppb);
   const bool tree = p.parent != nullptr;
   const bool too_large = tree && win.n > kMaxTree;
   const int col = 32 * w + n;
-  const int i_col = i0 + col % ppb;
-  const int head = g * hpg + col / ppb;
+  const int i_col = i0 + (col & (ppb - 1));
+  const int head = g * hpg + (col >> lg);
   const bool live_col = i_col < win.n;
-  const bool live = i0 + (32 * w) % ppb < win.n;
+  const bool live = i0 + ((32 * w) & (ppb - 1)) < win.n;
   const int own_row = P + i_col;
   const bool has_row = live_col && own_row >= 0 && !too_large;
   const int64_t qrow = (int64_t)(win.first + min(i_col, win.n - 1)) * p.H + head;
@@ -899,10 +945,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
   f32x16 qv[NIB];                              // q~, four chunks a block
   f32x4 qr[NR];
   {
-    const int npass = ppb >= 32 ? 1 : 32 / ppb;
+    const int npass = ppb >= 32 ? 1 : 32 >> lg;
     for (int ps = 0; ps < npass; ++ps) {
-      const bool mine = npass == 1 || n / ppb == ps;
-      const float* mh = static_cast<const float*>(p.m) + ((int64_t)(g * hpg + 32 * w / ppb + ps) * DV + n) * p.d_c;
+      const bool mine = npass == 1 || (n >> lg) == ps;
+      const float* mh = static_cast<const float*>(p.m) + ((int64_t)(g * hpg + (32 * w >> lg) + ps) * DV + n) * p.d_c;
       f32x16 e[NIB];
 #pragma unroll
       for (int ib = 0; ib < NIB; ++ib)
@@ -936,9 +982,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           float y0, y1;
-          rotate_query_pair(x[2 * k], x[2 * k + 1], (double)pos * p.inv_freq[i / 2 + k], p.scale_log2, y0, y1);
-          qr[c][2 * k] = y0;
-          qr[c][2 * k + 1] = y1;
+          rotate_quarters(x[2 * k], x[2 * k + 1], (double)pos * p.quarters[i / 2 + k], y0, y1);
+          qr[c][2 * k] = y0 * p.scale_log2;
+          qr[c][2 * k + 1] = y1 * p.scale_log2;
         }
       }
     }
@@ -981,11 +1027,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
     }
     if (masked) {
       if (live) {
-        const uint32_t sees = tree ? tree_sees(masks + (col % ppb) * kTreeWords, row0 - P) : ~0u;
-        const int last = tree ? kend - 1 : min(own_row, kend - 1);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (row0 + score_row(r, h) > last || !(sees >> score_row(r, h) & 1u)) sn[r] = -INFINITY;
+        const int last = (tree ? kend : min(own_row + 1, kend)) - row0;
+        uint32_t sees = last >= 32 ? ~0u : last <= 0 ? 0u : (1u << last) - 1u;
+        if (tree) sees &= tree_sees(masks + (col & (ppb - 1)) * kTreeWords, row0 - P);
+        hide(sn, sees >> (4 * h));
       }
       __syncthreads();                         // every wave has its scores
       for (int i = tid; i < V_BYTES / 16; i += kThreads) {
@@ -1059,9 +1104,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
     for (int it = 0; it < 4; ++it) {
       const int c = 8 * it + (lane >> 3);
       const f32x4 o = *reinterpret_cast<const f32x4*>(ob + c * PITCH + 4 * (lane & 7));
-      const int cc = 32 * w + c, i = i0 + cc % ppb;
+      const int cc = 32 * w + c, i = i0 + (cc & (ppb - 1));
       if (i < win.n)
-        *reinterpret_cast<f32x4*>(out + (((int64_t)(win.first + i) * p.H + g * hpg + cc / ppb) * p.S + split) * DV + 32 * ib +
+        *reinterpret_cast<f32x4*>(out + (((int64_t)(win.first + i) * p.H + g * hpg + (cc >> lg)) * p.S + split) * DV + 32 * ib +
                                   4 * (lane & 7)) = o;
     }
   }
@@ -1256,17 +1301,19 @@ int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const vo
   p.n_rows = n_rows;
   p.S = S;
   p.split_rows = split;
-  p.rows = 32 * plan.cw / (d->n_heads / d->n_groups);
+  const int rows = 32 * plan.cw / (d->n_heads / d->n_groups);   // a power of two
+  while ((1 << p.rows_log2) < rows) ++p.rows_log2;
   if (pg != nullptr) {
     p.page_rows = pg->page_rows;
     p.max_pages = pg->max_pages;
     p.n_pages = pg->n_pages;
   }
   p.scale_log2 = scale_log2(d);
-  fill_inv_freq(d, p.inv_freq);
+  fill_inv_freq(d, p.quarters);
+  for (double& x : p.quarters) x *= 0.63661977236758134308;     // 2 / pi
   WindowFn fn = d->d_v == 128 ? pick_window_nrc<128>(d->d_r, plan.cw, plan.kw) : pick_window_nrc<64>(d->d_r, plan.cw, plan.kw);
   if (d->dtype == GVA_DTYPE_F32) fn = d->d_v == 128 ? pick_window_f32<128>(d->d_r) : pick_window_f32<64>(d->d_r);
-  long long items = window_blocks(d, n_rows, p.rows) * S;
+  long long items = window_blocks(d, n_rows, rows) * S;
   if (S > 1) items = (items + 7) / 8 * 8;
   hipLaunchKernelGGL(fn, dim3((unsigned)(items * d->n_groups)), dim3(64 * plan.cw * plan.kw), 0, s, p);
   st = launch_status();
