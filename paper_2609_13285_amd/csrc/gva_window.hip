@@ -209,6 +209,12 @@ __device__ __forceinline__ void copy_kb(i32x4 desc, uint32_t dst, int voff, int 
                ::"s"(dst), "v"(voff), "s"(desc), "s"(soff)
                : "memory", "m0");
 }
+// The same for rows that are read once: kept out of the caches' normal replacement.
+__device__ __forceinline__ void copy_kb_nt(i32x4 desc, uint32_t dst, int voff, int soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+               ::"s"(dst), "v"(voff), "s"(desc), "s"(soff)
+               : "memory", "m0");
+}
 template <int N>
 __device__ __forceinline__ void wait_copies() {   // until at most N of this wave's copies are in flight
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -330,7 +336,7 @@ struct WindowCfg {
   static constexpr int V_BYTES = kTileRows * DV * 2;
   static constexpr int KB = V_BYTES / 1024;                // KB per value tile
   static constexpr int TILE_BYTES = V_BYTES + NRC * 1024;
-  static constexpr int NBUF = KW == 4 ? 3 : 4;             // tiles: weighted, scored, and the rest in flight
+  static constexpr int NBUF = KW * 4 * TILE_BYTES <= 150 * 1024 ? 4 : 3;   // tiles: weighted, scored, and the rest in flight
   static constexpr int AHEAD = NBUF - 2;
   static constexpr int KCOPIES = (NRC + CW - 1) / CW;
   static constexpr int COPIES = KB / CW + KCOPIES;         // per wave and tile
@@ -347,7 +353,7 @@ struct WindowCfg {
 };
 
 template <int DV, int NRC, int CW, int KW>
-__global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(WindowParams p) {
+__global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2) window_kernel(WindowParams p) {
   using Cfg = WindowCfg<DV, NRC, CW, KW>;
   constexpr int NCH = Cfg::NCH, NIB = Cfg::NIB, RA = Cfg::READ_AHEAD, NBUF = Cfg::NBUF, AHEAD = Cfg::AHEAD;
   __shared__ __attribute__((aligned(1024))) char lds[Cfg::LDS];
@@ -430,7 +436,8 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
 #pragma unroll
     for (int k = 0; k < Cfg::KB / CW; ++k) {
       const int kb = w * (Cfg::KB / CW) + k;
-      copy_kb(vdesc, dst + kb * 1024, v_voff, row * DV * 2 + kb * 1024);
+      if constexpr (KW == 4) copy_kb_nt(vdesc, dst + kb * 1024, v_voff, row * DV * 2 + kb * 1024);
+      else copy_kb(vdesc, dst + kb * 1024, v_voff, row * DV * 2 + kb * 1024);
     }
     // the positional tile is 32 d_r 2 bytes <= NRC KB: whole KBs (what follows
     // it lands in padding); waves past NRC repeat one, so that all copy alike
@@ -472,20 +479,19 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
     // swapped, so that a lane's 16 results of a block are two B operands of the
     // score product as they lie.  One pass per head of the wave's columns, each
     // with the loads of CS chunks of 16 columns ahead of the products.
-    f32x16 d[NIB];
     const int mrow = (n & 19) | ((n & 4) << 1) | ((n & 8) >> 1);
-    auto absorb = [&](auto cs_tag, int hd, f32x16 (&e)[NIB]) __attribute__((always_inline)) {
-      constexpr int CS = decltype(cs_tag)::value;
-      const uint16_t* const mh = static_cast<const uint16_t*>(p.m) + ((int64_t)hd * DV + mrow) * p.d_c;
+    auto absorb = [&](auto cs_tag, int hd, int ib0, auto& e) __attribute__((always_inline)) {
+      constexpr int CS = decltype(cs_tag)::value, NB = sizeof(e) / sizeof(f32x16);
+      const uint16_t* const mh = static_cast<const uint16_t*>(p.m) + ((int64_t)hd * DV + 32 * ib0 + mrow) * p.d_c;
       const int nround = (p.d_c + 16 * CS - 1) / (16 * CS);
-      u32x4 xq[2][CS], xm[2][CS][NIB];
+      u32x4 xq[2][CS], xm[2][CS][NB];
       auto load = [&](int ro, int at) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < CS; ++c) {         // columns past d_c: any valid ones against zeros
           const int kc = min(16 * (CS * ro + c) + 8 * h, p.d_c - 8);
           xq[at][c] = *reinterpret_cast<const u32x4*>(qraw + kc);
 #pragma unroll
-          for (int ib = 0; ib < NIB; ++ib)
+          for (int ib = 0; ib < NB; ++ib)
             xm[at][c][ib] = *reinterpret_cast<const u32x4*>(mh + (int64_t)(32 * ib) * p.d_c + kc);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -495,12 +501,12 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
         for (int c = 0; c < CS; ++c) {
           const bf16x8 bq = 16 * (CS * ro + c) < p.d_c ? as_bf16x8(xq[at][c]) : zero8;
 #pragma unroll
-          for (int ib = 0; ib < NIB; ++ib) e[ib] = mfma32(as_bf16x8(xm[at][c][ib]), bq, e[ib]);
+          for (int ib = 0; ib < NB; ++ib) e[ib] = mfma32(as_bf16x8(xm[at][c][ib]), bq, e[ib]);
         }
         __builtin_amdgcn_sched_barrier(0);
       };
 #pragma unroll
-      for (int ib = 0; ib < NIB; ++ib)
+      for (int ib = 0; ib < NB; ++ib)
 #pragma unroll
         for (int r = 0; r < 16; ++r) e[ib][r] = 0.f;
       load(0, 0);
@@ -514,27 +520,68 @@ __global__ void __launch_bounds__(64 * CW * KW, KW == 4 ? 1 : 2) window_kernel(W
         }
       }
     };
-    const int h_first = g * hpg + (32 * w >> lg);
-    if (ppb >= 32) {
-      absorb(std::integral_constant<int, 4>{}, h_first, d);
-    } else {
+    const int h_first = g * hpg + (32 * w >> lg), npass = ppb >= 32 ? 1 : 32 >> lg;
+    if constexpr (KW < 4) {                    // each set for itself: two of four waves have no room to share
+      f32x16 d[NIB];
+      if (npass == 1) {
+        absorb(std::integral_constant<int, 4>{}, h_first, 0, d);
+      } else {
 #pragma unroll 1
-      for (int ps = 0; ps < 32 >> lg; ++ps) {
-        f32x16 e[NIB];
-        absorb(std::integral_constant<int, 2>{}, h_first + ps, e);
-        const bool mine = (n >> lg) == ps;
+        for (int ps = 0; ps < npass; ++ps) {
+          f32x16 e[NIB];
+          absorb(std::integral_constant<int, 2>{}, h_first + ps, 0, e);
+          const bool mine = (n >> lg) == ps;
 #pragma unroll
-        for (int ib = 0; ib < NIB; ++ib)
+          for (int ib = 0; ib < NIB; ++ib)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) d[ib][r] = ps == 0 || mine ? e[ib][r] : d[ib][r];
+            for (int r = 0; r < 16; ++r) d[ib][r] = ps == 0 || mine ? e[ib][r] : d[ib][r];
+        }
       }
-    }
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      float xv[8];
+      for (int c = 0; c < NCH; ++c) {
+        float xv[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) xv[j] = d[c >> 1][8 * (c & 1) + j];
-      put_query(qh[c], ql[c], q3[c], xv);
+        for (int j = 0; j < 8; ++j) xv[j] = d[c >> 1][8 * (c & 1) + j];
+        put_query(qh[c], ql[c], q3[c], xv);
+      }
+    } else {
+      // The sets share the work, blocks of 32 rows of a head's map in turn, and
+      // pass the parts on through LDS that no tile has reached yet: part k of chunk
+      // c of column wave w at share(k, c), a lane's 16 bytes in place.
+      static_assert((NBUF - AHEAD) * Cfg::TILE_BYTES * KW >= 3 * CW * NCH * 1024, "the queries pass through buffers not yet in use");
+      constexpr int ROOM = (NBUF - AHEAD) * Cfg::TILE_BYTES / 1024;       // KB of a set's free buffers
+      auto share = [&](int part, int c) {
+        const int kb = (part * CW + w) * NCH + c;
+        return reinterpret_cast<bf16x8*>(lds + kb / ROOM * Cfg::SET_BYTES + AHEAD * Cfg::TILE_BYTES + kb % ROOM * 1024 + lane * 16);
+      };
+      constexpr int NU = 2;                    // blocks of a turn
+#pragma unroll 1
+      for (int u = grp; u < npass * (NIB / NU); u += KW) {
+        const int ps = u / (NIB / NU), ib0 = u % (NIB / NU) * NU;
+        f32x16 e[NU];
+        absorb(std::integral_constant<int, 4>{}, h_first + ps, ib0, e);
+        if (npass == 1 || (n >> lg) == ps) {
+#pragma unroll
+          for (int c = 0; c < 2 * NU; ++c) {
+            float xv[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) xv[j] = e[c >> 1][8 * (c & 1) + j];
+            bf16x8 hi, lo, third;
+            put_query(hi, lo, third, xv);
+            *share(0, 2 * ib0 + c) = hi;
+            *share(1, 2 * ib0 + c) = lo;
+            *share(2, 2 * ib0 + c) = third;
+          }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      tile_barrier();
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        qh[c] = *share(0, c);
+        ql[c] = *share(1, c);
+        q3[c] = *share(2, c);
+      }
     }
   } else {
     const float* qa = p.q_abs + qrow * DV + 8 * h;
@@ -1170,7 +1217,7 @@ using WindowFn = void (*)(WindowParams);
 template <int DV, int NRC>
 WindowFn pick_window_waves(int cw, int kw) {
   if (cw == 4) return kw == 2 ? window_kernel<DV, NRC, 4, 2> : window_kernel<DV, NRC, 4, 1>;
-  if (cw == 2) return window_kernel<DV, NRC, 2, 2>;
+  if (cw == 2) return window_kernel<DV, NRC, 2, 4>;
   return window_kernel<DV, NRC, 1, 4>;
 }
 
@@ -1210,7 +1257,7 @@ WindowPlan window_plan(const gva_dims* d, int n_rows, int S) {
   WindowPlan plan{4, 1, false};
   if (d->dtype == GVA_DTYPE_F32) return {4, 1, true};
   if (cols <= 32) plan = {1, 4, false};
-  else if (cols <= 64) plan = {2, 2, false};
+  else if (cols <= 64) plan = {2, 4, false};
   else if (window_blocks(d, n_rows, 128 / hpg) * d->n_groups * S < device_cu_count() * 3 / 2) plan = {4, 2, false};
   plan.inside = S == 1 && d->d_c <= 512;
   return plan;
