@@ -3,6 +3,7 @@
 // drafted tokens (gva_tree_attention), on contiguous or paged caches.
 
 #include <cfloat>
+#include <map>
 #include <type_traits>
 
 #include "gva_window.h"
@@ -201,19 +202,29 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// One wave copies 1 KB into LDS, 16 bytes a lane in lane order: see copy_kb of
-// the prompt kernel (in asm, so that the compiler does not drain the copies in
-// flight before each LDS read; it writes no register but m0).
-__device__ __forceinline__ void copy_kb(i32x4 desc, uint32_t dst, int voff, int soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               ::"s"(dst), "v"(voff), "s"(desc), "s"(soff)
-               : "memory", "m0");
+// One wave copies 1 KB into LDS, 16 bytes a lane in lane order, from byte soff +
+// OFF behind the descriptor to m0 + OFF (zeros past the descriptor's end).  In asm so
+// that the compiler does not drain the copies in flight before each LDS read (see the
+// prompt kernel); it writes no register but m0, and the copies of a tile that lie
+// one behind the other share one setting of it.  NT: rows that are read once, kept
+// out of the caches' normal replacement.
+__device__ __forceinline__ void copy_to(uint32_t dst) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(dst) : "memory", "m0"); }
+template <int OFF, bool NT>
+__device__ __forceinline__ void copy_kb(i32x4 desc, int voff, int soff) {
+  if constexpr (NT)
+    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 nt lds" ::"v"(voff), "s"(desc), "s"(soff), "n"(OFF) : "memory");
+  else
+    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" ::"v"(voff), "s"(desc), "s"(soff), "n"(OFF) : "memory");
 }
-// The same for rows that are read once: kept out of the caches' normal replacement.
-__device__ __forceinline__ void copy_kb_nt(i32x4 desc, uint32_t dst, int voff, int soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
-               ::"s"(dst), "v"(voff), "s"(desc), "s"(soff)
-               : "memory", "m0");
+// N KB in a row.
+template <int N, bool NT>
+__device__ __forceinline__ void copy_run(i32x4 desc, uint32_t dst, int voff, int soff) {
+  copy_to(dst);
+  copy_kb<0, NT>(desc, voff, soff);
+  if constexpr (N > 1) copy_kb<1024, NT>(desc, voff, soff);
+  if constexpr (N > 2) copy_kb<2048, NT>(desc, voff, soff);
+  if constexpr (N > 3) copy_kb<3072, NT>(desc, voff, soff);
+  if constexpr (N > 4) copy_run<N - 4, NT>(desc, dst + 4096, voff, soff + 4096);
 }
 template <int N>
 __device__ __forceinline__ void wait_copies() {   // until at most N of this wave's copies are in flight
@@ -336,10 +347,8 @@ struct WindowCfg {
   static constexpr int V_BYTES = kTileRows * DV * 2;
   static constexpr int KB = V_BYTES / 1024;                // KB per value tile
   static constexpr int TILE_BYTES = V_BYTES + NRC * 1024;
-  static constexpr int NBUF = KW * 4 * TILE_BYTES <= 150 * 1024 ? 4 : 3;   // tiles: weighted, scored, and the rest in flight
-  static constexpr int AHEAD = NBUF - 2;
-  static constexpr int KCOPIES = (NRC + CW - 1) / CW;
-  static constexpr int COPIES = KB / CW + KCOPIES;         // per wave and tile
+  static constexpr int NBUF = 4;                           // tiles: weighted, scored, scored next, in flight
+  static constexpr int KCOPIES = (NRC + CW - 1) / CW;      // of the positional tile, per wave
   static constexpr int SET_BYTES = NBUF * TILE_BYTES;
   static constexpr int MERGE_BYTES = (KW - 1) * CW * 64 * (NIB * 16 + 2) * 4;
   static constexpr int OUT_PITCH = DV * 2 + 16;            // bytes of a column's outputs in LDS
@@ -353,9 +362,9 @@ struct WindowCfg {
 };
 
 template <int DV, int NRC, int CW, int KW>
-__global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2) window_kernel(WindowParams p) {
+__global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(WindowParams p) {
   using Cfg = WindowCfg<DV, NRC, CW, KW>;
-  constexpr int NCH = Cfg::NCH, NIB = Cfg::NIB, RA = Cfg::READ_AHEAD, NBUF = Cfg::NBUF, AHEAD = Cfg::AHEAD;
+  constexpr int NCH = Cfg::NCH, NIB = Cfg::NIB, RA = Cfg::READ_AHEAD, NBUF = Cfg::NBUF;
   __shared__ __attribute__((aligned(1024))) char lds[Cfg::LDS];
   __shared__ uint32_t masks[Cfg::COLS * kTreeWords];
   __shared__ int16_t tree_parent[kMaxTree];
@@ -412,50 +421,61 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
   const int32_t* const table = p.block_table + (paged ? (int64_t)b * p.max_pages : 0);
   int page = (kbeg / kTileRows + grp) / tiles_per_page;    // of the next tile to copy
   int in_page = (kbeg / kTileRows + grp) % tiles_per_page;
-  int next_copy = 0;
-  int id_base = page, ids = b;
+  const int page_step = KW / tiles_per_page, tile_step = KW % tiles_per_page;
+  int next_copy = 0, id_base = page, ids = b;
   auto load_ids = [&]() {
-    if (!paged) return;
     id_base = page;
     const int id = table[min(id_base + lane, p.max_pages - 1)];
     ids = min(max(id, 0), p.n_pages - 1);
   };
-  load_ids();
+  if (paged) load_ids();
   char* const set_lds = lds + grp * Cfg::SET_BYTES;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)set_lds;
   const int v_voff = (lane >> 4) * 256 + (((lane & 15) ^ (4 * (lane >> 4))) << 4);
-  auto copy_next = [&](int buf) {
+  // Where the next tile is: the page's descriptors, which past the last tile
+  // are empty, and the tile's place behind them.
+  const uint32_t v_page = (uint32_t)page_rows * (DV / 8), k_page = (uint32_t)page_rows * (uint32_t)p.d_r / 8;   // 16-byte pieces
+  const uint32_t v_pages = v_page * p.G;
+  i32x4 vdesc, kdesc;
+  int v_soff, k_soff;
+  auto aim = [&]() __attribute__((always_inline)) {
+    if (paged && page - id_base >= 64) load_ids();
     const bool in = KW * next_copy + grp < ntiles;
-    const int64_t id = paged ? __builtin_amdgcn_readlane(ids, min(max(page - id_base, 0), 63)) : b;
-    const uint64_t va = (uint64_t)(uintptr_t)p.v + (uint64_t)((id * p.G + g) * page_rows) * (DV * 2);
-    const uint64_t ka = (uint64_t)(uintptr_t)p.kr + (uint64_t)(id * page_rows) * (uint64_t)(p.d_r * 2);
-    const i32x4 vdesc = {(int)(uint32_t)va, (int)(uint32_t)(va >> 32) & 0xFFFF, in ? page_rows * DV * 2 : 0, kBufferWord3};
-    const i32x4 kdesc = {(int)(uint32_t)ka, (int)(uint32_t)(ka >> 32) & 0xFFFF, in ? page_rows * p.d_r * 2 : 0, kBufferWord3};
-    const int row = in_page * kTileRows;
+    const uint32_t id = paged ? (uint32_t)__builtin_amdgcn_readlane(ids, min(max(page - id_base, 0), 63)) : (uint32_t)b;
+    const uint64_t va = (uint64_t)(uintptr_t)p.v + (((uint64_t)id * v_pages + (uint32_t)g * v_page) << 4);
+    const uint64_t ka = (uint64_t)(uintptr_t)p.kr + (((uint64_t)id * k_page) << 4);
+    vdesc = i32x4{(int)(uint32_t)va, (int)(uint32_t)(va >> 32) & 0xFFFF, in ? (int)(v_page * 16) : 0, kBufferWord3};
+    kdesc = i32x4{(int)(uint32_t)ka, (int)(uint32_t)(ka >> 32) & 0xFFFF, in ? (int)(k_page * 16) : 0, kBufferWord3};
+    v_soff = in_page * (kTileRows * DV * 2);
+    k_soff = in_page * (kTileRows * 2) * p.d_r;
+  };
+  aim();
+  auto copy_next = [&](int buf) __attribute__((always_inline)) {
     const uint32_t dst = lds0 + buf * Cfg::TILE_BYTES;
-#pragma unroll
-    for (int k = 0; k < Cfg::KB / CW; ++k) {
-      const int kb = w * (Cfg::KB / CW) + k;
-      if constexpr (KW == 4) copy_kb_nt(vdesc, dst + kb * 1024, v_voff, row * DV * 2 + kb * 1024);
-      else copy_kb(vdesc, dst + kb * 1024, v_voff, row * DV * 2 + kb * 1024);
-    }
+    constexpr int KBW = Cfg::KB / CW;
+    copy_run<KBW, (KW > 2)>(vdesc, dst + w * (KBW * 1024), v_voff, v_soff + w * (KBW * 1024));
     // the positional tile is 32 d_r 2 bytes <= NRC KB: whole KBs (what follows
     // it lands in padding); waves past NRC repeat one, so that all copy alike
-#pragma unroll
-    for (int k = 0; k < Cfg::KCOPIES; ++k) {
-      const int kb = (w * Cfg::KCOPIES + k) % NRC;
-      copy_kb(kdesc, dst + Cfg::V_BYTES + kb * 1024, lane * 16, row * p.d_r * 2 + kb * 1024);
-    }
+    const int kb = w * Cfg::KCOPIES % NRC;
+    copy_run<Cfg::KCOPIES, false>(kdesc, dst + Cfg::V_BYTES + kb * 1024, lane * 16, k_soff + kb * 1024);
     ++next_copy;
-    in_page += KW;
+    page += page_step;
+    in_page += tile_step;
+    bool moved = page_step > 0 || KW * next_copy + grp >= ntiles;
     if (in_page >= tiles_per_page) {
-      page += in_page / tiles_per_page;
-      in_page %= tiles_per_page;
-      if (paged && page - id_base >= 64) load_ids();
+      in_page -= tiles_per_page;
+      ++page;
+      moved = true;
+    }
+    if (moved) {
+      aim();
+    } else {
+      v_soff += KW * kTileRows * DV * 2;
+      k_soff += KW * kTileRows * 2 * p.d_r;
     }
   };
-#pragma unroll
-  for (int a = 0; a < AHEAD; ++a) copy_next(a);
+  copy_next(0);
+  copy_next(1);
 
   // ---- a tree's masks and depths
   if (tree && !too_large) tree_masks(p, win, i0, ppb, Cfg::COLS, 64 * CW * KW, masks, tree_parent, tree_depth);
@@ -521,7 +541,7 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
       }
     };
     const int h_first = g * hpg + (32 * w >> lg), npass = ppb >= 32 ? 1 : 32 >> lg;
-    if constexpr (KW < 4) {                    // each set for itself: two of four waves have no room to share
+    if constexpr (KW < 3) {                    // each set for itself: two of four waves have no room to share
       f32x16 d[NIB];
       if (npass == 1) {
         absorb(std::integral_constant<int, 4>{}, h_first, 0, d);
@@ -548,11 +568,11 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
       // The sets share the work, blocks of 32 rows of a head's map in turn, and
       // pass the parts on through LDS that no tile has reached yet: part k of chunk
       // c of column wave w at share(k, c), a lane's 16 bytes in place.
-      static_assert((NBUF - AHEAD) * Cfg::TILE_BYTES * KW >= 3 * CW * NCH * 1024, "the queries pass through buffers not yet in use");
-      constexpr int ROOM = (NBUF - AHEAD) * Cfg::TILE_BYTES / 1024;       // KB of a set's free buffers
+      static_assert(2 * Cfg::TILE_BYTES * KW >= 3 * CW * NCH * 1024, "the queries pass through buffers not yet in use");
+      constexpr int ROOM = 2 * Cfg::TILE_BYTES / 1024;       // KB of a set's free buffers
       auto share = [&](int part, int c) {
         const int kb = (part * CW + w) * NCH + c;
-        return reinterpret_cast<bf16x8*>(lds + kb / ROOM * Cfg::SET_BYTES + AHEAD * Cfg::TILE_BYTES + kb % ROOM * 1024 + lane * 16);
+        return reinterpret_cast<bf16x8*>(lds + kb / ROOM * Cfg::SET_BYTES + 2 * Cfg::TILE_BYTES + kb % ROOM * 1024 + lane * 16);
       };
       constexpr int NU = 2;                    // blocks of a turn
 #pragma unroll 1
@@ -638,6 +658,12 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
     tile_sum = r == 0 ? pr[r] : tile_sum + pr[r];
     if (r == 15) l_run += tile_sum;
   };
+  // Between the waves of a set, which meet once a tile.  A set of one needs no
+  // barrier: its copies, reads and writes are in order.
+  auto set_barrier = [&]() __attribute__((always_inline)) {
+    if constexpr (CW > 1) tile_barrier();
+    else asm volatile("" ::: "memory");
+  };
   // (the same answer for all sets, which share the barriers)
   auto is_masked = [&](int j) { return kbeg + (KW * j + KW) * kTileRows > masked_from; };
   // Set to 0 in a masked tile: rows past the keys, infinities and NaN.
@@ -668,31 +694,44 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
     if (tree) sees &= tree_sees(masks + (col & (ppb - 1)) * kTreeWords, row0 - P);
     hide(sn, sees >> (4 * h));
   };
-  // One tile: scores sn of tile j, beside them the softmax weights of the
-  // tile before (scores sp), then that tile's P.V, beside it tile j's maxima.
-  // The orders are pinned (scheduling barriers): on these matrix cores a few
-  // vector instructions between two products are nearly free, a run of them
-  // is not.  FIRST: the workgroup's first tile, with none before it.
+  constexpr int NA = NCH + NRC;
+  bf16x8 a[NA];                                // a tile's score operands; the first RA are read ahead of its step
+  auto operand = [&](int buf, int k) __attribute__((always_inline)) {
+    const char* const tile = set_lds + buf * Cfg::TILE_BYTES;
+    if (k < NCH) return *reinterpret_cast<const bf16x8*>(tile + v_off[k & 1] + k * 512);
+    return *reinterpret_cast<const bf16x8*>(tile + k_off[k >= NCH ? k - NCH : 0]);
+  };
+  float mt = -INFINITY;                        // the maximum of a lane's scores of the tile before
+  auto move_max = [&](bool first) __attribute__((always_inline)) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+    mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    if (first || __ballot(mt > m_run + kWindowLazyMax) != 0) {
+      const float m_new = fmaxf(mt, m_run);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int ib = 0; ib < NIB; ++ib) acc[ib] *= alpha;
+      m_run = m_new;
+    }
+  };
+  // One tile j: its scores sn, beside them the softmax weights of the tile
+  // before (scores sp); then the waves meet; then that tile's P.V, beside it tile
+  // j's maxima and the reads of tile j + 1.  What the meeting stands for: tile j + 1
+  // has landed (every wave has waited for its own copies), tile j - 1 is clean, and
+  // the P.V of tile j - 2 is over, so that tile j + 2 may be copied over it.  The
+  // orders are pinned (scheduling barriers): on these matrix cores a few vector
+  // instructions between two products are nearly free, a run of them is not.
+  // FIRST: the workgroup's first tile, with none before it.
   auto step = [&](auto first_tag, int j, int buf, const f32x16& sp, f32x16& sn) __attribute__((always_inline)) {
     constexpr bool FIRST = decltype(first_tag)::value;
     const int row0 = tile_row(j);
-    const int pbuf = buf == 0 ? NBUF - 1 : buf - 1;
+    const int pbuf = (buf + NBUF - 1) % NBUF;
     const bool cleaned = !FIRST && is_masked(j - 1);
-    copy_next(buf + AHEAD >= NBUF ? buf + AHEAD - NBUF : buf + AHEAD);
     if (cleaned) clean(j - 1, pbuf);
-    const char* const tile = set_lds + buf * Cfg::TILE_BYTES;
-    constexpr int NA = NCH + NRC;
-    auto operand = [&](int k) {
-      if (k < NCH) return *reinterpret_cast<const bf16x8*>(tile + v_off[k & 1] + k * 512);
-      return *reinterpret_cast<const bf16x8*>(tile + k_off[k >= NCH ? k - NCH : 0]);
-    };
-    bf16x8 a[NA], av[2 * NIB];
+    bf16x8 av[2 * NIB];
     float pr[16];
     bf16x8 bn[2];
     if (live) {
-#pragma unroll
-      for (int k = 0; k < RA; ++k) a[k] = operand(k);
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) sn[r] = 0.f;
       constexpr int NM = 2 * NA;               // products of this phase
@@ -705,11 +744,18 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
         if constexpr (FIRST) {
           if ((i & 1) == 1) sn = mfma32(a[k], k < NCH ? q3[k < NCH ? k : 0] : r3[k >= NCH ? k - NCH : 0], sn);
         }
-        if ((i & 1) == 1 && k + RA < NA) a[k + RA] = operand(k + RA);
+        if ((i & 1) == 1) {
+          if (k + RA < NA) a[k + RA] = operand(buf, k + RA);
+          else if (!FIRST) av[k + RA - NA] = vt_piece(pbuf, k + RA - NA);
+        }
         if constexpr (!FIRST) {
-          // sixteen exponentials over the phase's products
+          if (i == 0) {
+            __builtin_amdgcn_sched_barrier(0);
+            move_max(false);                   // of the tile before, beside the first products
+          }
+          // sixteen exponentials over the products from the second on
 #pragma unroll
-          for (int r = i * 16 / NM; r < (i + 1) * 16 / NM; ++r) {
+          for (int r = i == 0 ? 16 : (i - 1) * 16 / (NM - 1); r < i * 16 / (NM - 1); ++r) {
             exps(sp, pr, r);
             if (r == 7) bn[0] = to_bf16x8(pr);
             if (r == 15) bn[1] = to_bf16x8(pr + 8);
@@ -722,52 +768,40 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
       mask(sn, row0);
       __builtin_amdgcn_s_setprio(0);
     }
-    if (!FIRST && cleaned) {                   // the tile before has been cleaned by all
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      tile_barrier();
-    }
+    if (cleaned) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wait_copies<0>();
+    set_barrier();
+    copy_next((buf + 2) % NBUF);
     if (live) {
-      float mt = -INFINITY;
-      if constexpr (!FIRST) {
+      if (cleaned) {                           // what was read ahead was not clean yet
 #pragma unroll
         for (int k = 0; k < RA; ++k) av[k] = vt_piece(pbuf, k);
       }
+      const int nbuf = (buf + 1) % NBUF;
+      mt = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 2 * NIB; ++k) {
         if constexpr (!FIRST) {
           acc[k >> 1] = mfma32(av[k], bn[k & 1], acc[k >> 1]);
           if (k + RA < 2 * NIB) av[k + RA] = vt_piece(pbuf, k + RA);
-          __builtin_amdgcn_sched_barrier(0);
         }
+        if (k >= 2 * NIB - RA) a[k - (2 * NIB - RA)] = operand(nbuf, k - (2 * NIB - RA));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = k * (8 / NIB); r < (k + 1) * (8 / NIB); ++r) mt = fmaxf(mt, sn[r]);
         __builtin_amdgcn_sched_barrier(0);
       }
-      {
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-        mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-      }
-      if (FIRST || __ballot(mt > m_run + kWindowLazyMax) != 0) {
-        const float m_new = fmaxf(mt, m_run);
-        if constexpr (!FIRST) {
-          const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-          l_run *= alpha;
-#pragma unroll
-          for (int ib = 0; ib < NIB; ++ib) acc[ib] *= alpha;
-        }
-        m_run = m_new;
-      }
+      if constexpr (FIRST) move_max(true);
     }
-    wait_copies<Cfg::COPIES*(AHEAD - 1)>();    // the next tile has landed (those after it may be in flight)
-    tile_barrier();
   };
   auto last = [&](int j, int buf, const f32x16& sp) {   // the last tile's weights and P.V
     if (is_masked(j)) {
       clean(j, buf);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      tile_barrier();
+      set_barrier();
     }
     if (!live) return;
+    if (j > 0) move_max(false);
     float pr[16];
     bf16x8 bn[2];
 #pragma unroll
@@ -778,25 +812,26 @@ __global__ void __launch_bounds__(64 * CW * KW, CW * KW == 4 && KW == 4 ? 1 : 2)
     for (int k = 0; k < 2 * NIB; ++k) acc[k >> 1] = mfma32(vt_piece(buf, k), bn[k & 1], acc[k >> 1]);
   };
 
-  wait_copies<Cfg::COPIES*(AHEAD - 1)>();
-  tile_barrier();
+  wait_copies<0>();
+  set_barrier();
   if (nit > 0) {
     f32x16 s0, s1;                             // the scores of even and odd tiles
+    if (live) {
+#pragma unroll
+      for (int k = 0; k < RA; ++k) a[k] = operand(0, k);
+    }
     step(std::true_type{}, 0, 0, s0, s0);
-    int buf = 1, j = 1;
+    int j = 1;
     for (; j + 1 < nit; j += 2) {
-      step(std::false_type{}, j, buf, s0, s1);
-      buf = buf == NBUF - 1 ? 0 : buf + 1;
-      step(std::false_type{}, j + 1, buf, s1, s0);
-      buf = buf == NBUF - 1 ? 0 : buf + 1;
+      step(std::false_type{}, j, j % NBUF, s0, s1);
+      step(std::false_type{}, j + 1, (j + 1) % NBUF, s1, s0);
     }
     if (j < nit) {
-      step(std::false_type{}, j, buf, s0, s1);
+      step(std::false_type{}, j, j % NBUF, s0, s1);
       s0 = s1;
       ++j;
-      buf = buf == NBUF - 1 ? 0 : buf + 1;
     }
-    last(j - 1, buf == 0 ? NBUF - 1 : buf - 1, s0);
+    last(j - 1, (j - 1) % NBUF, s0);
   }
 
   // ---- merge the sets, normalise, write
@@ -977,10 +1012,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
     for (int k = 0; k < V_BYTES / 4096; ++k) {
       const int kb = w * (V_BYTES / 4096) + k;             // pieces 4 kb .. 4 kb + 3 of a layout tile
       const int f = 4 * (kb & 1) + (lane >> 4);
-      copy_kb(vdesc, dst + kb * 1024, (lane >> 4) * 256 + (((lane & 15) ^ f) << 4), at * DV * 4 + kb * 1024);
+      copy_run<1, false>(vdesc, dst + kb * 1024, (lane >> 4) * 256 + (((lane & 15) ^ f) << 4), at * DV * 4 + kb * 1024);
     }
     for (int kb = w; kb < NR * 2; kb += kWaves)            // 32 d_r 4 bytes, in whole KBs
-      if (kb < NR) copy_kb(kdesc, dst + V_BYTES + kb * 1024, lane * 16, at * p.d_r * 4 + kb * 1024);
+      if (kb < NR) copy_run<1, false>(kdesc, dst + V_BYTES + kb * 1024, lane * 16, at * p.d_r * 4 + kb * 1024);
   };
 
   if (tree && !too_large) tree_masks(p, win, i0, ppb, 128, kThreads, masks, tree_parent, tree_depth);
@@ -1169,56 +1204,80 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
 }
 
 // ---------------------------------------------------------------- combine
-// The merge of the splits of a (row, head): d_v / 4 lanes, four columns each.
-// Rows that no sequence has are left as they were.
+// The merge of the splits of a (row, head), by a wave: the splits' log-sum-exps
+// in one read, four to a lane, then the partials of those with rows, d_v / 4 lanes
+// each, so 2 or 4 splits at a time and four times that in flight.  Rows that no
+// sequence has are left as they were.  Bound by latency: two round trips (one lane
+// row per (row, head), all splits in turn, took 18 us for 4048 of up to 36 splits).
 template <typename T, int DV>
 __global__ void __launch_bounds__(kThreads) window_combine_kernel(const float* o_part, const float* lse_part, const int32_t* cu,
                                                                  T* o, float* lse, int32_t B, int32_t H, int32_t n_rows,
                                                                  int32_t S) {
-  constexpr int LPR = DV / 4;
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
-  const int e = threadIdx.x % LPR;
+  constexpr int LPR = DV / 4, SLOTS = 64 / LPR;
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int row = (int)(id / H);
   if (id >= (int64_t)n_rows * H || row < cu[0] || row >= cu[B]) return;
   const float* lp = lse_part + id * S;
-  const float* op = o_part + id * S * DV + 4 * e;
-  float mx = -INFINITY;
-  bool any = false;                            // a split with rows: it may be a NaN, which no maximum shows
-#pragma unroll 8
-  for (int s = 0; s < S; ++s) {
-    mx = fmaxf(mx, lp[s]);
-    any = any || lp[s] != -INFINITY;
+  float l[4], mx = -INFINITY;
+  int last = 0;                                // splits up to the last with rows (it may be a NaN, which no maximum shows)
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int s = lane + 64 * k;
+    l[k] = s < S ? lp[s] : -INFINITY;
+    mx = fmaxf(mx, l[k]);
+    const unsigned long long some = __ballot(l[k] != -INFINITY);
+    if (some != 0ull) last = 64 * k + 64 - __builtin_clzll(some);
   }
+  mx = wave_max(mx);
+  const float* op = o_part + id * S * DV + 4 * (lane % LPR);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (64 * k >= last) break;
+    const float wgt = l[k] == -INFINITY ? 0.f : __expf(l[k] - mx);
+    const int end = min(64, last - 64 * k);
 #pragma unroll 4
-  for (int s = 0; s < S; ++s) {
-    const float l = lp[s];
-    if (l == -INFINITY) continue;
-    const float wgt = __expf(l - mx);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(op + (int64_t)s * DV);
-    sum += wgt;
-    acc += x * wgt;
+    for (int s = 0; s < end; s += SLOTS) {
+      const int mine = s + lane / LPR;
+      const float ws = __shfl(wgt, mine & 63, 64);
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};          // a split without rows has no partial
+      if (mine < end && ws != 0.f) x = *reinterpret_cast<const f32x4*>(op + (int64_t)(64 * k + mine) * DV);
+      if (mine < end) {
+        sum += ws;
+        acc += x * ws;
+      }
+    }
   }
-  const float inv = any ? 1.f / sum : 0.f;
-  const f32x4 x = any ? acc * inv : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int off = LPR; off < 64; off *= 2) {
+    sum += __shfl_xor(sum, off, 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
+  }
+  if (lane >= LPR) return;
+  const f32x4 x = last > 0 ? acc * (1.f / sum) : f32x4{0.f, 0.f, 0.f, 0.f};
+  T* const out = o + id * DV + 4 * lane;
   if constexpr (sizeof(T) == 2) {
     const bf16x2 a = __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2), c = __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2);
-    *reinterpret_cast<uint64_t*>(o + id * DV + 4 * e) =
-        (uint64_t)__builtin_bit_cast(uint32_t, c) << 32 | __builtin_bit_cast(uint32_t, a);
+    *reinterpret_cast<uint64_t*>(out) = (uint64_t)__builtin_bit_cast(uint32_t, c) << 32 | __builtin_bit_cast(uint32_t, a);
   } else {
-    *reinterpret_cast<f32x4*>(o + id * DV + 4 * e) = x;
+    *reinterpret_cast<f32x4*>(out) = x;
   }
-  if (lse != nullptr && e == 0) lse[id] = any ? mx + logf(sum) : -INFINITY;
+  if (lse != nullptr && lane == 0) lse[id] = last > 0 ? mx + logf(sum) : -INFINITY;
 }
 
 using WindowFn = void (*)(WindowParams);
 
+// Sets of one or two waves: as many as four tiles each leave room for in LDS.
+constexpr int window_sets(int d_v, int nrc) { return d_v == 128 && nrc > 1 ? 3 : 4; }
+
 template <int DV, int NRC>
 WindowFn pick_window_waves(int cw, int kw) {
   if (cw == 4) return kw == 2 ? window_kernel<DV, NRC, 4, 2> : window_kernel<DV, NRC, 4, 1>;
-  if (cw == 2) return window_kernel<DV, NRC, 2, 4>;
-  return window_kernel<DV, NRC, 1, 4>;
+  constexpr int KW = window_sets(DV, NRC);
+  return cw == 2 ? window_kernel<DV, NRC, 2, KW> : window_kernel<DV, NRC, 1, KW>;
 }
 
 template <int DV>
@@ -1233,8 +1292,7 @@ WindowFn pick_window_f32(int d_r) {
 
 template <typename T>
 void launch_combine(const WindowParams& p, int d_v, hipStream_t s) {
-  const int per = kThreads / (d_v / 4);
-  const dim3 grid((unsigned)(((long long)p.n_rows * p.H + per - 1) / per));
+  const dim3 grid((unsigned)(((long long)p.n_rows * p.H + kWaves - 1) / kWaves));
   const auto fn = d_v == 128 ? window_combine_kernel<T, 128> : window_combine_kernel<T, 64>;
   hipLaunchKernelGGL(fn, grid, dim3(kThreads), 0, s, p.o_part, p.lse_part, p.cu, static_cast<T*>(p.o), p.lse, p.B, p.H,
                      p.n_rows, p.S);
@@ -1256,8 +1314,7 @@ WindowPlan window_plan(const gva_dims* d, int n_rows, int S) {
   const long long cols = ((long long)n_rows + d->batch - 1) / d->batch * hpg;   // of a sequence, on average
   WindowPlan plan{4, 1, false};
   if (d->dtype == GVA_DTYPE_F32) return {4, 1, true};
-  if (cols <= 32) plan = {1, 4, false};
-  else if (cols <= 64) plan = {2, 4, false};
+  if (cols <= 64) plan = {cols <= 32 ? 1 : 2, window_sets(d->d_v, d->d_r <= 16 ? 1 : 2), false};
   else if (window_blocks(d, n_rows, 128 / hpg) * d->n_groups * S < device_cu_count() * 3 / 2) plan = {4, 2, false};
   plan.inside = S == 1 && d->d_c <= 512;
   return plan;
@@ -1300,6 +1357,67 @@ int check_window(const gva_dims* d, const gva_paging* pg, int n_rows, int S, int
   if (n_rows > (1 << 20) || (long long)n_rows * d->n_heads > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   if (n_rows > 0 && window_blocks(d, n_rows, 32 / hpg) * S * d->n_groups > 0x7FFFFFF0LL) return GVA_ERR_UNSUPPORTED;
   return GVA_OK;
+}
+
+// ---------------------------------------------------------------- the plan
+int window_len(const gva_dims* d, const int32_t* lens, int b) {
+  return lens == nullptr ? d->t_max : (lens[b] < 0 ? 0 : lens[b] > d->t_max ? d->t_max : lens[b]);
+}
+int window_new(const gva_dims* d, const int32_t* n_new, int n_rows, int b) {
+  const int n = n_new == nullptr ? n_rows / d->batch + (b < n_rows % d->batch ? 1 : 0) : n_new[b];
+  return n < 0 ? 0 : n;
+}
+
+// About what a call takes with a plan: its workgroups are dealt in order to
+// the places that the device has for them, each to the first that is free.  The
+// times of a workgroup and of a tile of 32 keys are measured ones (two workgroups
+// of one set a CU at H32 G8 d 128/16: 1.2 us a tile each, 18 us of start and end
+// with the absorption and 9 without; sets of one or two waves, one workgroup a CU:
+// 0.3 and 0.5 us a tile, 17 and 10 us).  A plan of several splits pays for the
+// absorption's launch, the partials' way through memory and their merge.
+struct WindowTimes {
+  double us;
+  int S, rows;
+};
+WindowTimes window_time(const gva_dims* d, const int32_t* lens, const int32_t* n_new, int n_rows, int n_cu, int S, int split) {
+  const WindowPlan plan = window_plan(d, n_rows, S);
+  const int hpg = d->n_heads / d->n_groups, rows = 32 * plan.cw / hpg;
+  const bool f32 = d->dtype == GVA_DTYPE_F32;
+  const double wide = d->d_v / 128.0 * (f32 ? 8.0 : 1.0);
+  const int places = (plan.cw * plan.kw > 4 || plan.cw < 4 ? 1 : 2) * n_cu;
+  double start = (plan.inside ? 18.0 : 9.0) * (0.5 + 0.5 * d->d_v / 128.0), tile = (plan.cw == 1 ? 0.3 : plan.cw == 2 ? 0.5 : plan.kw == 2 ? 0.8 : 1.2) * wide;
+  std::map<double, long long> free_at{{0.0, places}};
+  double end = 0.0, partials = 0.0;
+  int steps = 0;
+  for (int b = 0; b < d->batch; ++b) {
+    const int L = window_len(d, lens, b), n = window_new(d, n_new, n_rows, b);
+    if (n == 0 || L == 0) continue;
+    int parts = S;
+    if (S > 1 && split > 0) {
+      parts = (L + split - 1) / split;
+      parts = parts > S ? S : parts;
+    }
+    const int blocks = (n + rows - 1) / rows;
+    // a block of few rows leaves waves without work, a prompt's keys are half of its own rows on average
+    const double cols = (double)n / blocks / rows, part = cols < 0.25 ? 0.25 : cols;
+    const double keys = (L - 0.5 * (n < L ? n : L)) / parts;
+    const double t = start + keys / kTileRows * tile * (plan.cw == 4 ? 0.3 + 0.7 * part : 1.0);
+    partials += (double)n * parts;
+    long long left = (long long)blocks * parts * d->n_groups;
+    while (left > 0 && ++steps < 20000) {
+      const auto first = free_at.begin();
+      const long long k = left < first->second ? left : first->second;
+      const double at = first->first + t;
+      if ((first->second -= k) == 0) free_at.erase(first);
+      free_at[at] += k;
+      if (at > end) end = at;
+      left -= k;
+    }
+  }
+  const double row_bytes = (double)d->n_heads * d->d_v * 4.0;
+  if (!plan.inside) end += 4.0 + n_rows * row_bytes / 1.5e6;
+  if (S > 1) end += 5.0 + partials * row_bytes * 2.0 / 3e6;
+  return {end, S, S > 1 ? split : 0};
 }
 
 int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const void* m, const void* v, const void* kr,
@@ -1387,29 +1505,19 @@ int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int3
   if (split_rows != nullptr) *split_rows = 0;
   if (check_window(dims, nullptr, n_rows, 1, 0) != GVA_OK || n_rows == 0) return 1;
   if (n_cu <= 0) n_cu = device_cu_count();
-  const int rows = 32 * window_plan(dims, n_rows, 1).cw / (dims->n_heads / dims->n_groups);
-  // key rows that all workgroups read, and the longest sequence's
-  double work = 0.0, items = 0.0;
+  WindowTimes best = window_time(dims, lens, n_new, n_rows, n_cu, 1, 0);
   int longest = 0;
   for (int b = 0; b < dims->batch; ++b) {
-    const int L = lens == nullptr ? dims->t_max : (lens[b] < 0 ? 0 : lens[b] > dims->t_max ? dims->t_max : lens[b]);
-    const int even = n_rows / dims->batch + (b < n_rows % dims->batch ? 1 : 0);
-    const int n = n_new == nullptr ? even : n_new[b];
-    if (n <= 0 || L == 0) continue;
-    const int nb = (n + rows - 1) / rows;
-    items += nb;
-    work += (double)nb * L;
-    if (L > longest) longest = L;
+    const int L = window_len(dims, lens, b);
+    if (L > longest && window_new(dims, n_new, n_rows, b) > 0) longest = L;
   }
-  if (items * dims->n_groups >= n_cu || longest <= 512) return 1;
-  long long chunk = (long long)(work * dims->n_groups / (2.0 * n_cu));
-  if (chunk < 256) chunk = 256;
-  chunk = (chunk + kTileRows - 1) / kTileRows * kTileRows;
-  long long S = (longest + chunk - 1) / chunk;
-  if (S > 64) S = 64;
-  if (S <= 1) return 1;
-  if (split_rows != nullptr) *split_rows = (int32_t)chunk;
-  return (int)S;
+  for (int S = 2; S <= 64 && longest / S >= 128; S += S < 8 ? 1 : S / 8) {
+    const int rows = split_rows == nullptr ? 0 : (longest + kTileRows * S - 1) / (kTileRows * S) * kTileRows;
+    const WindowTimes t = window_time(dims, lens, n_new, n_rows, n_cu, S, rows);
+    if (t.us < best.us) best = t;
+  }
+  if (split_rows != nullptr) *split_rows = best.rows;
+  return best.S;
 }
 
 int gva_packed_prefill(const gva_dims* dims, const gva_paging* paging, const void* q, const void* m, const void* v_cache,
