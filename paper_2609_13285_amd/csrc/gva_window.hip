@@ -62,21 +62,34 @@ struct WindowParams {
   double quarters[kMaxPairs];   // a pair's frequency, in quarter turns a position
 };
 
+// What a workgroup's first instructions need comes ahead of the block as scalar
+// arguments, which are in registers before a wave starts (see decode_args).
+#define WINDOW_HEAD_ARGS                                                                                         \
+  const int32_t *head_cu, const int32_t *head_lens, int32_t head_B, int32_t head_G, int32_t head_rows_log2,       \
+      int32_t head_S, int32_t head_n_rows, int32_t head_t_max, int32_t head_split_rows
+#define WINDOW_HEAD_NAMES \
+  head_cu, head_lens, head_B, head_G, head_rows_log2, head_S, head_n_rows, head_t_max, head_split_rows
+struct WindowHead {
+  const int32_t* cu;
+  const int32_t* lens;
+  int32_t B, G, rows_log2, S, n_rows, t_max, split_rows;
+};
+
 // A sequence's window: its first packed row, rows and cached rows.
 struct Window {
   int first, n, L;
 };
-__device__ __forceinline__ Window window_of(const WindowParams& p, int b) {
+__device__ __forceinline__ Window window_of(const WindowHead& p, int b) {
   const int a = min(max(p.cu[b], 0), p.n_rows), e = min(max(p.cu[b + 1], 0), p.n_rows);
   return Window{a, max(e - a, 0), clamp_len(p.lens, b, p.t_max)};
 }
 
 // blocks of query rows
-__device__ __forceinline__ int window_blocks_of(const WindowParams& p, int n) {
+__device__ __forceinline__ int window_blocks_of(const WindowHead& p, int n) {
   return (int)(((unsigned)n + (1u << p.rows_log2) - 1) >> p.rows_log2);
 }
 
-__device__ __forceinline__ int window_splits(const WindowParams& p, int L) {
+__device__ __forceinline__ int window_splits(const WindowHead& p, int L) {
   return p.S == 1 ? 1 : max(1, min(p.S, split_count(L, p.S, p.split_rows)));
 }
 
@@ -91,6 +104,17 @@ __device__ __forceinline__ int wave_sum_dpp(int v) {
   return __builtin_amdgcn_readfirstlane((int)(c[0] + c[1]));
 }
 
+__device__ __forceinline__ int wave_max_dpp(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x1B, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false));
+  const auto a = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
+  v = max((int)a[0], (int)a[1]);
+  const auto c = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+  return __builtin_amdgcn_readfirstlane(max((int)c[0], (int)c[1]));
+}
+
 // Item i of the (sequence, block of query rows, split) triples that exist.
 //  - One split, up to 256 sequences: the blocks with most key tiles first.  The
 //    number of blocks with at least t tiles is a sum over the sequences, four
@@ -98,16 +122,19 @@ __device__ __forceinline__ int wave_sum_dpp(int v) {
 //    sequence among those that have a block of exactly t tiles.
 //  - Otherwise sequence by sequence, splits in order, a split's blocks (which
 //    read the same keys) next to each other.
-__device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b, int& blk, int& s) {
+__device__ __forceinline__ bool window_item(const WindowHead& p, int i, int& b, int& blk, int& s, Window& win) {
   const int lane = threadIdx.x & 63;
   if (p.S == 1 && p.B <= 256) {
-    int P[4], n[4], base[4];
+    int P[4], n[4], first[4];
+    int hi = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int bb = lane + 64 * k;
       const Window w = bb < p.B ? window_of(p, bb) : Window{0, 0, 0};
       n[k] = w.n;
       P[k] = w.L - w.n;
+      first[k] = w.first;
+      hi = max(hi, w.n > 0 ? w.L : 0);
     }
     // blocks of a sequence below the first with at least t tiles (all, if none)
     auto below = [&](int k, int t) {
@@ -125,7 +152,8 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
       return wave_sum_dpp(c);
     };
     if (i >= at_least(0)) return false;
-    int lo = 0, hi = (p.t_max + kTileRows - 1) / kTileRows + 1;   // at_least(lo) > i >= at_least(hi)
+    int lo = 0;                                // at_least(lo) > i >= at_least(hi)
+    hi = (wave_max_dpp(hi) + kTileRows - 1) / kTileRows + 1;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
       if (at_least(mid) > i) lo = mid;
@@ -135,14 +163,16 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
     b = blk = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      base[k] = below(k, lo);
-      const int cnt = below(k, lo + 1) - base[k];
+      const int base = below(k, lo), cnt = below(k, lo + 1) - base;
       const int incl = wave_incl_scan(cnt);
       const unsigned long long hit = __ballot(cnt > 0 && incl > rest && incl - cnt <= rest);
       if (hit != 0ull) {
         const int l = __builtin_ctzll(hit);
         b = 64 * k + l;
-        blk = __builtin_amdgcn_readlane(base[k], l) + rest - __builtin_amdgcn_readlane(incl - cnt, l);
+        blk = __builtin_amdgcn_readlane(base, l) + rest - __builtin_amdgcn_readlane(incl - cnt, l);
+        win.first = __builtin_amdgcn_readlane(first[k], l);
+        win.n = __builtin_amdgcn_readlane(n[k], l);
+        win.L = __builtin_amdgcn_readlane(P[k], l) + win.n;
         break;
       }
       rest -= __builtin_amdgcn_readlane(incl, 63);
@@ -174,7 +204,8 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
     }
     local -= __builtin_amdgcn_readlane(in2, 63);
   }
-  const int nb = window_blocks_of(p, window_of(p, b).n);
+  win = window_of(p, b);
+  const int nb = window_blocks_of(p, win.n);
   s = __builtin_amdgcn_readfirstlane(local / nb);
   blk = __builtin_amdgcn_readfirstlane(local % nb);
   return true;
@@ -184,15 +215,15 @@ __device__ __forceinline__ bool window_item(const WindowParams& p, int i, int& b
 // multiple of 8 an XCD keeps to its groups' streams, which the blocks of a
 // sequence share.  More splits: the groups of an item on one XCD (see
 // work_item), as they share the positional keys.
-__device__ __forceinline__ bool window_work(const WindowParams& p, int& b, int& blk, int& s, int& g) {
+__device__ __forceinline__ bool window_work(const WindowHead& p, int& b, int& blk, int& s, int& g, Window& win) {
   const int x = blockIdx.x;
   if (p.S == 1) {
     g = x % p.G;
-    return window_item(p, x / p.G, b, blk, s);
+    return window_item(p, x / p.G, b, blk, s, win);
   }
   const int slot = x >> 3;
   g = slot % p.G;
-  return window_item(p, 8 * (slot / p.G) + (x & 7), b, blk, s);
+  return window_item(p, 8 * (slot / p.G) + (x & 7), b, blk, s, win);
 }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -362,7 +393,8 @@ struct WindowCfg {
 };
 
 template <int DV, int NRC, int CW, int KW>
-__global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(WindowParams p) {
+__global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(WINDOW_HEAD_ARGS, WindowParams p) {
+  const WindowHead hd{WINDOW_HEAD_NAMES};
   using Cfg = WindowCfg<DV, NRC, CW, KW>;
   constexpr int NCH = Cfg::NCH, NIB = Cfg::NIB, RA = Cfg::READ_AHEAD, NBUF = Cfg::NBUF;
   __shared__ __attribute__((aligned(1024))) char lds[Cfg::LDS];
@@ -372,14 +404,14 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
 
   const int hpg = p.H / p.G;
   int b, blk, split, g;
-  if (!window_work(p, b, blk, split, g)) return;
+  Window win;
+  if (!window_work(hd, b, blk, split, g, win)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave / CW, w = wave % CW;
   const int n = lane & 31, h = lane >> 5;      // column, and half of the rows / K-chunk
   const bf16x8 zero8 = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
 
-  const Window win = window_of(p, b);
   const int P = win.L - win.n;                 // rows before the window (negative: some of it has no row)
   const int lg = p.rows_log2, ppb = 1 << lg;   // query rows of the block
   const int i0 = blk << lg, i1 = min(win.n, i0 + ppb);
@@ -500,9 +532,9 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
     // score product as they lie.  One pass per head of the wave's columns, each
     // with the loads of CS chunks of 16 columns ahead of the products.
     const int mrow = (n & 19) | ((n & 4) << 1) | ((n & 8) >> 1);
-    auto absorb = [&](auto cs_tag, int hd, int ib0, auto& e) __attribute__((always_inline)) {
+    auto absorb = [&](auto cs_tag, int hm, int ib0, auto& e) __attribute__((always_inline)) {
       constexpr int CS = decltype(cs_tag)::value, NB = sizeof(e) / sizeof(f32x16);
-      const uint16_t* const mh = static_cast<const uint16_t*>(p.m) + ((int64_t)hd * DV + 32 * ib0 + mrow) * p.d_c;
+      const uint16_t* const mh = static_cast<const uint16_t*>(p.m) + ((int64_t)hm * DV + 32 * ib0 + mrow) * p.d_c;
       const int nround = (p.d_c + 16 * CS - 1) / (16 * CS);
       u32x4 xq[2][CS], xm[2][CS][NB];
       auto load = [&](int ro, int at) __attribute__((always_inline)) {
@@ -934,7 +966,7 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
     float* const lp = p.lse_part + qrow * p.S;
     lp[split] = lse;
     if (split == 0)                            // splits that no workgroup takes
-      for (int k = window_splits(p, win.L); k < p.S; ++k) lp[k] = -INFINITY;
+      for (int k = window_splits(hd, win.L); k < p.S; ++k) lp[k] = -INFINITY;
   }
 }
 
@@ -948,7 +980,8 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
 // stored in the order row ^ (k mod 8), so that eight pieces of a row lie in
 // different banks.
 template <int DV, int NRC>
-__global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p) {
+__global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WINDOW_HEAD_ARGS, WindowParams p) {
+  const WindowHead hd{WINDOW_HEAD_NAMES};
   constexpr int NC = DV / 8, NR = 2 * NRC, NIB = DV / 32;  // 8-wide chunks, 32-wide output blocks
   constexpr int V_BYTES = kTileRows * DV * 4, TILE_BYTES = V_BYTES + NR * 1024;
   constexpr int PITCH = 36;                    // floats of a column's 32-wide block of outputs
@@ -960,12 +993,12 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
 
   const int hpg = p.H / p.G;
   int b, blk, split, g;
-  if (!window_work(p, b, blk, split, g)) return;
+  Window win;
+  if (!window_work(hd, b, blk, split, g, win)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
 
-  const Window win = window_of(p, b);
   const int P = win.L - win.n;
   const int lg = p.rows_log2, ppb = 1 << lg;   // query rows of the block
   const int i0 = blk << lg, i1 = min(win.n, i0 + ppb);
@@ -1200,7 +1233,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WindowParams p)
   float* const lp = p.lse_part + qrow * p.S;
   lp[split] = lse;
   if (split == 0)
-    for (int k = window_splits(p, win.L); k < p.S; ++k) lp[k] = -INFINITY;
+    for (int k = window_splits(hd, win.L); k < p.S; ++k) lp[k] = -INFINITY;
 }
 
 // ---------------------------------------------------------------- combine
@@ -1268,7 +1301,7 @@ __global__ void __launch_bounds__(kThreads) window_combine_kernel(const float* o
   if (lse != nullptr && lane == 0) lse[id] = last > 0 ? mx + logf(sum) : -INFINITY;
 }
 
-using WindowFn = void (*)(WindowParams);
+using WindowFn = void (*)(WINDOW_HEAD_ARGS, WindowParams);
 
 // Sets of one or two waves: as many as four tiles each leave room for in LDS.
 constexpr int window_sets(int d_v, int nrc) { return d_v == 128 && nrc > 1 ? 3 : 4; }
@@ -1480,7 +1513,8 @@ int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const vo
   if (d->dtype == GVA_DTYPE_F32) fn = d->d_v == 128 ? pick_window_f32<128>(d->d_r) : pick_window_f32<64>(d->d_r);
   long long items = window_blocks(d, n_rows, rows) * S;
   if (S > 1) items = (items + 7) / 8 * 8;
-  hipLaunchKernelGGL(fn, dim3((unsigned)(items * d->n_groups)), dim3(64 * plan.cw * plan.kw), 0, s, p);
+  hipLaunchKernelGGL(fn, dim3((unsigned)(items * d->n_groups)), dim3(64 * plan.cw * plan.kw), 0, s, p.cu, p.lens, p.B, p.G,
+                     p.rows_log2, p.S, p.n_rows, p.t_max, p.split_rows, p);
   st = launch_status();
   if (st != GVA_OK || S == 1) return st;
   if (d->dtype == GVA_DTYPE_BF16) launch_combine<uint16_t>(p, d->d_v, s);
