@@ -43,7 +43,8 @@
  *   on `stream` (a hipStream_t; NULL is the null stream) and returns.
  * - Storage dtype (`dims->dtype`) applies to q, M, the caches and the new
  *   rows: GVA_DTYPE_BF16 (bfloat16) or GVA_DTYPE_F32.  Absorbed queries,
- *   partials and outputs are always fp32.
+ *   partials and outputs are always fp32, but for the outputs of packed queries
+ *   (gva_packed_prefill, gva_tree_attention), which have the storage dtype.
  * - Layouts (B batch, H query heads, G value groups, T = dims->t_max):
  *     q        [B][H][d_c + d_r]   content slice first, then the positional
  *                                  slice, unrotated
@@ -661,7 +662,8 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
  *                takes, slot and row (the position) what gva_append_slots takes: both
  *                skip rows of -1.  Each of the three may be NULL.
  * lens, n_new and n_free are only read, so the call can be repeated with the
- * same result; new_lens, cu_rows and new_n_free must not overlap them.  dims gives
+ * same result; nothing that is written may overlap them, nor block_table and
+ * free_pages each other or what else is written.  dims gives
  * batch (<= 65535) and t_max = max_pages * page_rows; its other entries are
  * checked as everywhere, and not used.
  */
@@ -699,8 +701,8 @@ int gva_append_slots(const gva_dims* dims, const gva_paging* paging, void* v_poo
  * num_splits, split_rows: a sequence's rows are divided as in
  * gva_decode_attention (any plan is right for any lengths).
  * Supported: d_v in {64, 128}, d_c a multiple of 32 (<= 512), d_r one of 8
- * (<= 64), H/G in {1, 2, 4, 8}, n_rows <= 2^20, and what the caches' layout
- * takes.  Others: GVA_ERR_UNSUPPORTED.  Pointers 16-byte aligned (int32 arrays
+ * (<= 64), H/G in {1, 2, 4, 8}, n_rows <= 2^20, T <= 2^30, and what the caches'
+ * layout takes.  Others: GVA_ERR_UNSUPPORTED.  Pointers 16-byte aligned (int32 arrays
  * and lse 4).  The caches are read only.
  * gva_packed_workspace_size -- the bytes of `workspace` that the two attention
  * calls need for the same dims, n_rows and num_splits on the current device:
@@ -751,7 +753,8 @@ int gva_tree_attention(const gva_dims* dims, const gva_paging* paging, const voi
  * max(L_b - n_b, 0) and accepted -1, for trees of more than GVA_MAX_TREE nodes or more than
  * L_b.  bf16 or fp32 caches of any shape that the tiled layout takes, contiguous
  * (paging and block_table NULL) or paged; rows whose page is not in the pool are
- * skipped.  new_lens must not overlap lens.  Not repeatable: the rows have moved.
+ * skipped.  new_lens and accepted must not overlap what is read.  Not repeatable:
+ * the rows have moved.
  */
 int gva_tree_commit(const gva_dims* dims, const gva_paging* paging, void* v_cache, void* kr_cache, const int32_t* block_table,
                     const int32_t* lens, const int32_t* cu_rows, const int32_t* parent, const int32_t* leaf, int32_t n_rows,

@@ -231,6 +231,15 @@ __global__ void __launch_bounds__(kThreads) page_tables_kernel(TablesParams p) {
   if (lane == 0) p.new_n_free[0] = top - given;
 }
 
+// n int32 from p on.
+struct Span {
+  const int32_t* p;
+  long long n;
+};
+bool overlap(const Span& a, const Span& b) {
+  return a.p != nullptr && b.p != nullptr && a.n > 0 && b.n > 0 && a.p < b.p + b.n && b.p < a.p + a.n;
+}
+
 // ================================================================== commit
 // A workgroup per sequence and group, and one more for the positional keys.
 // Every wave holds the parents, four to a lane, walks from the leaf up by lane reads
@@ -345,11 +354,26 @@ int gva_page_tables(const gva_dims* dims, const gva_paging* paging, const int32_
                         (const void*)seq, (const void*)row, (const void*)slot})
     if (!aligned(x, 4)) return GVA_ERR_INVALID_ARG;
   const int B = dims->batch;
-  auto apart = [](const int32_t* a, long long na, const int32_t* c, long long nc) { return a + na <= c || c + nc <= a; };
-  for (const int32_t* in : {lens, n_new})
-    if (!apart(new_lens, B, in, B) || !apart(cu_rows, B + 1, in, B) || !apart(new_n_free, 1, in, B)) return GVA_ERR_INVALID_ARG;
-  if (!apart(new_lens, B, n_free, 1) || !apart(cu_rows, B + 1, n_free, 1) || new_n_free == n_free) return GVA_ERR_INVALID_ARG;
+  const Span small_in[] = {{lens, B}, {n_new, B}, {n_free, 1}}, small_out[] = {{new_lens, B}, {cu_rows, B + 1}, {new_n_free, 1}};
+  for (const Span& in : small_in)
+    for (const Span& out : small_out)
+      if (overlap(in, out)) return GVA_ERR_INVALID_ARG;
   if (B > 65535 || (long long)paging->n_pages * paging->page_rows > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
+  // workgroups read all lengths, and some entries of the table and the stack, while others write
+  const Span large[] = {{block_table, (long long)B * paging->max_pages}, {free_pages, paging->n_pages}};
+  const Span maps[] = {{seq, n_rows}, {row, n_rows}, {slot, n_rows}};
+  if (overlap(large[0], large[1])) return GVA_ERR_INVALID_ARG;
+  for (const Span& map : maps)
+    for (const Span& in : small_in)
+      if (overlap(in, map)) return GVA_ERR_INVALID_ARG;
+  for (const Span& x : large) {
+    for (const Span& map : maps)
+      if (overlap(x, map)) return GVA_ERR_INVALID_ARG;
+    for (const Span& in : small_in)
+      if (overlap(x, in)) return GVA_ERR_INVALID_ARG;
+    for (const Span& out : small_out)
+      if (overlap(x, out)) return GVA_ERR_INVALID_ARG;
+  }
   const long long most = device_cu_count();
   const auto capped = [&](long long n) { return (int)(n < most ? n : most); };
   TablesParams p{lens, n_new, block_table, free_pages, n_free, new_lens, new_n_free, cu_rows, seq, row, slot,
@@ -375,9 +399,13 @@ int gva_tree_commit(const gva_dims* dims, const gva_paging* paging, void* v_cach
   if (!aligned(v_cache, 16) || (dims->d_r > 0 && !aligned(kr_cache, 16)) || !aligned(block_table, 4) || !aligned(lens, 4) ||
       !aligned(cu_rows, 4) || !aligned(parent, 4) || !aligned(leaf, 4) || !aligned(new_lens, 4) || !aligned(accepted, 4))
     return GVA_ERR_INVALID_ARG;
-  if (new_lens < lens + dims->batch && lens < new_lens + dims->batch) return GVA_ERR_INVALID_ARG;
+  const long long B = dims->batch;
+  const Span in[] = {{lens, B}, {cu_rows, B + 1}, {leaf, B}, {parent, n_rows}};
+  if (overlap(in[0], {new_lens, B})) return GVA_ERR_INVALID_ARG;
   st = check_cache_layout(dims);
   if (st != GVA_OK) return st;
+  for (const Span& x : in)                     // a sequence's other workgroups may read them later
+    if (overlap(x, {new_lens, B}) || overlap(x, {accepted, n_rows})) return GVA_ERR_INVALID_ARG;
   const int streams = dims->n_groups + (dims->d_r > 0 ? 1 : 0);
   if (streams > 65535) return GVA_ERR_UNSUPPORTED;
   const int piece = (int)(16 / elem_size(dims));

@@ -4,6 +4,7 @@
 
 #include <cfloat>
 #include <map>
+#include <new>
 #include <type_traits>
 
 #include "gva_window.h"
@@ -254,7 +255,7 @@ __device__ __forceinline__ void copy_run(i32x4 desc, uint32_t dst, int voff, int
   copy_kb<0, NT>(desc, voff, soff);
   if constexpr (N > 1) copy_kb<1024, NT>(desc, voff, soff);
   if constexpr (N > 2) copy_kb<2048, NT>(desc, voff, soff);
-  if constexpr (N > 3) copy_kb<3072, NT>(desc, voff, soff);
+  if constexpr (N > 3) copy_kb<3 * 1024, NT>(desc, voff, soff);
   if constexpr (N > 4) copy_run<N - 4, NT>(desc, dst + 4096, voff, soff + 4096);
 }
 template <int N>
@@ -313,7 +314,7 @@ __device__ __forceinline__ void rotate_quarters(float x0, float x1, double quart
   const float x = (float)(quarters - whole) * 1.57079632679489661923f, z = x * x;
   const float si = x + x * z * fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f);
   const float co = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
-  const int k = (int)whole;
+  const int k = (int)(whole - 4.0 * floor(0.25 * whole));     // of any size: a base below 1 turns fast
   float s = (k & 1) ? co : si, c = (k & 1) ? si : co;
   if (k & 2) s = -s;
   if ((k + 1) & 2) c = -c;
@@ -1387,6 +1388,7 @@ int check_window(const gva_dims* d, const gva_paging* pg, int n_rows, int S, int
   if (hpg != 1 && hpg != 2 && hpg != 4 && hpg != 8) return GVA_ERR_UNSUPPORTED;
   if (d->d_v != 64 && d->d_v != 128) return GVA_ERR_UNSUPPORTED;
   if (d->d_c < 32 || d->d_c % 32 != 0 || d->d_c > 512 || d->d_r % 8 != 0 || d->d_r > 64) return GVA_ERR_UNSUPPORTED;
+  if (d->t_max > (1 << 30)) return GVA_ERR_UNSUPPORTED;         // row + chunk stays below 2^31
   if (n_rows > (1 << 20) || (long long)n_rows * d->n_heads > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   if (n_rows > 0 && window_blocks(d, n_rows, 32 / hpg) * S * d->n_groups > 0x7FFFFFF0LL) return GVA_ERR_UNSUPPORTED;
   return GVA_OK;
@@ -1398,7 +1400,7 @@ int window_len(const gva_dims* d, const int32_t* lens, int b) {
 }
 int window_new(const gva_dims* d, const int32_t* n_new, int n_rows, int b) {
   const int n = n_new == nullptr ? n_rows / d->batch + (b < n_rows % d->batch ? 1 : 0) : n_new[b];
-  return n < 0 ? 0 : n;
+  return n < 0 ? 0 : n > n_rows ? n_rows : n;
 }
 
 // About what a call takes with a plan: its workgroups are dealt in order to
@@ -1498,7 +1500,7 @@ int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const vo
   p.t_max = d->t_max;
   p.n_rows = n_rows;
   p.S = S;
-  p.split_rows = split;
+  p.split_rows = split < (1 << 30) ? split : (1 << 30);
   const int rows = 32 * plan.cw / (d->n_heads / d->n_groups);   // a power of two
   while ((1 << p.rows_log2) < rows) ++p.rows_log2;
   if (pg != nullptr) {
@@ -1539,16 +1541,21 @@ int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int3
   if (split_rows != nullptr) *split_rows = 0;
   if (check_window(dims, nullptr, n_rows, 1, 0) != GVA_OK || n_rows == 0) return 1;
   if (n_cu <= 0) n_cu = device_cu_count();
-  WindowTimes best = window_time(dims, lens, n_new, n_rows, n_cu, 1, 0);
-  int longest = 0;
-  for (int b = 0; b < dims->batch; ++b) {
-    const int L = window_len(dims, lens, b);
-    if (L > longest && window_new(dims, n_new, n_rows, b) > 0) longest = L;
-  }
-  for (int S = 2; S <= 64 && longest / S >= 128; S += S < 8 ? 1 : S / 8) {
-    const int rows = split_rows == nullptr ? 0 : (longest + kTileRows * S - 1) / (kTileRows * S) * kTileRows;
-    const WindowTimes t = window_time(dims, lens, n_new, n_rows, n_cu, S, rows);
-    if (t.us < best.us) best = t;
+  WindowTimes best{0.0, 1, 0};
+  try {
+    best = window_time(dims, lens, n_new, n_rows, n_cu, 1, 0);
+    int longest = 0;
+    for (int b = 0; b < dims->batch; ++b) {
+      const int L = window_len(dims, lens, b);
+      if (L > longest && window_new(dims, n_new, n_rows, b) > 0) longest = L;
+    }
+    for (int S = 2; S <= 64 && longest / S >= 128; S += S < 8 ? 1 : S / 8) {
+      const int rows = split_rows == nullptr ? 0 : (longest + kTileRows * S - 1) / (kTileRows * S) * kTileRows;
+      const WindowTimes t = window_time(dims, lens, n_new, n_rows, n_cu, S, rows);
+      if (t.us < best.us) best = t;
+    }
+  } catch (const std::bad_alloc&) {            // no memory for the list of places: one split is always right
+    best = WindowTimes{0.0, 1, 0};
   }
   if (split_rows != nullptr) *split_rows = best.rows;
   return best.S;

@@ -110,6 +110,7 @@ def test_attention_refusals(call):
     assert call(dims(), S=0) == BAD and call(dims(), S=257) == BAD
     assert call(dims(), rows=16) == BAD and call(dims(), rows=-32) == BAD
     assert call(dims(), n=(1 << 20) + 1) == UNSUP
+    assert call(dims(t_max=(1 << 30) + 32), pg=paging((1 << 30) + 32, 1, 1), table=A) == UNSUP
     need = gva.gva_packed_workspace_size(dims(), 4, 3)
     assert need >= 4 * 8 * 3 * 129 * 4
     assert call(dims(), S=3, ws=None) == BAD and call(dims(), S=3, nb=need - 1) == BAD and call(dims(), S=3, ws=A + 16) == BAD
@@ -117,6 +118,22 @@ def test_attention_refusals(call):
     assert gva.gva_packed_workspace_size(dims(), 0, 3) == 0
     with pytest.raises(gva.GvaError):
         gva.gva_packed_workspace_size(dims(), 4, 0)
+
+
+def test_maps_refuse_overlaps():
+    apart = dict(seq=2 * A, row=3 * A, slot=4 * A, table=5 * A, free=6 * A)
+    reads = (A, A + 4096, A + 8192)                    # lens, n_new, n_free
+    for name in ("seq", "row", "slot"):
+        for at in reads + (5 * A, 6 * A):
+            assert tables_status(dims(), **{**apart, name: at}) == BAD, name
+    for name in ("table", "free"):
+        for at in reads + (A + 12288, A + 16384, A + 20480):
+            assert tables_status(dims(), **{**apart, name: at}) == BAD, name
+    assert tables_status(dims(), **{**apart, "free": 5 * A + 8}) == BAD
+    apart = dict(lens=A, cu=2 * A, parent=3 * A, leaf=4 * A, new=5 * A, acc=6 * A)
+    for name in ("new", "acc"):
+        for at in range(1, 5):
+            assert commit_status(dims(), **{**apart, name: at * A}) == BAD, (name, at)
 
 
 def test_commit_and_slots_shapes():
@@ -135,6 +152,7 @@ def test_plans_are_host_only():
         assert gva.gva_packed_pick_splits(d, lens, torch.tensor(new, dtype=torch.int32), n_cu=256, chunked=False)[1] == 0
     assert gva.gva_packed_pick_splits(d, None, None, 64)[0] > 1          # few queries, long caches
     assert gva.gva_packed_pick_splits(dims(d_v=96), None, None, 64) == (1, 0)
+    assert gva.gva_packed_pick_splits(d, lens, torch.tensor([(1 << 31) - 1] * 4, dtype=torch.int32), 64)[0] >= 1
     with pytest.raises(ValueError):
         gva.packed_plan_for(d, lens[:3], lens)
 
@@ -427,6 +445,37 @@ def test_columns_of_a_workgroup(H, G, d_v, n, tree):
     dev = upload(x)
     for S, rows in ((1, 0), (6, 128)):
         check(x, *call(x, S, rows, dev))
+
+
+# few queries per sequence with wide positional keys: three or four sets of waves
+@gpu
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("n", [3, 8])
+@pytest.mark.parametrize("d_v,d_c,d_r", [(128, 64, 24), (128, 128, 32), (128, 32, 40), (128, 256, 64), (64, 64, 32), (64, 96, 64)])
+def test_sets_of_waves(d_v, d_c, d_r, n, tree):
+    lens, new = [n + 290, 257, n, 640, 30], [n, n - 1, n, n, 0]
+    for R in (0, 32, 160):
+        x = problem(lens, new, 8, 1, d_v, d_c, d_r, 640, R, seed=n + d_r, parent=trees(new, n) if tree else None)
+        note(f"sets {d_v}/{d_c}/{d_r} n={n} R={R} tree={tree}")
+        dev = upload(x)
+        for S, rows in ((1, 0), (3, 128)):
+            check(x, *call(x, S, rows, dev))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bases_below_one(dtype, monkeypatch):
+    """Angles of thousands of millions of quarter turns.  The fastest pair's is 7e9 at the last
+    position, whose roundings (2^-53 of it, three of them) are 2e-6; scores are off by less than
+    4e-5 for it (entries of normal numbers stay below 4), which the bound holds: 2^-17 (bf16) or
+    164 x 2^-24 (fp32) of the sizes of the scores' products, of about 40."""
+    base = 4e-9
+    monkeypatch.setattr(ref, "BASE", base)
+    x = problem([300, 77], [40, 3], 4, 2, 64, 64, 16, 320, seed=5, dtype=dtype)
+    x["d"] = gva.make_dims(2, 4, 2, 64, 64, 16, 320, dtype, rope_base=base)
+    note(f"base {base} {dtype}")
+    for S in (1, 3):
+        check(x, *call(x, S))
 
 
 @gpu
