@@ -1343,13 +1343,23 @@ long long window_blocks(const gva_dims* d, int n_rows, int rows) {
   return (n_rows + seqs * (rows - 1)) / rows;
 }
 
+// Up to 64 columns a sequence on average: sets of one or two waves, as many as fit.
+// More: one set of four, or two of them where there is one split, fewer than 1.5
+// workgroups a CU and room for long sequences.  A second set halves the walk
+// over the keys but doubles the copies of the absorption (causal prompts of up to
+// 2048 rows, 2 sequences, G8 H8 d 64: 37.9 us with two sets, 49.5 with one; d 128
+// 53.3 and 62.3; 1024 rows of d 64 23.5 and 27.7, of d 128 34.9 and 36.3; 256 rows
+// of d 128 23.1 and 19.5; 28 trees of 19 with nothing ahead 29.7 and 19.0).  With
+// several splits the keys are divided already (100 rows behind 8000: 24.0 and 22.9).
 WindowPlan window_plan(const gva_dims* d, int n_rows, int S) {
   const int hpg = d->n_heads / d->n_groups;
   const long long cols = ((long long)n_rows + d->batch - 1) / d->batch * hpg;   // of a sequence, on average
   WindowPlan plan{4, 1, false};
   if (d->dtype == GVA_DTYPE_F32) return {4, 1, true};
   if (cols <= 64) plan = {cols <= 32 ? 1 : 2, window_sets(d->d_v, d->d_r <= 16 ? 1 : 2), false};
-  else if (window_blocks(d, n_rows, 128 / hpg) * d->n_groups * S < device_cu_count() * 3 / 2) plan = {4, 2, false};
+  else if (S == 1 && (long long)d->t_max * 64 / d->d_v >= 1024 &&
+           window_blocks(d, n_rows, 128 / hpg) * d->n_groups < device_cu_count() * 3 / 2)
+    plan = {4, 2, false};
   plan.inside = S == 1 && d->d_c <= 512;
   return plan;
 }
