@@ -1343,9 +1343,14 @@ long long window_blocks(const gva_dims* d, int n_rows, int rows) {
   return (n_rows + seqs * (rows - 1)) / rows;
 }
 
-// Up to 64 columns a sequence on average: sets of one or two waves, as many as fit.
-// More: one set of four, or two of them where there is one split, fewer than 1.5
-// workgroups a CU and room for long sequences.  A second set halves the walk
+// One set of four waves, unless a sequence can be long enough for more sets to pay:
+//  - up to 64 columns a sequence on average: sets of one or two waves, as many as fit,
+//    from 1024 rows on, or from 256 (d 64) or 512 (d 128) while a CU has one workgroup.
+//    The sets need its LDS alone, so of many short sequences they take fewer at a time
+//    (7 nodes, H32 G8 d 64, of up to 64 rows: 96 trees 35.6 us with sets, 21.7 with
+//    one; of up to 512: 48.5 and 43.7, 16 trees 15.6 and 19.9; of up to 1024: 61.1 and
+//    65.5, at d 128 89.0 and 101.9).
+//  - more: two sets of four where there is one split and fewer than 1.5 workgroups a CU.  A second set halves the walk
 // over the keys but doubles the copies of the absorption (causal prompts of up to
 // 2048 rows, 2 sequences, G8 H8 d 64: 37.9 us with two sets, 49.5 with one; d 128
 // 53.3 and 62.3; 1024 rows of d 64 23.5 and 27.7, of d 128 34.9 and 36.3; 256 rows
@@ -1356,10 +1361,12 @@ WindowPlan window_plan(const gva_dims* d, int n_rows, int S) {
   const long long cols = ((long long)n_rows + d->batch - 1) / d->batch * hpg;   // of a sequence, on average
   WindowPlan plan{4, 1, false};
   if (d->dtype == GVA_DTYPE_F32) return {4, 1, true};
-  if (cols <= 64) plan = {cols <= 32 ? 1 : 2, window_sets(d->d_v, d->d_r <= 16 ? 1 : 2), false};
-  else if (S == 1 && (long long)d->t_max * 64 / d->d_v >= 1024 &&
-           window_blocks(d, n_rows, 128 / hpg) * d->n_groups < device_cu_count() * 3 / 2)
+  const long long items = window_blocks(d, n_rows, 128 / hpg) * d->n_groups * S, n_cu = device_cu_count();
+  if (cols <= 64) {
+    if (d->t_max >= (items > n_cu ? 1024 : 4 * d->d_v)) plan = {cols <= 32 ? 1 : 2, window_sets(d->d_v, d->d_r <= 16 ? 1 : 2), false};
+  } else if (S == 1 && d->t_max >= 16 * d->d_v && items < n_cu * 3 / 2) {
     plan = {4, 2, false};
+  }
   plan.inside = S == 1 && d->d_c <= 512;
   return plan;
 }
