@@ -1425,7 +1425,8 @@ int window_new(const gva_dims* d, const int32_t* n_new, int n_rows, int b) {
 // times of a workgroup and of a tile of 32 keys are measured ones (two workgroups
 // of one set a CU at H32 G8 d 128/16: 1.2 us a tile each, 18 us of start and end
 // with the absorption and 9 without; sets of one or two waves, one workgroup a CU:
-// 0.3 and 0.5 us a tile, 17 and 10 us).  A plan of several splits pays for the
+// 0.3 and 0.5 us a tile, 17 and 10 us; fp32: the 136 products of a tile, which fill
+// a CU with one workgroup, 4 us).  A plan of several splits pays for the
 // absorption's launch, the partials' way through memory and their merge.
 struct WindowTimes {
   double us;
@@ -1435,9 +1436,10 @@ WindowTimes window_time(const gva_dims* d, const int32_t* lens, const int32_t* n
   const WindowPlan plan = window_plan(d, n_rows, S);
   const int hpg = d->n_heads / d->n_groups, rows = 32 * plan.cw / hpg;
   const bool f32 = d->dtype == GVA_DTYPE_F32;
-  const double wide = d->d_v / 128.0 * (f32 ? 8.0 : 1.0);
-  const int places = (plan.cw * plan.kw > 4 || plan.cw < 4 ? 1 : 2) * n_cu;
+  const double wide = d->d_v / 128.0;
+  const int places = (f32 || plan.cw * plan.kw > 4 || plan.cw < 4 ? 1 : 2) * n_cu;
   double start = (plan.inside ? 18.0 : 9.0) * (0.5 + 0.5 * d->d_v / 128.0), tile = (plan.cw == 1 ? 0.3 : plan.cw == 2 ? 0.5 : plan.kw == 2 ? 0.8 : 1.2) * wide;
+  if (f32) tile = 4.0 * wide;
   std::map<double, long long> free_at{{0.0, places}};
   double end = 0.0, partials = 0.0;
   int steps = 0;
@@ -1566,7 +1568,7 @@ int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int3
       const int L = window_len(dims, lens, b);
       if (L > longest && window_new(dims, n_new, n_rows, b) > 0) longest = L;
     }
-    for (int S = 2; S <= 64 && longest / S >= 128; S += S < 8 ? 1 : S / 8) {
+    for (int S = 2; S <= 64 && longest / S >= (dims->dtype == GVA_DTYPE_F32 ? 32 : 128); S += S < 8 ? 1 : S / 8) {
       const int rows = split_rows == nullptr ? 0 : (longest + kTileRows * S - 1) / (kTileRows * S) * kTileRows;
       const WindowTimes t = window_time(dims, lens, n_new, n_rows, n_cu, S, rows);
       if (t.us < best.us) best = t;
