@@ -41,7 +41,21 @@ namespace {
 // prompt, a tree's own rows) are masked, and, because 0 x NaN is NaN, their
 // infinities and NaN are set to 0 in LDS after the scores have been taken:
 // a column that sees such a row has the NaN (or infinite) score, one that does
+// a column that sees such a row has the NaN (or infinite) score, one that does
 // not is none the wiser.  Rows past the last key are set to 0 whole.
+//
+// Bound by the matrix cores: the parts of the queries make it 26 products for every
+// 17 of the formulas (d 128/16; 28 for 18 at 128/32).  They run at 1.02 PFLOP/s in
+// 15 K packed prompt rows (484 us, 323 GFLOP of the formulas) and at 1.20 in 860 rows
+// behind up to 32 K (375 us of the kernel), where a library product of 8192 cubed has
+// 1.18: the pipes are busy in 50 and 63% of the cycles, at 1.76 GHz.  Small calls are a chain of latencies: the
+// item, copies, queries, tiles and end of 8 drafts behind 400 rows take 2, 2, 3, 4
+// and 2 us.  A wave has 32 columns and a SIMD two waves, so that one's
+// exponentials run beside the other's products: 64 columns a wave, which halves the
+// LDS reads, leave registers for one wave and took 625 us and more.  Several sets
+// where a sequence has few columns: 16 drafts behind 8 K rows (32 sequences, 549
+// MB) 131 us against 156 with one; of it the loop without its copies takes 80, the
+// copies into LDS add 24, HBM 9.
 struct WindowParams {
   const int32_t* cu;            // [B + 1] packed offsets
   const int32_t* lens;          // [B]
@@ -979,7 +993,7 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
 // leaves q~.  The weights in register r are rows score_row(r, h), and P.V reads
 // those rows' entries from LDS, single ones of 32 columns: the rows of piece k are
 // stored in the order row ^ (k mod 8), so that eight pieces of a row lie in
-// different banks.
+// different banks.  Two prompts of 300 to 1000 rows, H32 G8 d 128/16: 143 us.
 template <int DV, int NRC>
 __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WINDOW_HEAD_ARGS, WindowParams p) {
   const WindowHead hd{WINDOW_HEAD_NAMES};
@@ -1241,8 +1255,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_f32_kernel(WINDOW_HEAD_ARG
 // The merge of the splits of a (row, head), by a wave: the splits' log-sum-exps
 // in one read, four to a lane, then the partials of those with rows, d_v / 4 lanes
 // each, so 2 or 4 splits at a time and four times that in flight.  Rows that no
-// sequence has are left as they were.  Bound by latency: two round trips (one lane
-// row per (row, head), all splits in turn, took 18 us for 4048 of up to 36 splits).
+// sequence has are left as they were.  Bound by latency: two round trips, 8.8 us
+// for 4048 (row, head) of up to 36 splits (18 with one lane row per (row, head), all
+// splits in turn), 19 us for 27 K.
 template <typename T, int DV>
 __global__ void __launch_bounds__(kThreads) window_combine_kernel(const float* o_part, const float* lse_part, const int32_t* cu,
                                                                  T* o, float* lse, int32_t B, int32_t H, int32_t n_rows,
