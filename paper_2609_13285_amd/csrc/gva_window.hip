@@ -649,6 +649,13 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
         ql[c] = *share(1, c);
         q3[c] = *share(2, c);
       }
+      // Sets of one wave meet no other set before a set's third tile is copied over the
+      // parts in its buffers: all of them have been read by then.  (Larger sets meet at
+      // their barriers, which are the workgroup's.)
+      if constexpr (CW == 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        tile_barrier();
+      }
     }
   } else {
     const float* qa = p.q_abs + qrow * DV + 8 * h;
@@ -706,7 +713,7 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
     if (r == 15) l_run += tile_sum;
   };
   // Between the waves of a set, which meet once a tile.  A set of one needs no
-  // barrier: its copies, reads and writes are in order.
+  // barrier: its copies, reads and writes of its own tiles are in order.
   auto set_barrier = [&]() __attribute__((always_inline)) {
     if constexpr (CW > 1) tile_barrier();
     else asm volatile("" ::: "memory");

@@ -1,0 +1,77 @@
+"""The packed calls where they could go wrong without an ordinary test showing it:
+the order of reads and copies in LDS, offsets past 32 bits, the largest sizes,
+plans for other devices, many splits and sequences, values at the ends of their
+types, captured bookkeeping."""
+
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+import packed_ref as ref
+from gpu_helpers import note
+from paper_2609_13285_amd import gva
+from test_packed import call, check, dims, problem, trees, upload
+
+gpu = pytest.mark.gpu
+LLVM = "/opt/rocm/llvm/bin"
+
+
+# ------------------------------------------- sets of one wave share their queries
+def listings(tmp_path, pattern):
+    """{symbol: instructions} of the library's own kernels whose name matches."""
+    lib = shutil.copy(gva.LIB_PATH, tmp_path)
+    subprocess.run([f"{LLVM}/llvm-objdump", "--offloading", lib], check=True, capture_output=True, cwd=tmp_path)
+    out = {}
+    for name in sorted(os.listdir(tmp_path)):
+        if not name.endswith("gfx950"):
+            continue
+        path = os.path.join(tmp_path, name)
+        syms = subprocess.run([f"{LLVM}/llvm-readelf", "-sW", path], check=True, capture_output=True, text=True).stdout
+        for sym in sorted({w for w in syms.split() if re.search(pattern, w) and "." not in w}):
+            text = subprocess.run([f"{LLVM}/llvm-objdump", "-d", f"--disassemble-symbols={sym}", path], check=True,
+                                  capture_output=True, text=True).stdout
+            out[sym] = [x.split("//")[0].strip() for x in text.splitlines() if x.startswith("\t")]
+    return out
+
+
+@pytest.mark.skipif(not os.path.exists(f"{LLVM}/llvm-objdump"), reason="no disassembler")
+def test_shared_queries_are_read_before_copies_overwrite_them(tmp_path):
+    """Sets of one wave pass their queries' parts on through tile buffers: behind the barrier
+    after which they are read, and ahead of the first copy into LDS, there has to be another one
+    that waits for those reads."""
+    found = 0
+    for sym, code in listings(tmp_path, r"window_kernelILi\d+ELi\d+ELi1ELi[34]E").items():
+        d_v = int(re.search(r"window_kernelILi(\d+)E", sym).group(1))
+        parts = 3 * d_v // 16
+        starts = [i for i, x in enumerate(code) if x.startswith("s_barrier")]
+        shared = [i for i in starts if sum(x.startswith("ds_read_b128") for x in code[i + 1:i + 1 + 2 * parts]) >= parts]
+        assert len(shared) == 1, sym
+        rest = code[shared[0] + 1:]
+        end = next(i for i, x in enumerate(rest) if x.startswith("s_barrier") or re.match(r"buffer_load.* lds", x))
+        assert rest[end].startswith("s_barrier"), f"{sym}: {rest[end]}"
+        reads = [i for i, x in enumerate(rest[:end]) if x.startswith("ds_read_b128")]
+        assert len(reads) == parts, sym
+        assert any(x.startswith("s_waitcnt") and "lgkmcnt(0)" in x for x in rest[reads[-1]:end]), sym
+        found += 1
+    assert found == 6                                  # d_v 64 and 128 at three widths of the positional key
+
+
+@gpu
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("d_v,d_r", [(64, 16), (64, 64), (128, 16), (128, 64)])
+def test_sets_of_one_wave_repeat_themselves(d_v, d_r, tree):
+    """Sequences whose sets start a tile apart, or have none, many workgroups at once: bit for bit the same each time."""
+    B = 96
+    lens, new = [(37 * b) % 640 + 1 for b in range(B)], [1 + b % 4 for b in range(B)]
+    x = problem(lens, new, 8, 1, d_v, 64, d_r, 1024, 32, seed=d_v + d_r, parent=trees(new, 3) if tree else None)
+    note(f"sets of one wave {d_v}/{d_r} tree={tree}")
+    dev = upload(x)
+    first = call(x, 1, 0, dev)
+    check(x, *first)
+    for _ in range(20):
+        o, lse = call(x, 1, 0, dev)
+        assert torch.equal(o, first[0]) and torch.equal(lse, first[1])
