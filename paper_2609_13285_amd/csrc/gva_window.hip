@@ -480,16 +480,16 @@ __global__ void __launch_bounds__(64 * CW * KW, CW == 1 ? 1 : 2) window_kernel(W
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)set_lds;
   const int v_voff = (lane >> 4) * 256 + (((lane & 15) ^ (4 * (lane >> 4))) << 4);
   // Where the next tile is: the page's descriptors, which past the last tile
-  // are empty, and the tile's place behind them.
+  // are empty, and the tile's place behind them.  (A stream is below 2 GiB, a page
+  // of G streams may be of any size.)
   const uint32_t v_page = (uint32_t)page_rows * (DV / 8), k_page = (uint32_t)page_rows * (uint32_t)p.d_r / 8;   // 16-byte pieces
-  const uint32_t v_pages = v_page * p.G;
   i32x4 vdesc, kdesc;
   int v_soff, k_soff;
   auto aim = [&]() __attribute__((always_inline)) {
     if (paged && page - id_base >= 64) load_ids();
     const bool in = KW * next_copy + grp < ntiles;
     const uint32_t id = paged ? (uint32_t)__builtin_amdgcn_readlane(ids, min(max(page - id_base, 0), 63)) : (uint32_t)b;
-    const uint64_t va = (uint64_t)(uintptr_t)p.v + (((uint64_t)id * v_pages + (uint32_t)g * v_page) << 4);
+    const uint64_t va = (uint64_t)(uintptr_t)p.v + ((((uint64_t)id * (uint32_t)p.G + (uint32_t)g) * v_page) << 4);
     const uint64_t ka = (uint64_t)(uintptr_t)p.kr + (((uint64_t)id * k_page) << 4);
     vdesc = i32x4{(int)(uint32_t)va, (int)(uint32_t)(va >> 32) & 0xFFFF, in ? (int)(v_page * 16) : 0, kBufferWord3};
     kdesc = i32x4{(int)(uint32_t)ka, (int)(uint32_t)(ka >> 32) & 0xFFFF, in ? (int)(k_page * 16) : 0, kBufferWord3};

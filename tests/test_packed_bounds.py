@@ -75,3 +75,31 @@ def test_sets_of_one_wave_repeat_themselves(d_v, d_r, tree):
     for _ in range(20):
         o, lse = call(x, 1, 0, dev)
         assert torch.equal(o, first[0]) and torch.equal(lse, first[1])
+
+
+# ------------------------------------------------------------- places and sizes
+@gpu
+@pytest.mark.parametrize("tree", [False, True])
+def test_sequences_past_sixty_four_gigabytes(tree):
+    """34 streams of almost 2 GiB each: their offsets in 16-byte pieces pass 2^32 within a sequence and
+    between the two.  Only the rows that the lengths cover are written, or read."""
+    H = G = 34
+    d_v, d_c, d_r, T = 128, 32, 16, (((1 << 31) - (1 << 24)) // 256 - 1) // 32 * 32
+    assert (G - 1) * T * d_v * 2 // 16 > 1 << 32
+    size = 2 * G * T * d_v * 2
+    if torch.cuda.mem_get_info()[0] < size + (4 << 30):
+        pytest.skip("too little memory on this GPU")
+    note(f"sequences of {size >> 31} GiB tree={tree}")
+    v = torch.empty(2, G, T, d_v, dtype=torch.bfloat16, device="cuda")
+    kr = torch.empty(2, T, d_r, dtype=torch.bfloat16, device="cuda")
+    try:
+        for new in ([3, 2], [40, 70]):                 # sets of one wave, and one set of four
+            lens, rows = [new[0] + 30, new[1] + 90], 160
+            x = problem(lens, new, H, G, d_v, d_c, d_r, rows, 0, seed=30 + new[0], parent=trees(new, 2) if tree else None)
+            v[:, :, :rows], kr[:, :rows] = (t.cuda() for t in (gva.tiled(x["v"]), gva.tiled(x["kr"])))
+            x["d"] = gva.make_dims(2, H, G, d_v, d_c, d_r, T, "bf16")
+            for S, split in ((1, 0), (3, 64)):
+                check(x, *call(x, S, split, (v, kr)))
+    finally:
+        del v, kr
+        torch.cuda.empty_cache()
