@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(kThreads) page_tables_kernel(TablesParams p) {
   };
 
   if ((int)blockIdx.x < p.row_blocks) {        // the packed rows
-    for (int i = blockIdx.x * kThreads + tid; i < p.n_rows; i += p.row_blocks * kThreads) {
+    // (unsigned: a step behind the last of 2^31 - 1 rows is past 2^31)
+    for (unsigned i = blockIdx.x * kThreads + tid; i < (unsigned)p.n_rows; i += p.row_blocks * kThreads) {
       int seq = -1, row = -1, slot = -1;
       if (i < s_rows[kThreads]) {
         int lo = 0, hi = kThreads;                         // s_rows[lo] <= i < s_rows[hi]

@@ -14,7 +14,7 @@ import torch
 import packed_ref as ref
 from gpu_helpers import note
 from paper_2609_13285_amd import gva
-from test_packed import call, check, dims, problem, trees, upload
+from test_packed import call, check, dims, ints, problem, trees, upload
 
 gpu = pytest.mark.gpu
 LLVM = "/opt/rocm/llvm/bin"
@@ -102,4 +102,29 @@ def test_sequences_past_sixty_four_gigabytes(tree):
                 check(x, *call(x, S, split, (v, kr)))
     finally:
         del v, kr
+        torch.cuda.empty_cache()
+
+
+@gpu
+def test_maps_of_all_rows_that_an_int_counts():
+    """n_rows = 2^31 - 1: the last rows are written, and nothing around them."""
+    n, pad, R = (1 << 31) - 1, 4097, 32
+    d, pg = dims(batch=3, t_max=4 * R), gva.GvaPaging(R, 4, 12)
+    if torch.cuda.mem_get_info()[0] < 5 * n + (4 << 30):
+        pytest.skip("too little memory on this GPU")
+    note("maps of 2^31 - 1 rows")
+    raw = torch.full((n + 2 * pad,), 7, dtype=torch.int32, device="cuda")
+    lens, new, table, free = [5, 0, 40], [2, 33, -10], [[3, -7, -7, -7], [-7] * 4, [9, 1, -7, -7]], list(range(12))
+    try:
+        out = {k: ints([7] * s) for k, s in (("lens", 3), ("n_free", 1), ("cu", 4))}
+        gva.gva_page_tables(d, pg, ints(lens), ints(new), ints(table), ints(free), ints([6]), out["lens"], out["n_free"], out["cu"],
+                            slot=raw[pad:pad + n])
+        want = ref.page_tables(lens, new, table, free, 6, 64, 4 * R, R, 12)
+        assert all(out[k].tolist() == (want[k] if k != "n_free" else [want[k]]) for k in out)
+        assert raw[pad:pad + 64].tolist() == want["slot"]
+        for part in raw[pad + 64:pad + n].split(1 << 28):
+            assert bool((part == -1).all())
+        assert bool((raw[:pad] == 7).all()) and bool((raw[pad + n:] == 7).all())
+    finally:
+        del raw
         torch.cuda.empty_cache()
