@@ -1360,6 +1360,8 @@ struct WindowPlan {
   bool inside;
 };
 
+bool window_absorbs(const gva_dims* d, int S) { return d->dtype == GVA_DTYPE_F32 || S == 1; }
+
 long long window_blocks(const gva_dims* d, int n_rows, int rows) {
   const long long seqs = d->batch < n_rows ? d->batch : n_rows;
   return (n_rows + seqs * (rows - 1)) / rows;
@@ -1378,18 +1380,17 @@ long long window_blocks(const gva_dims* d, int n_rows, int rows) {
 // 53.3 and 62.3; 1024 rows of d 64 23.5 and 27.7, of d 128 34.9 and 36.3; 256 rows
 // of d 128 23.1 and 19.5; 28 trees of 19 with nothing ahead 29.7 and 19.0).  With
 // several splits the keys are divided already (100 rows behind 8000: 24.0 and 22.9).
-WindowPlan window_plan(const gva_dims* d, int n_rows, int S) {
+WindowPlan window_plan(const gva_dims* d, int n_rows, int S, int n_cu) {
   const int hpg = d->n_heads / d->n_groups;
   const long long cols = ((long long)n_rows + d->batch - 1) / d->batch * hpg;   // of a sequence, on average
-  WindowPlan plan{4, 1, false};
-  if (d->dtype == GVA_DTYPE_F32) return {4, 1, true};
-  const long long items = window_blocks(d, n_rows, 128 / hpg) * d->n_groups * S, n_cu = device_cu_count();
+  WindowPlan plan{4, 1, window_absorbs(d, S)};
+  if (d->dtype == GVA_DTYPE_F32) return plan;
+  const long long items = window_blocks(d, n_rows, 128 / hpg) * d->n_groups * S;
   if (cols <= 64) {
-    if (d->t_max >= (items > n_cu ? 1024 : 4 * d->d_v)) plan = {cols <= 32 ? 1 : 2, window_sets(d->d_v, d->d_r <= 16 ? 1 : 2), false};
-  } else if (S == 1 && d->t_max >= 16 * d->d_v && items < n_cu * 3 / 2) {
-    plan = {4, 2, false};
+    if (d->t_max >= (items > n_cu ? 1024 : 4 * d->d_v)) plan = {cols <= 32 ? 1 : 2, window_sets(d->d_v, d->d_r <= 16 ? 1 : 2), plan.inside};
+  } else if (S == 1 && d->t_max >= 16 * d->d_v && items < (long long)n_cu * 3 / 2) {
+    plan.kw = 2;
   }
-  plan.inside = S == 1 && d->d_c <= 512;
   return plan;
 }
 
@@ -1406,7 +1407,7 @@ WindowLayout window_layout(const gva_dims* d, int n_rows, int S) {
     L.bytes += (bytes + 255) / 256 * 256;
     return at;
   };
-  const bool inside = window_plan(d, n_rows, S).inside;
+  const bool inside = window_absorbs(d, S);
   L.q_abs = take(inside ? 0 : rows * d->d_v * 4);
   L.o_part = take(S > 1 ? rows * S * d->d_v * 4 : 0);
   L.lse_part = take(S > 1 ? rows * S * 4 : 0);
@@ -1455,7 +1456,7 @@ struct WindowTimes {
   int S, rows;
 };
 WindowTimes window_time(const gva_dims* d, const int32_t* lens, const int32_t* n_new, int n_rows, int n_cu, int S, int split) {
-  const WindowPlan plan = window_plan(d, n_rows, S);
+  const WindowPlan plan = window_plan(d, n_rows, S, n_cu);
   const int hpg = d->n_heads / d->n_groups, rows = 32 * plan.cw / hpg;
   const bool f32 = d->dtype == GVA_DTYPE_F32;
   const double wide = d->d_v / 128.0;
@@ -1509,7 +1510,7 @@ int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const vo
     return GVA_ERR_INVALID_ARG;
   const WindowLayout L = window_layout(d, n_rows, S);
   if (L.bytes > 0 && (workspace == nullptr || workspace_bytes < L.bytes || !aligned(workspace, 256))) return GVA_ERR_INVALID_ARG;
-  const WindowPlan plan = window_plan(d, n_rows, S);
+  const WindowPlan plan = window_plan(d, n_rows, S, device_cu_count());
   char* const ws = static_cast<char*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   float* q_abs = plan.inside ? nullptr : reinterpret_cast<float*>(ws + L.q_abs);

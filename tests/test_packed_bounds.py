@@ -128,3 +128,16 @@ def test_maps_of_all_rows_that_an_int_counts():
     finally:
         del raw
         torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------------- plans
+@pytest.mark.parametrize("H,G,T,L,n", [(16, 2, 512, 330, 2), (16, 2, 512, 312, 8), (16, 4, 2048, 1705, 64), (32, 4, 4096, 2235, 32)])
+def test_plans_are_for_the_device_that_they_are_asked_for(H, G, T, L, n):
+    """Four times the sequences on four times the compute units: as many workgroups a unit, so the same kernel and splits.
+    The times that do not scale with the units (partials through memory) are small at these sizes."""
+    plans = []
+    for k in (1, 4):
+        d = dims(batch=16 * k, n_heads=H, n_groups=G, t_max=T)
+        lens, new = (torch.full((16 * k,), x, dtype=torch.int32) for x in (L, n))
+        plans.append(gva.gva_packed_pick_splits(d, lens, new, n_cu=64 * k))
+    assert plans[0] == plans[1]
