@@ -1414,7 +1414,7 @@ WindowLayout window_layout(const gva_dims* d, int n_rows, int S) {
   return L;
 }
 
-int check_window(const gva_dims* d, const gva_paging* pg, int n_rows, int S, int split_rows) {
+int check_window(const gva_dims* d, const gva_paging* pg, int n_rows, int S, int split_rows, int n_cu) {
   const int st = check_dims(d);
   if (st != GVA_OK) return st;
   if (n_rows < 0 || S < 1 || S > GVA_MAX_SPLITS || split_rows < 0 || split_rows % kTileRows != 0) return GVA_ERR_INVALID_ARG;
@@ -1430,7 +1430,12 @@ int check_window(const gva_dims* d, const gva_paging* pg, int n_rows, int S, int
   if (d->d_c < 32 || d->d_c % 32 != 0 || d->d_c > 512 || d->d_r % 8 != 0 || d->d_r > 64) return GVA_ERR_UNSUPPORTED;
   if (d->t_max > (1 << 30)) return GVA_ERR_UNSUPPORTED;         // row + chunk stays below 2^31
   if (n_rows > (1 << 20) || (long long)n_rows * d->n_heads > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
-  if (n_rows > 0 && window_blocks(d, n_rows, 32 / hpg) * S * d->n_groups > 0x7FFFFFF0LL) return GVA_ERR_UNSUPPORTED;
+  if (n_rows > 0) {                            // a launch has fewer than 2^32 threads
+    const WindowPlan plan = window_plan(d, n_rows, S, n_cu);
+    const long long items = (window_blocks(d, n_rows, 32 * plan.cw / hpg) * S + 7) / 8 * 8;
+    if (items * d->n_groups * 64 * plan.cw * plan.kw > 0xFFFFFFFFLL) return GVA_ERR_UNSUPPORTED;
+    if (S > 1 && ((long long)n_rows * d->n_heads + kWaves - 1) / kWaves * kThreads > 0xFFFFFFFFLL) return GVA_ERR_UNSUPPORTED;
+  }
   return GVA_OK;
 }
 
@@ -1500,7 +1505,8 @@ WindowTimes window_time(const gva_dims* d, const int32_t* lens, const int32_t* n
 int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const void* m, const void* v, const void* kr,
                 const int32_t* block_table, const int32_t* lens, const int32_t* cu, const int32_t* parent, int32_t n_rows,
                 int32_t S, int32_t split, void* workspace, size_t workspace_bytes, void* o, float* lse, void* stream) {
-  int st = check_window(d, pg, n_rows, S, split);
+  const int n_cu = device_cu_count();
+  int st = check_window(d, pg, n_rows, S, split, n_cu);
   if (st != GVA_OK) return st;
   if (n_rows == 0) return GVA_OK;
   if (!q || !m || !v || !lens || !cu || !o || (d->d_r > 0 && !kr)) return GVA_ERR_INVALID_ARG;
@@ -1510,7 +1516,7 @@ int window_impl(const gva_dims* d, const gva_paging* pg, const void* q, const vo
     return GVA_ERR_INVALID_ARG;
   const WindowLayout L = window_layout(d, n_rows, S);
   if (L.bytes > 0 && (workspace == nullptr || workspace_bytes < L.bytes || !aligned(workspace, 256))) return GVA_ERR_INVALID_ARG;
-  const WindowPlan plan = window_plan(d, n_rows, S, device_cu_count());
+  const WindowPlan plan = window_plan(d, n_rows, S, n_cu);
   char* const ws = static_cast<char*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   float* q_abs = plan.inside ? nullptr : reinterpret_cast<float*>(ws + L.q_abs);
@@ -1572,7 +1578,7 @@ extern "C" {
 
 int gva_packed_workspace_size(const gva_dims* dims, int32_t n_rows, int32_t num_splits, size_t* bytes) {
   if (bytes == nullptr) return GVA_ERR_INVALID_ARG;
-  const int st = check_window(dims, nullptr, n_rows, num_splits, 0);
+  const int st = check_window(dims, nullptr, n_rows, num_splits, 0, device_cu_count());
   if (st != GVA_OK) return st;
   *bytes = n_rows == 0 ? 0 : window_layout(dims, n_rows, num_splits).bytes;
   return GVA_OK;
@@ -1581,8 +1587,8 @@ int gva_packed_workspace_size(const gva_dims* dims, int32_t n_rows, int32_t num_
 int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int32_t* n_new, int32_t n_rows, int32_t n_cu,
                            int32_t* split_rows) {
   if (split_rows != nullptr) *split_rows = 0;
-  if (check_window(dims, nullptr, n_rows, 1, 0) != GVA_OK || n_rows == 0) return 1;
   if (n_cu <= 0) n_cu = device_cu_count();
+  if (check_window(dims, nullptr, n_rows, 1, 0, n_cu) != GVA_OK || n_rows == 0) return 1;
   WindowTimes best{0.0, 1, 0};
   try {
     best = window_time(dims, lens, n_new, n_rows, n_cu, 1, 0);
@@ -1593,6 +1599,7 @@ int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int3
     }
     for (int S = 2; S <= 64 && longest / S >= (dims->dtype == GVA_DTYPE_F32 ? 32 : 128); S += S < 8 ? 1 : S / 8) {
       const int rows = split_rows == nullptr ? 0 : (longest + kTileRows * S - 1) / (kTileRows * S) * kTileRows;
+      if (check_window(dims, nullptr, n_rows, S, rows, n_cu) != GVA_OK) break;
       const WindowTimes t = window_time(dims, lens, n_new, n_rows, n_cu, S, rows);
       if (t.us < best.us) best = t;
     }

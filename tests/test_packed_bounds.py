@@ -14,7 +14,7 @@ import torch
 import packed_ref as ref
 from gpu_helpers import note
 from paper_2609_13285_amd import gva
-from test_packed import call, check, dims, ints, problem, trees, upload
+from test_packed import BAD, UNSUP, call, check, dims, ints, problem, prompt_status, tree_status, trees, upload
 
 gpu = pytest.mark.gpu
 LLVM = "/opt/rocm/llvm/bin"
@@ -141,3 +141,19 @@ def test_plans_are_for_the_device_that_they_are_asked_for(H, G, T, L, n):
         lens, new = (torch.full((16 * k,), x, dtype=torch.int32) for x in (L, n))
         plans.append(gva.gva_packed_pick_splits(d, lens, new, n_cu=64 * k))
     assert plans[0] == plans[1]
+
+
+@pytest.mark.parametrize("attend", [prompt_status, tree_status])
+def test_calls_of_more_threads_than_a_launch_has_are_refused(attend):
+    """2^32 threads: of the merge (a wave per row and head) and of the attention (a workgroup per block, split and group)."""
+    n = 1 << 20
+    merge = dims(batch=1, n_heads=64, n_groups=64, d_v=64, d_c=32)
+    assert attend(merge, n=n, S=2, lens=None) == UNSUP
+    assert attend(merge, n=n - 1, S=2, lens=None) == BAD           # (a missing pointer, looked for later)
+    blocks = dims(batch=1, n_heads=32, n_groups=32, d_v=64, d_c=32)
+    assert attend(blocks, n=n, S=63, lens=None) == BAD             # 2^13 blocks, 63 splits, 2^5 groups, 2^8 threads
+    for d, S in ((blocks, 64), (dims(batch=1 << 18, n_heads=64, n_groups=64, d_v=64, d_c=32), 1)):
+        assert attend(d, n=n, S=S, lens=None) == UNSUP
+        with pytest.raises(gva.GvaError):
+            gva.gva_packed_workspace_size(d, n, S)
+    assert gva.gva_packed_pick_splits(merge, None, None, n) == (1, 0)
