@@ -701,10 +701,11 @@ int gva_append_slots(const gva_dims* dims, const gva_paging* paging, void* v_poo
  * num_splits, split_rows: a sequence's rows are divided as in
  * gva_decode_attention (any plan is right for any lengths).
  * Supported: d_v in {64, 128}, d_c a multiple of 32 (<= 512), d_r one of 8
- * (<= 64), H/G in {1, 2, 4, 8}, n_rows <= 2^20, T <= 2^30, what the caches'
- * layout takes, and launches of less than 2^32 threads (num_splits n_rows H up to
- * 2^23 always fit).  Others: GVA_ERR_UNSUPPORTED.  Pointers 16-byte aligned (int32
- * arrays and lse 4).  The caches are read only.
+ * (<= 64), H/G in {1, 2, 4, 8}, n_rows <= 2^20, T a multiple of 16 and T rows of
+ * values (of one group) below 2^31 - 2^24 bytes, paged or not (bf16, d_v 64: T < 2^24 -
+ * 2^17), and launches of less than 2^32 threads (num_splits n_rows H up to 2^23 always
+ * fit).  Others: GVA_ERR_UNSUPPORTED.  Pointers 16-byte aligned (int32 arrays and lse
+ * 4).  The caches are read only.
  * gva_packed_workspace_size -- the bytes of `workspace` that the two attention
  * calls need for the same dims, n_rows and num_splits on the current device:
  * scratch, 256-byte aligned (0 bytes: may be NULL).  Calls that run at the same

@@ -1428,7 +1428,6 @@ int check_window(const gva_dims* d, const gva_paging* pg, int n_rows, int S, int
   if (hpg != 1 && hpg != 2 && hpg != 4 && hpg != 8) return GVA_ERR_UNSUPPORTED;
   if (d->d_v != 64 && d->d_v != 128) return GVA_ERR_UNSUPPORTED;
   if (d->d_c < 32 || d->d_c % 32 != 0 || d->d_c > 512 || d->d_r % 8 != 0 || d->d_r > 64) return GVA_ERR_UNSUPPORTED;
-  if (d->t_max > (1 << 30)) return GVA_ERR_UNSUPPORTED;         // row + chunk stays below 2^31
   if (n_rows > (1 << 20) || (long long)n_rows * d->n_heads > 0x7FFFFFFFLL) return GVA_ERR_UNSUPPORTED;
   if (n_rows > 0) {                            // a launch has fewer than 2^32 threads
     const WindowPlan plan = window_plan(d, n_rows, S, n_cu);

@@ -14,7 +14,7 @@ import torch
 import packed_ref as ref
 from gpu_helpers import note
 from paper_2609_13285_amd import gva
-from test_packed import BAD, UNSUP, call, check, dims, ints, problem, prompt_status, tree_status, trees, upload
+from test_packed import A, BAD, UNSUP, call, check, dims, ints, problem, prompt_status, tree_status, trees, upload
 
 gpu = pytest.mark.gpu
 LLVM = "/opt/rocm/llvm/bin"
@@ -157,3 +157,14 @@ def test_calls_of_more_threads_than_a_launch_has_are_refused(attend):
         with pytest.raises(gva.GvaError):
             gva.gva_packed_workspace_size(d, n, S)
     assert gva.gva_packed_pick_splits(merge, None, None, n) == (1, 0)
+
+
+@pytest.mark.parametrize("attend", [prompt_status, tree_status])
+@pytest.mark.parametrize("d_v,dtype,size", [(64, "bf16", 2), (128, "bf16", 2), (64, "f32", 4), (128, "f32", 4)])
+def test_the_longest_capacity(attend, d_v, dtype, size):
+    """T rows of values below 2^31 - 2^24 bytes; paged, with pages of a 32nd of it."""
+    most = ((1 << 31) - (1 << 24)) // (d_v * size)
+    R = most // 32 // 32 * 32
+    for T, pg, want in ((most - 16, None, BAD), (most, None, UNSUP), (32 * (R - 32), gva.GvaPaging(R - 32, 32, 4), BAD),
+                        (32 * (R + 32), gva.GvaPaging(R + 32, 32, 4), UNSUP)):
+        assert attend(dims(d_v=d_v, dtype=dtype, t_max=T), pg=pg, table=A if pg else None, lens=None) == want, (T, pg)
