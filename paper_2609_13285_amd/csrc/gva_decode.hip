@@ -335,7 +335,6 @@ __global__ void __launch_bounds__(128) absorb_f32_kernel(AbsorbParams p) {
   for (int i = threadIdx.x; i < p.d_v; i += blockDim.x) {
     p.q_abs[(int64_t)bh * p.d_v + i] = dot_f32(q, m + (int64_t)i * p.d_c, p.d_c);
   }
-  if (p.q_rot == nullptr) return;
   const int pos = query_pos(p, b);
   for (int i = threadIdx.x; i < p.d_r / 2; i += blockDim.x) {
     double y0, y1;
@@ -1959,12 +1958,8 @@ int absorb_rows(const gva_dims* dims, int n_rows, const void* q, const void* m, 
   // rows of 32 heads take 15.3 us one at a time, 12.7 two at a time
   const int heads = dims->n_heads, want = 2 * device_cu_count();
   p.row_blocks = (long long)heads * ((n_rows + 63) / 64) >= want ? 4 : (long long)heads * ((n_rows + 31) / 32) >= want ? 2 : 1;
-  if (dims->dtype == GVA_DTYPE_BF16) {
-    const int per = 16 * p.row_blocks;
-    hipLaunchKernelGGL(absorb_bf16_kernel, dim3(dims->n_heads, (n_rows + per - 1) / per), dim3(kThreads), 0, stream, p);
-  } else {
-    hipLaunchKernelGGL(absorb_f32_kernel, dim3((unsigned)((long long)n_rows * dims->n_heads)), dim3(128), 0, stream, p);
-  }
+  const int per = 16 * p.row_blocks;
+  hipLaunchKernelGGL(absorb_bf16_kernel, dim3(dims->n_heads, (n_rows + per - 1) / per), dim3(kThreads), 0, stream, p);
   return launch_status();
 }
 
