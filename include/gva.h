@@ -634,27 +634,34 @@ int gva_evict_rows(const gva_dims* dims, int32_t n_keep, int32_t n_first, int32_
  * A step is gva_page_tables for the rows to come, gva_append_slots for their
  * values and keys, gva_packed_prefill or gva_tree_attention for their queries
  * (or gva_paged_decode_attention where every sequence has one), and after a tree
- * gva_tree_commit and gva_page_tables with what the tree has lost.
+ * gva_tree_commit and gva_page_tables with what the tree has lost.  A sequence
+ * that was refused its rows (new_lens[b] = lens[b], n_new[b] > 0) has others at its
+ * end: what its queries in the step get means nothing, and gva_tree_commit would
+ * take those rows for the tree's, so it gets offsets (cu_rows, parent) without it.
  */
 
 /*
  * gva_page_tables -- block tables and slot maps from the requests' lengths.
  * n_new[b] rows are to join sequence b, or, where it is negative, -n_new[b] of
- * its last rows to go (all of them: it has ended), with lens[b] before the call
- * (n_new is read as clamped to [-lens[b], T]).  With pages(x) = ceil(x /
- * page_rows) a sequence holds block_table[b][0 .. pages(lens[b]) - 1], and the
- * stack free_pages [n_pages], of n_free[0] entries, the pages that none holds.
+ * its last rows to go (all of them: it has ended), with lens[b] before the call.
+ * n_new is read as clamped to [-lens[b], T]: more than T is cut to T, which an empty
+ * sequence may be granted, and the packed offsets behind it count T, so counts that
+ * rows are packed by have to be T at most.  With pages(x) = ceil(x / page_rows) a
+ * sequence holds block_table[b][0 .. pages(lens[b]) - 1], and the stack free_pages
+ * [n_pages], of n_free[0] entries, the pages that none holds.
  *   back   the pages of rows that go are put on the stack, in order of sequence
  *          and page; of a page some rows of which stay, nothing changes
  *   grant  then the sequences that grow take theirs from its top, in order of
  *          sequence and page.  Nobody overtakes: a sequence gets its pages if it
  *          needs none, or if the stack holds what it and all growing ones before
- *          it need.  One that would pass T rows gets none and counts for none.
+ *          it need.  One that would pass T rows, as n_new is read, gets none and
+ *          counts for none.
  * Written: the entries of new pages in block_table (others are left as they
  * were), free_pages, new_n_free[0], and
  *   new_lens[b]  lens[b] + n_new[b], or lens[b] where nothing was granted
  *   cu_rows      the packed offsets of the rows to come, max(n_new, 0) of each
- *                sequence whether granted or not (at most n_rows)
+ *                sequence whether granted or not, at most n_rows (rows past n_rows are
+ *                granted all the same, and have no entry in the maps)
  *   seq, row, slot [n_rows]  of each packed row its sequence (-1 past the last),
  *                its row in it, from lens[b] on, and its slot; row and slot are -1
  *                where nothing was granted, and so is the slot where the table names
@@ -692,7 +699,9 @@ int gva_append_slots(const gva_dims* dims, const gva_paging* paging, void* v_poo
  *   lse[r][h] = log sum_t exp(x_t)                      fp32; lse may be NULL
  * Queries with p < 0 get o = 0, lse = -inf; rows of o and lse that no sequence
  * has are left as they were.  An infinity or a NaN in a row that a query does not
- * see does not reach it.
+ * see does not reach it.  In one that it sees, a score of NaN or +inf makes its o and
+ * lse NaN; with a score of -inf the row draws no weight, but o and lse may be NaN (an
+ * infinity times the parts that a bf16 query enters as, or times a weight of 0).
  * o is in the storage dtype, half of the bytes, because what follows a prompt's
  * rows is a matrix product in that type.  bf16: the queries enter the products
  * as bf16 high + low pairs, the softmax weights as bf16 (off by at most 2^-8 each,
