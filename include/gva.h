@@ -723,7 +723,8 @@ int gva_append_slots(const gva_dims* dims, const gva_paging* paging, void* v_poo
  * counts of new rows in the HOST arrays lens and n_new [B] (NULL: every sequence
  * t_max; n_rows shared evenly), on a device with n_cu compute units (0 = ask the
  * current device).  Returns num_splits, and in split_rows what to pass with it
- * (NULL: even splits only); 1 for dims that the calls do not take.  Pure host code.
+ * (NULL: even splits only); 1 for dims that the calls do not take.  Pure host code;
+ * about a millisecond for 64 sequences, 12 for 512, so for plans that are kept.
  */
 int gva_packed_workspace_size(const gva_dims* dims, int32_t n_rows, int32_t num_splits, size_t* bytes);
 int gva_packed_pick_splits(const gva_dims* dims, const int32_t* lens, const int32_t* n_new, int32_t n_rows, int32_t n_cu,

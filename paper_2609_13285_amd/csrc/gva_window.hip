@@ -16,8 +16,9 @@ namespace {
 // last n_b cached rows; P = L_b - n_b rows are before them.  A workgroup takes
 // 32 CW (row, head) columns of one group, 32 CW / hpg consecutive rows times
 // the H/G heads that share the group's value rows, and one split of the keys.
-// Its 4 (or 8) waves are KW sets of CW: a set walks every KW-th tile of 32
-// keys, a wave of it scores its own 32 columns; the sets are merged at the end.
+// Its waves are KW sets of CW (one or two of four, three or four of one or two):
+// a set walks every KW-th tile of 32 keys, a wave of it scores its own 32 columns;
+// the sets are merged at the end.
 //
 // Per tile, on 32x32x16 products (lane = column, registers = rows):
 //  - the tile's value and positional-key rows go straight to LDS, copied by the
@@ -41,7 +42,6 @@ namespace {
 // prompt, a tree's own rows) are masked, and, because 0 x NaN is NaN, their
 // infinities and NaN are set to 0 in LDS after the scores have been taken:
 // a column that sees such a row has the NaN (or infinite) score, one that does
-// a column that sees such a row has the NaN (or infinite) score, one that does
 // not is none the wiser.  Rows past the last key are set to 0 whole.
 //
 // Bound by the matrix cores: the parts of the queries make it 26 products for every
@@ -54,8 +54,8 @@ namespace {
 // exponentials run beside the other's products: 64 columns a wave, which halves the
 // LDS reads, leave registers for one wave and took 625 us and more.  Several sets
 // where a sequence has few columns: 16 drafts behind 8 K rows (32 sequences, 549
-// MB) 131 us against 156 with one; of it the loop without its copies takes 80, the
-// copies into LDS add 24, HBM 9.
+// MB) 131 us against 156 with one (131 to 136 on different GPUs); of it the loop
+// without its copies takes 80, the copies into LDS add 24, HBM 9.
 struct WindowParams {
   const int32_t* cu;            // [B + 1] packed offsets
   const int32_t* lens;          // [B]
@@ -1367,7 +1367,10 @@ long long window_blocks(const gva_dims* d, int n_rows, int rows) {
   return (n_rows + seqs * (rows - 1)) / rows;
 }
 
-// One set of four waves, unless a sequence can be long enough for more sets to pay:
+// One set of four waves, unless a sequence can be long enough for more sets to pay.
+// The lengths are on the device, so this goes by the capacity T and by the average
+// of n_rows: the times below are of caches cut to their sequences, and short sequences
+// in caches of many rows get the sets whether they pay or not:
 //  - up to 64 columns a sequence on average: sets of one or two waves, as many as fit,
 //    from 1024 rows on, or from 256 (d 64) or 512 (d 128) while a CU has one workgroup.
 //    The sets need its LDS alone, so of many short sequences they take fewer at a time
@@ -1455,6 +1458,9 @@ int window_new(const gva_dims* d, const int32_t* n_new, int n_rows, int b) {
 // 0.3 and 0.5 us a tile, 17 and 10 us; fp32: the 136 products of a tile, which fill
 // a CU with one workgroup, 4 us).  A plan of several splits pays for the
 // absorption's launch, the partials' way through memory and their merge.
+// On the host 0.08 ms for 8 sequences, 1 for 64, 11 to 12 for 512, 16 to 18 for 1024
+// (30 candidates; lengths of 1 K to 16 K): for plans that are kept over many steps.
+// A candidate is dealt for 20000 steps, what is left of it then counts as nothing.
 struct WindowTimes {
   double us;
   int S, rows;
